@@ -1,4 +1,4 @@
-"""Build libpase.so (host planner + gfx950 kernels) in-tree with hipcc.
+"""Build libpase.so (host planner, gfx950 kernels, layer operators) in-tree with hipcc.
 
 The sources are compiled to objects in parallel, then linked."""
 from __future__ import annotations
@@ -16,11 +16,15 @@ ARCH = "gfx950"
 # Every HIP compile disables packed FP32 instruction selection (no v_pk_*_f32).
 HIP_FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-             "-fno-honor-nans", "-Wall", "-Wno-unused-function"]
+             "-Wall", "-Wno-unused-function"]
+# The search's keys are never NaN; the layer operators pass NaN on.
+SEARCH_FLAGS = ["-fno-honor-nans"]
+SEARCH = ("host.cpp", "launch_plan.cpp", "assign.cpp", "device.hip")
+OPERATORS = ("operators.cpp", "layer_norm.hip", "softmax_loss.hip", "grouped_matmul.hip")
 
 
 def sources():
-    return [os.path.join(CSRC, f) for f in ("host.cpp", "launch_plan.cpp", "assign.cpp", "device.hip")]
+    return [os.path.join(CSRC, f) for f in SEARCH + OPERATORS]
 
 
 def build(verbose: bool = False, out: str = LIB, extra=()) -> str:
@@ -29,7 +33,8 @@ def build(verbose: bool = False, out: str = LIB, extra=()) -> str:
     objs, procs = [], []
     for src in sources():
         obj = out + "." + os.path.splitext(os.path.basename(src))[0] + ".o"
-        cmd = [hipcc, *HIP_FLAGS, *inc, "-c", src, "-o", obj, *extra]
+        flags = SEARCH_FLAGS if os.path.basename(src) in SEARCH else []
+        cmd = [hipcc, *HIP_FLAGS, *flags, *inc, "-c", src, "-o", obj, *extra]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((subprocess.Popen(cmd), cmd))
@@ -48,7 +53,7 @@ def build(verbose: bool = False, out: str = LIB, extra=()) -> str:
     return out
 
 
-# Host-only build of the planner (host.cpp, launch_plan.cpp, assign.cpp) with a stub
+# Host-only build of the planner and of the operators' argument checks with a stub
 # device runtime, under AddressSanitizer and UBSan, for the CPU test suite.
 # The GPU library is never built this way: this is g++ on host sources only.
 SAN_LIB = os.path.join(ROOT, "_build", "libpase_host_san.so")
@@ -58,7 +63,7 @@ SAN_FLAGS = ["-O1", "-g", "-std=c++17", "-fPIC", "-shared", "-fno-omit-frame-poi
 
 def build_host_sanitized(out: str = SAN_LIB, verbose: bool = False) -> str:
     os.makedirs(os.path.dirname(out), exist_ok=True)
-    srcs = [os.path.join(CSRC, f) for f in ("host.cpp", "launch_plan.cpp", "assign.cpp", "device_stub.cpp")]
+    srcs = [os.path.join(CSRC, f) for f in ("host.cpp", "launch_plan.cpp", "assign.cpp", "operators.cpp", "device_stub.cpp")]
     cmd = [os.environ.get("CXX", "g++"), *SAN_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            *srcs, "-o", out + ".tmp"]
     if verbose:

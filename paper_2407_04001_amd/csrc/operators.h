@@ -1,0 +1,80 @@
+// Arguments of the layer operators, between the checks of operators.cpp (host)
+// and the launches in layer_norm.hip, softmax_loss.hip and grouped_matmul.hip.
+#pragma once
+
+#include <cstdint>
+
+#include "pase_operators.h"
+
+namespace pase {
+
+struct NormForward {
+    int dtype, param_dtype;
+    int64_t rows;
+    int width;
+    const void *x, *residual, *gain, *bias;
+    void *y, *z;
+    int64_t ldx, ldr, ldy, ldz;
+    float *mean, *rstd;
+    float eps;
+};
+
+struct NormBackward {
+    int dtype, param_dtype;
+    int64_t rows;
+    int width;
+    const void *dy, *z, *dz, *gain;
+    const float *mean, *rstd;
+    void *dx, *dgain, *dbias;
+    int64_t lddy, ldz, lddz, lddx;
+    float *partial;      // [blocks][2][width]: the blocks' sums of dgain and dbias
+    int blocks;
+};
+
+struct SoftmaxLoss {
+    int dtype, targets_64;
+    int64_t rows, classes;
+    const void *logits, *targets;
+    int64_t ldl, ignore;
+    const float *dloss;
+    int64_t dloss_stride;
+    float *loss, *lse;
+    void *dlogits;
+    int64_t lddl;
+    float *partial;      // [rows][splits][2]: the chunks' maxima and sums
+    int splits;          // workgroups sharing a row (1: a row is one workgroup's)
+};
+
+// c[m][j] = sum over the contraction of a and b; see grouped_matmul.hip for
+// what rows, n and k are in each direction.
+struct GroupedProduct {
+    int dtype, out_dtype, offsets_64;
+    int64_t rows;
+    int groups, n, k;    // w: groups x n x k
+    const void *x, *w, *dy, *offsets;
+    void *out;
+    int64_t ldx, lddy, ldo;
+    float *partial;      // weight gradient: [splits][groups][n][k] when splits > 1
+    int splits;
+};
+
+// blocks of the layer norm's backward pass (one row of partial sums each)
+int norm_backward_blocks(int dtype, int64_t rows, int width);
+// workgroups that share a row of the softmax loss
+int softmax_loss_splits(int dtype, int64_t rows, int64_t classes);
+// parts each group's rows are cut into by the weights' gradient
+int grouped_matmul_splits(int64_t rows, int groups, int n, int k);
+
+constexpr int kGradVecs = 1024;   // 16-byte vectors of a row that one workgroup of the loss gradient takes
+
+// Launches: 0 or a hipError_t.
+int launch_norm_forward(const NormForward &a, void *stream);
+int launch_norm_backward(const NormBackward &a, void *stream);
+int launch_softmax_loss(const SoftmaxLoss &a, void *stream);            // loss and lse; dlogits unless null
+int launch_softmax_loss_backward(const SoftmaxLoss &a, void *stream);   // dlogits from lse
+int launch_product_forward(const GroupedProduct &a, void *stream);
+int launch_product_rows_grad(const GroupedProduct &a, void *stream);
+int launch_product_weights_grad(const GroupedProduct &a, void *stream);
+const char *launch_error(int e);
+
+}  // namespace pase

@@ -1,0 +1,217 @@
+// Softmax loss of rows of logits, its gradient, and both in one pass
+// (pase_operators.h).
+//
+// With m the row's maximum, lse = m + ln sum exp(l - m): no exponent is
+// positive, so nothing overflows.  A row that fits is held in one workgroup's
+// registers as it was read, so that the maximum, the sum and the gradient take
+// one pass over HBM; a longer one is read again, its maximum and sum formed
+// together on the first pass (a sum of terms exp(l - m) grows by the factor
+// exp(m - m') when the maximum moves to m').
+// Bound by HBM: the logits read once, the gradient written once.
+#include "operators.h"
+#include "vectors.h"
+
+namespace pase {
+namespace {
+
+template <typename T> __device__ __forceinline__ T masked() {
+    return (T)(-__builtin_inff());
+}
+
+__device__ __forceinline__ int64_t target_of(const SoftmaxLoss &a, int64_t row) {
+    return a.targets_64 ? static_cast<const int64_t *>(a.targets)[row]
+                        : (int64_t) static_cast<const int32_t *>(a.targets)[row];
+}
+
+// The row's lse from its maximum and sum, and its loss.  sum is 0 exactly when
+// every class is masked (otherwise the maximum's own term is 1 or NaN).
+__device__ __forceinline__ float row_lse(float top, float sum) {
+    return sum == 0.0f ? -__builtin_inff() : top + logf(sum);
+}
+
+template <typename T>
+__device__ __forceinline__ float row_loss(const T *logits, int64_t classes, int64_t target, float lse) {
+    if (target < 0 || target >= classes) return __builtin_nanf("");
+    return lse == -__builtin_inff() ? __builtin_inff() : lse - (float)logits[target];
+}
+
+// Gradient of one vector: (exp(l - lse) - [target]) * scale, where scale is 0 for
+// a row with every class masked and NaN for a target out of range.
+template <typename T>
+__device__ __forceinline__ void grad_pack(T *out, int64_t at, int64_t n, const Pack<T> &l, float lse, int64_t target,
+                                          float scale) {
+    if (n <= 0) return;
+    Pack<T> o;
+    const int64_t hit = target - at;
+#pragma unroll
+    for (int j = 0; j < kVec<T>; j++) {
+        float p = __expf((float)l.e[j] - lse);
+        if (j == hit) p -= 1.0f;
+        o.e[j] = (T)(p * scale);
+    }
+    store_pack(out + at, n, o);
+}
+
+struct RowGrad {
+    float lse, scale;
+};
+
+__device__ __forceinline__ RowGrad row_grad(const SoftmaxLoss &a, int64_t row, int64_t target, float lse) {
+    const float g = a.dloss[row * a.dloss_stride];
+    if (target < 0 || target >= a.classes) return {lse, __builtin_nanf("")};
+    // every class masked: any finite lse makes exp(-inf - lse) = 0, and the scale takes the target's -1 away
+    if (lse == -__builtin_inff()) return {0.0f, 0.0f};
+    return {lse, g};
+}
+
+template <typename T> __device__ __forceinline__ void zero_row(T *out, int64_t classes, int threads) {
+    Pack<T> zero;
+    zero.v = 0;
+    for (int64_t at = (int64_t)threadIdx.x * kVec<T>; at < classes; at += (int64_t)threads * kVec<T>)
+        store_pack(out + at, classes - at, zero);
+}
+
+// One row a workgroup of WAVES waves, NV vectors a lane.
+template <typename T, int NV, int WAVES, bool GRAD>
+__global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
+    constexpr int V = kVec<T>, THREADS = WAVES * 64;
+    __shared__ float lds[2 * WAVES];
+    const int64_t row = blockIdx.x;
+    const T *logits = static_cast<const T *>(a.logits) + row * a.ldl;
+    T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
+    const int64_t target = target_of(a, row);
+    if (target == a.ignore) {
+        if (threadIdx.x == 0) a.loss[row] = 0, a.lse[row] = 0;
+        if (GRAD) zero_row(out, a.classes, THREADS);
+        return;
+    }
+    Pack<T> l[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int64_t at = (int64_t)(threadIdx.x + i * THREADS) * V;
+        l[i] = load_pack(logits + at, a.classes - at, masked<T>());
+    }
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int j = 0; j < V; j++) top = fmaxf(top, (float)l[i].e[j]);
+    top = group_max<WAVES>(top, lds);
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+    float s[1] = {0};
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int j = 0; j < V; j++) s[0] += __expf((float)l[i].e[j] - from);
+    group_sum<WAVES>(s, lds + WAVES);
+    const float lse = row_lse(top, s[0]);
+    if (threadIdx.x == 0) a.loss[row] = row_loss(logits, a.classes, target, lse), a.lse[row] = lse;
+    if (GRAD) {
+        // in place, the target's logit is read above before its own lane writes it
+        __syncthreads();
+        const RowGrad g = row_grad(a, row, target, lse);
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const int64_t at = (int64_t)(threadIdx.x + i * THREADS) * V;
+            grad_pack(out, at, a.classes - at, l[i], g.lse, target, g.scale);
+        }
+    }
+}
+
+// A row longer than the registers of a workgroup hold.
+template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_long(SoftmaxLoss a) {
+    constexpr int V = kVec<T>, WAVES = 16, THREADS = 1024;
+    __shared__ float lds[2 * WAVES];
+    const int64_t row = blockIdx.x;
+    const T *logits = static_cast<const T *>(a.logits) + row * a.ldl;
+    T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
+    const int64_t target = target_of(a, row);
+    if (target == a.ignore) {
+        if (threadIdx.x == 0) a.loss[row] = 0, a.lse[row] = 0;
+        if (GRAD) zero_row(out, a.classes, THREADS);
+        return;
+    }
+    float top = -__builtin_inff(), from = 0.0f, sum = 0.0f;
+    for (int64_t at = (int64_t)threadIdx.x * V; at < a.classes; at += (int64_t)THREADS * V) {
+        const Pack<T> l = load_pack(logits + at, a.classes - at, masked<T>());
+        float t = top;
+#pragma unroll
+        for (int j = 0; j < V; j++) t = fmaxf(t, (float)l.e[j]);
+        if (t > top) {
+            sum *= __expf(top - t);   // top is -inf only while the sum is 0 or NaN
+            top = from = t;
+        }
+#pragma unroll
+        for (int j = 0; j < V; j++) sum += __expf((float)l.e[j] - from);
+    }
+    const float all = group_max<WAVES>(top, lds);
+    float s[1] = {top == -__builtin_inff() ? sum : sum * __expf(top - all)};
+    group_sum<WAVES>(s, lds + WAVES);
+    const float lse = row_lse(all, s[0]);
+    if (threadIdx.x == 0) a.loss[row] = row_loss(logits, a.classes, target, lse), a.lse[row] = lse;
+    if (GRAD) {
+        __syncthreads();
+        const RowGrad g = row_grad(a, row, target, lse);
+        for (int64_t at = (int64_t)threadIdx.x * V; at < a.classes; at += (int64_t)THREADS * V) {
+            const Pack<T> l = load_pack(logits + at, a.classes - at, masked<T>());
+            grad_pack(out, at, a.classes - at, l, g.lse, target, g.scale);
+        }
+    }
+}
+
+// Gradient from the lse: 256 threads take 4 vectors each of one row.
+template <typename T> __global__ __launch_bounds__(256) void k_loss_grad(SoftmaxLoss a, int chunks) {
+    constexpr int V = kVec<T>;
+    const int64_t row = blockIdx.x / chunks, at0 = (int64_t)(blockIdx.x % chunks) * kGradVecs * V + threadIdx.x * V;
+    const T *logits = static_cast<const T *>(a.logits) + row * a.ldl;
+    T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
+    const int64_t target = target_of(a, row);
+    const bool ignored = target == a.ignore;
+    const RowGrad g = row_grad(a, row, target, a.lse[row]);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int64_t at = at0 + (int64_t)i * 256 * V, n = a.classes - at;
+        if (n <= 0) return;
+        if (ignored) {
+            Pack<T> zero;
+            zero.v = 0;
+            store_pack(out + at, n, zero);
+        } else {
+            grad_pack(out, at, n, load_pack(logits + at, n, masked<T>()), g.lse, target, g.scale);
+        }
+    }
+}
+
+template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *stream) {
+    const int64_t vecs = (a.classes + kVec<T> - 1) / kVec<T>;
+    if (vecs <= 256) return launch(k_loss_row<T, 4, 1, GRAD>, a.rows, 64, stream, a);
+    if (vecs <= 1024) return launch(k_loss_row<T, 4, 4, GRAD>, a.rows, 256, stream, a);
+    if (vecs <= 4096) return launch(k_loss_row<T, 8, 8, GRAD>, a.rows, 512, stream, a);
+    if (vecs <= 16384) return launch(k_loss_row<T, 16, 16, GRAD>, a.rows, 1024, stream, a);
+    return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
+}
+
+template <typename T> int loss_typed(const SoftmaxLoss &a, void *stream) {
+    return a.dlogits ? loss_rows<T, true>(a, stream) : loss_rows<T, false>(a, stream);
+}
+
+template <typename T> int grad_typed(const SoftmaxLoss &a, void *stream) {
+    const int chunks = (int)((a.classes + kGradVecs * kVec<T> - 1) / (kGradVecs * kVec<T>));
+    return launch(k_loss_grad<T>, a.rows * chunks, 256, stream, a, chunks);
+}
+
+}  // namespace
+
+int launch_softmax_loss(const SoftmaxLoss &a, void *stream) {
+    if (a.dtype == PASE_BF16) return loss_typed<__bf16>(a, stream);
+    if (a.dtype == PASE_FP16) return loss_typed<_Float16>(a, stream);
+    return loss_typed<float>(a, stream);
+}
+
+int launch_softmax_loss_backward(const SoftmaxLoss &a, void *stream) {
+    if (a.dtype == PASE_BF16) return grad_typed<__bf16>(a, stream);
+    if (a.dtype == PASE_FP16) return grad_typed<_Float16>(a, stream);
+    return grad_typed<float>(a, stream);
+}
+
+}  // namespace pase

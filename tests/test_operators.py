@@ -1,0 +1,142 @@
+"""Argument checks of the layer operators (no GPU): every refusal is made on the
+host before anything is enqueued, so the pointers here are never followed."""
+import ctypes as C
+import os
+import re
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20          # an address nobody follows, aligned to anything
+BF16, FP16, FP32 = range(3)
+OK, INVALID, TOO_LARGE, OUT_OF_MEMORY = 0, 1, 5, 6
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2407_04001_amd import ops
+    return ops.load()
+
+
+def test_every_declared_operator_is_exported(lib):
+    from paper_2407_04001_amd import ops
+    header = open(os.path.join(ROOT, "include", "pase_operators.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = set(re.findall(r"\b(pase_[a-z_]+)\s*\(", header))
+    assert declared == set(ops.EXPORTS)
+    for name in declared:
+        assert hasattr(lib, name), name
+
+
+NORM_F = dict(dtype=BF16, param=BF16, rows=4, width=8, x=P, ldx=8, res=P, ldr=8, gain=P, bias=P, eps=1e-5, y=P, ldy=8,
+              z=P, ldz=8, mean=P, rstd=P, stream=None)
+NORM_B = dict(dtype=BF16, param=BF16, rows=4, width=8, dy=P, lddy=8, z=P, ldz=8, dz=P, lddz=8, gain=P, mean=P, rstd=P,
+              dx=2 * P, lddx=8, dgain=P, dbias=P, ws=P, ws_bytes=1 << 20, stream=None)
+PROD_F = dict(dtype=BF16, out=BF16, rows=4, groups=2, n=8, k=8, x=P, ldx=8, w=P, offsets=P, off64=0, y=P, ldy=8,
+              stream=None)
+PROD_B = dict(dtype=BF16, grad=BF16, rows=4, groups=2, n=8, k=8, dy=P, lddy=8, x=P, ldx=8, w=P, offsets=P, off64=0,
+              dx=P, lddx=8, dw=P, ws=P, ws_bytes=1 << 20, stream=None)
+LOSS_F = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, loss=P, lse=P, ws=P,
+              ws_bytes=1 << 20, stream=None)
+LOSS_G = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, dloss=P, step=1, loss=P,
+              lse=P, dlogits=2 * P, lddl=8, ws=P, ws_bytes=1 << 20, stream=None)
+LOSS_B = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, lse=P, dloss=P, step=1,
+              dlogits=2 * P, lddl=8, stream=None)
+
+REFUSALS = [
+    ("pase_layer_norm_forward", NORM_F, INVALID, [
+        dict(dtype=3), dict(dtype=-1), dict(param=FP16), dict(width=0), dict(eps=-1.0), dict(eps=float("nan")),
+        dict(x=None), dict(x=P + 1), dict(ldx=7), dict(ldx=1 << 33), dict(ldr=7), dict(res=P + 1), dict(z=None),
+        dict(gain=None), dict(gain=P + 1), dict(bias=P + 1), dict(param=FP32, bias=P + 2), dict(y=None), dict(ldy=7),
+        dict(ldz=7), dict(mean=None), dict(rstd=None), dict(rstd=P + 2)]),
+    ("pase_layer_norm_forward", NORM_F, TOO_LARGE, [dict(width=16385, ldx=16385), dict(rows=1 << 41)]),
+    ("pase_layer_norm_backward", NORM_B, INVALID, [
+        dict(dtype=3), dict(param=FP16), dict(width=0), dict(dy=None), dict(lddy=7), dict(z=None), dict(ldz=7),
+        dict(lddz=7), dict(dx=None), dict(lddx=7), dict(gain=None), dict(mean=None), dict(rstd=P + 1),
+        dict(dgain=P + 1), dict(dbias=P + 1), dict(ws=None), dict(ws=P + 8), dict(dx=P, lddx=9)]),
+    ("pase_layer_norm_backward", NORM_B, OUT_OF_MEMORY, [dict(ws_bytes=0), dict(ws_bytes=8)]),
+    ("pase_grouped_matmul_forward", PROD_F, INVALID, [
+        dict(dtype=FP32), dict(dtype=7), dict(out=FP16), dict(groups=0), dict(n=0), dict(k=0), dict(x=None),
+        dict(x=P + 1), dict(ldx=7), dict(ldx=(1 << 22) + 1), dict(w=None), dict(offsets=None), dict(offsets=P + 2),
+        dict(off64=1, offsets=P + 4), dict(off64=2), dict(y=None), dict(ldy=7), dict(ldy=(1 << 22) + 1),
+        dict(out=FP32, y=P + 2)]),
+    ("pase_grouped_matmul_forward", PROD_F, TOO_LARGE, [
+        dict(groups=65537), dict(n=(1 << 20) + 1), dict(k=(1 << 20) + 1), dict(rows=1 << 31),
+        dict(rows=1 << 30, n=1 << 20), dict(groups=65536, n=1 << 20)]),
+    ("pase_grouped_matmul_backward", PROD_B, INVALID, [
+        dict(dtype=FP32), dict(grad=FP16), dict(groups=0), dict(dy=None), dict(lddy=7), dict(x=None), dict(ldx=7),
+        dict(w=None), dict(offsets=None), dict(lddx=7), dict(dx=P + 1), dict(dw=P + 1), dict(grad=FP32, dw=P + 2),
+        dict(lddy=(1 << 22) + 1), dict(ldx=(1 << 22) + 1), dict(lddx=(1 << 22) + 1)]),
+    ("pase_softmax_loss_forward", LOSS_F, INVALID, [
+        dict(dtype=3), dict(classes=0), dict(logits=None), dict(logits=P + 1), dict(ldl=7), dict(targets=None),
+        dict(targets=P + 4), dict(t64=2), dict(loss=None), dict(lse=None), dict(loss=P + 1)]),
+    ("pase_softmax_loss_forward", LOSS_F, TOO_LARGE, [dict(rows=1 << 31), dict(classes=1 << 31)]),
+    ("pase_softmax_loss_grad", LOSS_G, INVALID, [
+        dict(dtype=3), dict(classes=0), dict(logits=None), dict(ldl=7), dict(targets=None), dict(dloss=None),
+        dict(dloss=P + 2), dict(step=2), dict(dlogits=None), dict(lddl=7), dict(dlogits=P, lddl=9), dict(loss=None)]),
+    ("pase_softmax_loss_backward", LOSS_B, INVALID, [
+        dict(dtype=3), dict(classes=0), dict(logits=None), dict(ldl=7), dict(targets=None), dict(lse=None),
+        dict(dloss=None), dict(step=2), dict(dlogits=None), dict(lddl=7), dict(dlogits=P, lddl=9)]),
+    ("pase_softmax_loss_backward", LOSS_B, TOO_LARGE, [dict(rows=1 << 30, classes=1 << 20, ldl=1 << 20, lddl=1 << 20)]),
+]
+
+
+@pytest.mark.parametrize("name,good,status,change", [
+    pytest.param(n, g, s, c, id=f"{n[5:]}-{'-'.join(f'{k}={v}' for k, v in c.items())}")
+    for n, g, s, changes in REFUSALS for c in changes])
+def test_refusals(lib, name, good, status, change):
+    assert getattr(lib, name)(*{**good, **change}.values()) == status
+    assert lib.pase_operator_error()
+
+
+@pytest.mark.parametrize("name,args", [
+    ("pase_layer_norm_workspace", (BF16, 4, 8)), ("pase_grouped_matmul_workspace", (BF16, BF16, 4, 2, 8, 8)),
+    ("pase_softmax_loss_workspace", (BF16, 4, 8))])
+def test_workspace_sizes(lib, name, args):
+    need = C.c_uint64(12345)
+    assert getattr(lib, name)(*args, C.byref(need)) == OK
+    assert need.value < 1 << 30
+    assert getattr(lib, name)(*args, None) == INVALID
+    assert getattr(lib, name)(9, *args[1:], C.byref(need)) == INVALID
+
+
+@pytest.mark.parametrize("name,good", [
+    ("pase_layer_norm_forward", NORM_F), ("pase_grouped_matmul_forward", PROD_F),
+    ("pase_softmax_loss_forward", LOSS_F), ("pase_softmax_loss_grad", LOSS_G), ("pase_softmax_loss_backward", LOSS_B)])
+def test_no_rows_is_nothing_to_do(lib, name, good):
+    none = {k: (None if v in (P, 2 * P) and k != "ws_bytes" else v) for k, v in good.items()}
+    assert getattr(lib, name)(*{**none, "rows": 0}.values()) == OK
+
+
+def test_host_tensors_are_refused():
+    from paper_2407_04001_amd import PaseError, ops
+    x, g = torch.zeros(4, 8), torch.ones(8)
+    t = torch.zeros(4, dtype=torch.int64)
+    w, off = torch.zeros(2, 8, 8, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    for call in (lambda: ops.layer_norm_forward(x, g), lambda: ops.softmax_loss_forward(x, t),
+                 lambda: ops.grouped_matmul_forward(x.bfloat16(), w, off), lambda: ops.layer_norm(x, g)):
+        with pytest.raises(PaseError) as e:
+            call()
+        assert e.value.status == INVALID
+
+
+def test_argument_checks_under_sanitizers():
+    """This file's tests on the host-only build, under AddressSanitizer and UBSan."""
+    import shutil
+    import subprocess
+    import sys
+    if "libasan" in os.environ.get("LD_PRELOAD", ""):
+        pytest.skip("this is that run")
+    cxx = shutil.which(os.environ.get("CXX", "g++"))
+    if not cxx:
+        pytest.skip("no host C++ compiler")
+    from paper_2407_04001_amd import build
+    san = build.build_host_sanitized()
+    asan = subprocess.run([cxx, "-print-file-name=libasan.so"], capture_output=True, text=True).stdout.strip()
+    env = dict(os.environ, LD_PRELOAD=asan, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1:halt_on_error=1",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([sys.executable, "-m", "pytest", os.path.abspath(__file__), "-q", "-x", "-p",
+                        "no:cacheprovider", "--pase-lib", san], cwd=ROOT, env=env, capture_output=True, text=True,
+                       timeout=600)
+    assert r.returncode == 0 and " passed" in r.stdout, (r.stdout + r.stderr)[-4000:]
