@@ -51,6 +51,11 @@ __device__ __forceinline__ void group_rows(const GroupedProduct &a, int v, int64
     if (hi < lo) hi = lo;
 }
 
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
 struct Tile {
     int group;         // -1: rows of no group
     int64_t row, end;  // first row, end of its group's rows
@@ -113,6 +118,7 @@ template <int BM> __device__ Tile find_tile(const GroupedProduct &a, int cols) {
         rest -= __shfl(upto, 63, 64);
     }
     out.group = __builtin_amdgcn_readfirstlane(out.group);
+    out.row = uniform64(out.row), out.end = uniform64(out.end);
     return out;
 }
 
@@ -130,6 +136,49 @@ template <int R> __device__ __forceinline__ int across_m(int i, int c) {
 template <int R> __device__ __forceinline__ int across_j(int i, int c) {
     return i * (R / 8) + (c ^ ((i & 1) | ((i & 2) << 2)));
 }
+
+// What one workgroup computes: m_rows x j_rows of c (at most a tile of them)
+// from `depth` of the contraction.
+template <typename T, typename O> struct Part {
+    const T *a, *b;
+    O *c;
+    int64_t lda, ldb, m_rows, j_rows, depth;
+
+    template <Direction D, int BM, int BN> __device__ __forceinline__ bool find(const GroupedProduct &g) {
+        const T *x = static_cast<const T *>(g.x), *w = static_cast<const T *>(g.w), *dy = static_cast<const T *>(g.dy);
+        c = static_cast<O *>(g.out);
+        if (D == kWeights) {
+            const int nt = (g.n + BM - 1) / BM, kt = (g.k + BN - 1) / BN;
+            const int e = blockIdx.x / (nt * kt), t = blockIdx.x % (nt * kt), m0 = t / kt * BM, j0 = t % kt * BN;
+            int64_t lo, hi;
+            group_rows(g, e + 1, lo, hi);
+            lo = uniform64(lo), hi = uniform64(hi);
+            a = dy + lo * g.lddy + m0, lda = g.lddy, m_rows = g.n - m0;
+            b = x + lo * g.ldx + j0, ldb = g.ldx, j_rows = g.k - j0;
+            depth = hi - lo;
+            c += ((int64_t)e * g.n + m0) * g.k + j0;
+            return true;
+        }
+        const int cols = D == kForward ? g.n : g.k;
+        const Tile t = find_tile<BM>(g, (cols + BN - 1) / BN);
+        if (t.none) return false;
+        const int j0 = t.col * BN;
+        const int64_t e = t.group < 0 ? 0 : t.group;
+        m_rows = t.end - t.row, j_rows = cols - j0;
+        if (D == kForward) {
+            a = x + t.row * g.ldx, lda = g.ldx;
+            b = w + (e * g.n + j0) * g.k, ldb = g.k;
+            depth = g.k;
+        } else {
+            a = dy + t.row * g.lddy, lda = g.lddy;
+            b = w + e * g.n * g.k + j0, ldb = g.k;
+            depth = g.n;
+        }
+        if (t.group < 0) depth = 0;
+        c += t.row * g.ldo + j0;
+        return true;
+    }
+};
 
 // ---------------------------------------------------------------- any alignment
 // 128 x 128 tiles, 64 of i at a time; four waves, 64 x 64 each.  Operands go
@@ -203,38 +252,11 @@ template <typename T, typename O> __device__ __forceinline__ void store16(O *p, 
 template <typename T, typename O, Direction D> __global__ __launch_bounds__(256) void k_product(GroupedProduct a) {
     constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
     __shared__ Pack<T> lds[2][2][kTile * 8];
-    const T *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.w), *dy = static_cast<const T *>(a.dy);
-    const T *A, *B;
-    int64_t lda, ldb, m_rows, j_rows, depth;
-    O *c = static_cast<O *>(a.out);
-    if (D == kWeights) {
-        const int nt = (a.n + kTile - 1) / kTile, kt = (a.k + kTile - 1) / kTile;
-        const int e = blockIdx.x / (nt * kt), t = blockIdx.x % (nt * kt), m0 = t / kt * kTile, j0 = t % kt * kTile;
-        int64_t lo, hi;
-        group_rows(a, e + 1, lo, hi);
-        A = dy + lo * a.lddy + m0, lda = a.lddy, m_rows = a.n - m0;
-        B = x + lo * a.ldx + j0, ldb = a.ldx, j_rows = a.k - j0;
-        depth = hi - lo;
-        c += ((int64_t)e * a.n + m0) * a.k + j0;
-    } else {
-        const int cols = D == kForward ? a.n : a.k;
-        const Tile t = find_tile<kTile>(a, (cols + kTile - 1) / kTile);
-        if (t.none) return;
-        const int j0 = t.col * kTile;
-        const int64_t e = t.group < 0 ? 0 : t.group;
-        m_rows = t.end - t.row, j_rows = cols - j0;
-        if (D == kForward) {
-            A = x + t.row * a.ldx, lda = a.ldx;
-            B = w + (e * a.n + j0) * a.k, ldb = a.k;
-            depth = a.k;
-        } else {
-            A = dy + t.row * a.lddy, lda = a.lddy;
-            B = w + e * a.n * a.k + j0, ldb = a.k;
-            depth = a.n;
-        }
-        if (t.group < 0) depth = 0;
-        c += t.row * a.ldo + j0;
-    }
+    Part<T, O> p;
+    if (!p.template find<D, kTile, kTile>(a)) return;
+    const T *A = p.a, *B = p.b;
+    const int64_t lda = p.lda, ldb = p.ldb, m_rows = p.m_rows, j_rows = p.j_rows, depth = p.depth;
+    O *c = p.c;
     const int wave = threadIdx.x >> 6, wm = (wave >> 1) * 64, wj = (wave & 1) * 64;
     f32x4 acc[4][4] = {};
     Pack<T> ra[4], rb[4];
@@ -278,16 +300,139 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
     }
 }
 
-template <typename T, typename O, Direction D> int go(const GroupedProduct &a, void *stream) {
-    int64_t blocks;
-    if (D == kWeights) {
-        blocks = (int64_t)a.groups * ((a.n + kTile - 1) / kTile) * ((a.k + kTile - 1) / kTile);
-    } else {
-        const int cols = D == kForward ? a.n : a.k;
-        const int64_t tiles = (a.rows / kTile + a.groups + 2) * ((cols + kTile - 1) / kTile);
-        blocks = (tiles + kXcds - 1) / kXcds * kXcds;
+// ---------------------------------------------------------------- 4-byte aligned rows
+// 256 x 256 tiles, 64 of i at a time, eight waves of 128 x 64.  The operands go
+// from HBM to LDS without passing registers (buffer loads to LDS, 16 bytes a
+// lane): the buffer's range ends at the operand's last element, so what a tile
+// overhangs reads as 0.  Only what lies past i = depth in a row along i is
+// inside that range; the fragments of the last step are masked there.
+constexpr int kBig = 256;
+constexpr int kStage = 2 * kBig * 8 * 16;   // bytes of one step's two operands in LDS
+
+// One operand's loads: 4 of 16 bytes a lane and step.
+template <typename T, bool ACROSS, bool J> struct Feed {
+    const char *base;     // of the current step
+    int64_t left;         // i from this step on
+    int64_t ld;           // bytes
+    int rows, at[4];      // rows (along) or columns (across) that exist; the lane's byte offsets
+
+    __device__ __forceinline__ void begin(const T *p, int64_t ld_elems, int64_t have, int64_t depth) {
+        base = reinterpret_cast<const char *>(p), ld = ld_elems * 2, left = depth;
+        rows = (int)(have < kBig ? have : kBig);
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            const int q = threadIdx.x + s * 512;   // LDS chunk this lane's load fills; the permutation is its own inverse
+            if (ACROSS) {
+                const int i = q >> 5, c = (J ? across_j<kBig>(i, q & 31) : across_m<kBig>(i, q & 31)) - i * 32;
+                at[s] = i * (int)ld + c * 16;
+            } else {
+                const int r = q >> 3, c = (J ? along_j(r, q & 7) : along_m(r, q & 7)) - r * 8;
+                at[s] = r * (int)ld + c * 16;
+            }
+        }
     }
-    return launch(k_product<T, O, D>, blocks, 256, stream, a);
+
+    __device__ __forceinline__ void load(char *lds) {
+        const int64_t range = ACROSS ? ((left < 64 ? left : 64) - 1) * ld + rows * 2 : (rows - 1) * ld + left * 2;
+        // the range is checked by words of 4 bytes: the last element's own word has to be inside
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, (int)((range + 3) & ~3ll), 0x00020000);
+        char *dst = lds + (threadIdx.x >> 6) * 1024;
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                r, (__attribute__((address_space(3))) void *)reinterpret_cast<uintptr_t>(dst + s * 8192), 16, at[s], 0, 0, 0);
+        base += ACROSS ? 64 * ld : 128;
+        left -= 64;
+    }
+};
+
+template <typename F> __device__ __forceinline__ void mask_frag(F &f, int left) {
+    union {
+        F f;
+        uint32_t d[4];
+    } u;
+    u.f = f;
+#pragma unroll
+    for (int j = 0; j < 4; j++) u.d[j] = left >= 2 * j + 2 ? u.d[j] : left == 2 * j + 1 ? u.d[j] & 0xffff : 0;
+    f = u.f;
+}
+
+template <typename T, typename O, Direction D> __global__ __launch_bounds__(512) void k_product_big(GroupedProduct a) {
+    constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
+    typedef typename Mfma<T>::Frag Frag;
+    __shared__ __attribute__((aligned(1024))) char lds[2][kStage];
+    Part<T, O> p;
+    if (!p.template find<D, kBig, kBig>(a)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = (wave >> 2) * 128, wj = (wave & 3) * 64;
+    f32x4 acc[8][4] = {};
+    if (p.depth > 0) {
+        Feed<T, A_ACROSS, false> fa;
+        Feed<T, B_ACROSS, true> fb;
+        fa.begin(p.a, p.lda, p.m_rows, p.depth);
+        fb.begin(p.b, p.ldb, p.j_rows, p.depth);
+        const int steps = (int)((p.depth + 63) >> 6);
+        fa.load(lds[0]);
+        fb.load(lds[0] + kStage / 2);
+        for (int t = 0; t < steps; t++) {
+            char *cur = lds[t & 1], *next = lds[(t & 1) ^ 1];
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + 1 < steps) {
+                fa.load(next);
+                fb.load(next + kStage / 2);
+            }
+            const Pack<T> *la = reinterpret_cast<const Pack<T> *>(cur), *lb = reinterpret_cast<const Pack<T> *>(cur + kStage / 2);
+            const int left = (int)(p.depth - (int64_t)t * 64 < 64 ? p.depth - (int64_t)t * 64 : 64);
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                Frag f[8], g[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) g[j] = frag<T, B_ACROSS, true, kBig>(lb, wj, j, h);
+#pragma unroll
+                for (int m = 0; m < 8; m++) f[m] = frag<T, A_ACROSS, false, kBig>(la, wm, m, h);
+                if (D != kWeights && left < 64) {
+                    const int mine = left - h * 32 - ((threadIdx.x & 63) >> 4) * 8;
+#pragma unroll
+                    for (int m = 0; m < 8; m++) mask_frag(f[m], mine);
+                    if (!B_ACROSS)
+#pragma unroll
+                        for (int j = 0; j < 4; j++) mask_frag(g[j], mine);
+                }
+#pragma unroll
+                for (int m = 0; m < 8; m++)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) acc[m][j] = Mfma<T>::go(g[j], f[m], acc[m][j]);
+            }
+        }
+    }
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int m = 0; m < 8; m++) {
+        const int row = wm + m * 16 + (lane & 15), col = wj + (lane >> 4) * 16;
+        if (row < p.m_rows && col < p.j_rows) store16<T, O>(p.c + row * a.ldo + col, p.j_rows - col, acc[m]);
+    }
+}
+
+template <Direction D> bool feeds_big(const GroupedProduct &a) {
+    const auto even = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 2 == 0; };
+    if (D == kForward) return even(a.x, a.ldx) && even(a.w, a.k);
+    if (D == kRowsGrad) return even(a.dy, a.lddy) && even(a.w, a.k);
+    return even(a.dy, a.lddy) && even(a.x, a.ldx);
+}
+
+template <int BM, int BN, Direction D> int64_t blocks_for(const GroupedProduct &a) {
+    if (D == kWeights) return (int64_t)a.groups * ((a.n + BM - 1) / BM) * ((a.k + BN - 1) / BN);
+    const int cols = D == kForward ? a.n : a.k;
+    const int64_t tiles = (a.rows / BM + a.groups + 2) * ((cols + BN - 1) / BN);
+    return (tiles + kXcds - 1) / kXcds * kXcds;
+}
+
+template <typename T, typename O, Direction D> int go(const GroupedProduct &a, void *stream) {
+    if (feeds_big<D>(a) && (D == kWeights || a.rows / a.groups >= 128))
+        return launch(k_product_big<T, O, D>, blocks_for<kBig, kBig, D>(a), 512, stream, a);
+    return launch(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
 }
 
 template <Direction D> int by_type(const GroupedProduct &a, void *stream) {
