@@ -309,6 +309,19 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
 constexpr int kBig = 256;
 constexpr int kStage = 2 * kBig * 8 * 16;   // bytes of one step's two operands in LDS
 
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+    return (uint32_t) reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)p);
+}
+
+// 16 bytes a lane from buffer r, byte offset `at`, to LDS byte dst + 16 * lane (dst
+// the same for the wave, through M0, which nothing else here uses).  The load has no register result; whoever reads the
+// LDS bytes waits for it by wait_loads().  The builtin of the same instruction
+// makes the compiler wait for every such load before each transposing LDS read,
+// a step too early: 16384 x 4096 x 4096 rows gradient 510 us with it, XXX without.
+__device__ __forceinline__ void load_to_lds(u32x4 r, int at, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(r) : "memory");
+}
+
 // One operand's loads: 4 of 16 bytes a lane and step.
 template <typename T, bool ACROSS, bool J> struct Feed {
     const char *base;     // of the current step
@@ -335,17 +348,36 @@ template <typename T, bool ACROSS, bool J> struct Feed {
     __device__ __forceinline__ void load(char *lds) {
         const int64_t range = ACROSS ? ((left < 64 ? left : 64) - 1) * ld + rows * 2 : (rows - 1) * ld + left * 2;
         // the range is checked by words of 4 bytes: the last element's own word has to be inside
-        const __amdgpu_buffer_rsrc_t r =
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, (int)((range + 3) & ~3ll), 0x00020000);
-        char *dst = lds + (threadIdx.x >> 6) * 1024;
+        const uint64_t at0 = reinterpret_cast<uint64_t>(base);
+        const u32x4 r = {(uint32_t)at0, (uint32_t)(at0 >> 32) & 0xffff, (uint32_t)((range + 3) & ~3ll), 0x00020000};
+        const uint32_t dst = lds_address(lds) + (__builtin_amdgcn_readfirstlane(threadIdx.x) >> 6) * 1024;
 #pragma unroll
-        for (int s = 0; s < 4; s++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                r, (__attribute__((address_space(3))) void *)reinterpret_cast<uintptr_t>(dst + s * 8192), 16, at[s], 0, 0, 0);
+        for (int s = 0; s < 4; s++) load_to_lds(r, at[s], dst + s * 8192);
         base += ACROSS ? 64 * ld : 128;
         left -= 64;
     }
 };
+
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A barrier alone: what it orders is waited for where it is needed.
+__device__ __forceinline__ void barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Asks the scheduler for N times: an LDS read, then M products.
+template <int N, int M> __device__ __forceinline__ void interleave() {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 template <typename F> __device__ __forceinline__ void mask_frag(F &f, int left) {
     union {
@@ -372,39 +404,81 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         fa.begin(p.a, p.lda, p.m_rows, p.depth);
         fb.begin(p.b, p.ldb, p.j_rows, p.depth);
         const int steps = (int)((p.depth + 63) >> 6);
+        // A step is four groups of 16 products: i halves h, and for each the wave's upper
+        // and lower rows of A.  Each group's fragments are read while the group before
+        // it multiplies.  Before the last one everything of the step has been read and
+        // the next step has arrived, so one barrier a step is enough: after it the
+        // step after next is loaded into this step's half of LDS.
+        Frag f[2][4], g[2][4];
+        const auto read_a = [&](Frag(&to)[4], const char *at, int h, int low) {
+#pragma unroll
+            for (int m = 0; m < 4; m++) to[m] = frag<T, A_ACROSS, false, kBig>(reinterpret_cast<const Pack<T> *>(at), wm, low * 4 + m, h);
+        };
+        const auto read_b = [&](Frag(&to)[4], const char *at, int h) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) to[j] = frag<T, B_ACROSS, true, kBig>(reinterpret_cast<const Pack<T> *>(at + kStage / 2), wj, j, h);
+        };
+        const auto multiply = [&](const Frag(&fm)[4], const Frag(&gj)[4], int low) {
+#pragma unroll
+            for (int m = 0; m < 4; m++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) acc[low * 4 + m][j] = Mfma<T>::go(gj[j], fm[m], acc[low * 4 + m][j]);
+        };
+        const auto mask = [&](Frag(&of)[4], int left, int h) {
+#pragma unroll
+            for (int m = 0; m < 4; m++) mask_frag(of[m], left - h * 32 - ((threadIdx.x & 63) >> 4) * 8);
+        };
         fa.load(lds[0]);
         fb.load(lds[0] + kStage / 2);
-        for (int t = 0; t < steps; t++) {
+        if (steps > 1) {
+            fa.load(lds[1]);
+            fb.load(lds[1] + kStage / 2);
+            asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        } else {
+            wait_loads();
+        }
+        barrier();
+        read_a(f[0], lds[0], 0, 0);
+        read_b(g[0], lds[0], 0);
+        for (int t = 0; t + 1 < steps; t++) {
             char *cur = lds[t & 1], *next = lds[(t & 1) ^ 1];
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (t + 1 < steps) {
-                fa.load(next);
-                fb.load(next + kStage / 2);
+            read_a(f[1], cur, 0, 1);
+            multiply(f[0], g[0], 0);
+            interleave<4, 4>();
+            read_a(f[0], cur, 1, 0);
+            read_b(g[1], cur, 1);
+            multiply(f[1], g[0], 1);
+            interleave<8, 2>();
+            read_a(f[1], cur, 1, 1);
+            multiply(f[0], g[1], 0);
+            interleave<4, 4>();
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            barrier();
+            if (t + 2 < steps) {
+                fa.load(cur);
+                fb.load(cur + kStage / 2);
             }
-            const Pack<T> *la = reinterpret_cast<const Pack<T> *>(cur), *lb = reinterpret_cast<const Pack<T> *>(cur + kStage / 2);
-            const int left = (int)(p.depth - (int64_t)t * 64 < 64 ? p.depth - (int64_t)t * 64 : 64);
+            read_a(f[0], next, 0, 0);
+            read_b(g[0], next, 0);
+            multiply(f[1], g[1], 1);
+            interleave<8, 2>();
+        }
+        const char *cur = lds[(steps - 1) & 1];
+        const int left = (int)(p.depth - (int64_t)(steps - 1) * 64);
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                Frag f[8], g[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) g[j] = frag<T, B_ACROSS, true, kBig>(lb, wj, j, h);
-#pragma unroll
-                for (int m = 0; m < 8; m++) f[m] = frag<T, A_ACROSS, false, kBig>(la, wm, m, h);
-                if (D != kWeights && left < 64) {
-                    const int mine = left - h * 32 - ((threadIdx.x & 63) >> 4) * 8;
-#pragma unroll
-                    for (int m = 0; m < 8; m++) mask_frag(f[m], mine);
-                    if (!B_ACROSS)
-#pragma unroll
-                        for (int j = 0; j < 4; j++) mask_frag(g[j], mine);
-                }
-#pragma unroll
-                for (int m = 0; m < 8; m++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) acc[m][j] = Mfma<T>::go(g[j], f[m], acc[m][j]);
+        for (int h = 0; h < 2; h++) {
+            if (h) {
+                read_a(f[0], cur, 1, 0);
+                read_b(g[0], cur, 1);
             }
+            read_a(f[1], cur, h, 1);
+            if (D != kWeights) {
+                mask(f[0], left, h);
+                mask(f[1], left, h);
+                if (!B_ACROSS) mask(g[0], left, h);
+            }
+            multiply(f[0], g[0], 0);
+            multiply(f[1], g[0], 1);
         }
     }
     const int lane = threadIdx.x & 63;
