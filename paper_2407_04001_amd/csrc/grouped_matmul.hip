@@ -345,16 +345,25 @@ template <typename T, bool ACROSS, bool J> struct Feed {
         }
     }
 
-    __device__ __forceinline__ void load(char *lds) {
-        const int64_t range = ACROSS ? ((left < 64 ? left : 64) - 1) * ld + rows * 2 : (rows - 1) * ld + left * 2;
+    u32x4 range;      // buffer descriptor of the step being loaded
+    uint32_t dst;
+
+    __device__ __forceinline__ void next(const char *lds) {
+        const int64_t bytes = ACROSS ? ((left < 64 ? left : 64) - 1) * ld + rows * 2 : (rows - 1) * ld + left * 2;
         // the range is checked by words of 4 bytes: the last element's own word has to be inside
         const uint64_t at0 = reinterpret_cast<uint64_t>(base);
-        const u32x4 r = {(uint32_t)at0, (uint32_t)(at0 >> 32) & 0xffff, (uint32_t)((range + 3) & ~3ll), 0x00020000};
-        const uint32_t dst = lds_address(lds) + (__builtin_amdgcn_readfirstlane(threadIdx.x) >> 6) * 1024;
-#pragma unroll
-        for (int s = 0; s < 4; s++) load_to_lds(r, at[s], dst + s * 8192);
+        range = u32x4{(uint32_t)at0, (uint32_t)(at0 >> 32) & 0xffff, left > 0 ? (uint32_t)((bytes + 3) & ~3ll) : 0, 0x00020000};
+        dst = lds_address(lds) + (__builtin_amdgcn_readfirstlane(threadIdx.x) >> 6) * 1024;
         base += ACROSS ? 64 * ld : 128;
         left -= 64;
+    }
+
+    __device__ __forceinline__ void issue(int s) { load_to_lds(range, at[s], dst + s * 8192); }
+
+    __device__ __forceinline__ void load(const char *lds) {
+        next(lds);
+#pragma unroll
+        for (int s = 0; s < 4; s++) issue(s);
     }
 };
 
@@ -366,16 +375,6 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-// Asks the scheduler for N times: an LDS read, then M products.
-template <int N, int M> __device__ __forceinline__ void interleave() {
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
-    }
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -410,19 +409,16 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         // the next step has arrived, so one barrier a step is enough: after it the
         // step after next is loaded into this step's half of LDS.
         Frag f[2][4], g[2][4];
-        const auto read_a = [&](Frag(&to)[4], const char *at, int h, int low) {
-#pragma unroll
-            for (int m = 0; m < 4; m++) to[m] = frag<T, A_ACROSS, false, kBig>(reinterpret_cast<const Pack<T> *>(at), wm, low * 4 + m, h);
+        const auto read_a = [&](Frag &to, const char *at, int h, int m) {
+            to = frag<T, A_ACROSS, false, kBig>(reinterpret_cast<const Pack<T> *>(at), wm, m, h);
         };
-        const auto read_b = [&](Frag(&to)[4], const char *at, int h) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) to[j] = frag<T, B_ACROSS, true, kBig>(reinterpret_cast<const Pack<T> *>(at + kStage / 2), wj, j, h);
+        const auto read_b = [&](Frag &to, const char *at, int h, int j) {
+            to = frag<T, B_ACROSS, true, kBig>(reinterpret_cast<const Pack<T> *>(at + kStage / 2), wj, j, h);
         };
-        const auto multiply = [&](const Frag(&fm)[4], const Frag(&gj)[4], int low) {
+        // four products, and what is issued behind them
+        const auto multiply = [&](const Frag &fm, const Frag(&gj)[4], int m) {
 #pragma unroll
-            for (int m = 0; m < 4; m++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[low * 4 + m][j] = Mfma<T>::go(gj[j], fm[m], acc[low * 4 + m][j]);
+            for (int j = 0; j < 4; j++) acc[m][j] = Mfma<T>::go(gj[j], fm, acc[m][j]);
         };
         const auto mask = [&](Frag(&of)[4], int left, int h) {
 #pragma unroll
@@ -430,56 +426,71 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         };
         fa.load(lds[0]);
         fb.load(lds[0] + kStage / 2);
-        if (steps > 1) {
-            fa.load(lds[1]);
-            fb.load(lds[1] + kStage / 2);
-            asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-        } else {
-            wait_loads();
-        }
+        fa.load(lds[1]);
+        fb.load(lds[1] + kStage / 2);
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
         barrier();
-        read_a(f[0], lds[0], 0, 0);
-        read_b(g[0], lds[0], 0);
+#pragma unroll
+        for (int j = 0; j < 4; j++) read_b(g[0][j], lds[0], 0, j);
+#pragma unroll
+        for (int m = 0; m < 4; m++) read_a(f[0][m], lds[0], 0, m);
         for (int t = 0; t + 1 < steps; t++) {
             char *cur = lds[t & 1], *next = lds[(t & 1) ^ 1];
-            read_a(f[1], cur, 0, 1);
-            multiply(f[0], g[0], 0);
-            interleave<4, 4>();
-            read_a(f[0], cur, 1, 0);
-            read_b(g[1], cur, 1);
-            multiply(f[1], g[0], 1);
-            interleave<8, 2>();
-            read_a(f[1], cur, 1, 1);
-            multiply(f[0], g[1], 0);
-            interleave<4, 4>();
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                multiply(f[0][m], g[0], m);
+                read_a(f[1][m], cur, 0, 4 + m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                multiply(f[1][m], g[0], 4 + m);
+                read_b(g[1][m], cur, 1, m);
+                read_a(f[0][m], cur, 1, m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                multiply(f[0][m], g[1], m);
+                read_a(f[1][m], cur, 1, 4 + m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            fa.next(cur);
+            fb.next(cur + kStage / 2);
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             barrier();
-            if (t + 2 < steps) {
-                fa.load(cur);
-                fb.load(cur + kStage / 2);
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                multiply(f[1][m], g[1], 4 + m);
+                __builtin_amdgcn_sched_barrier(0);
+                read_b(g[0][m], next, 0, m);
+                read_a(f[0][m], next, 0, m);
+                fa.issue(m);
+                fb.issue(m);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            read_a(f[0], next, 0, 0);
-            read_b(g[0], next, 0);
-            multiply(f[1], g[1], 1);
-            interleave<8, 2>();
         }
         const char *cur = lds[(steps - 1) & 1];
         const int left = (int)(p.depth - (int64_t)(steps - 1) * 64);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            if (h) {
-                read_a(f[0], cur, 1, 0);
-                read_b(g[0], cur, 1);
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                if (h) {
+                    read_b(g[0][m], cur, 1, m);
+                    read_a(f[0][m], cur, 1, m);
+                }
+                read_a(f[1][m], cur, h, 4 + m);
             }
-            read_a(f[1], cur, h, 1);
             if (D != kWeights) {
                 mask(f[0], left, h);
                 mask(f[1], left, h);
                 if (!B_ACROSS) mask(g[0], left, h);
             }
-            multiply(f[0], g[0], 0);
-            multiply(f[1], g[0], 1);
+#pragma unroll
+            for (int m = 0; m < 8; m++) multiply(f[m >> 2][m & 3], g[0], m);
         }
+        wait_loads();   // of nothing but zeros, yet into this workgroup's LDS
     }
     const int lane = threadIdx.x & 63;
 #pragma unroll
