@@ -378,6 +378,42 @@ __device__ __forceinline__ void barrier() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// The same fragments as frag(), by byte address: `at` is `base` plus the address
+// of the operand's stage.  One address register an operand, from which each
+// fragment's place follows by an exclusive or and a constant.
+template <typename T, bool ACROSS, bool J> struct Reader {
+    typedef typename Mfma<T>::Frag Frag;
+    uint32_t base;
+
+    __device__ __forceinline__ explicit Reader(int first) {
+        const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
+        if (ACROSS) {
+            const int i = q * 8 + (l >> 2), col = first + (J ? (l & 3) * 16 : (l & 3) * 4);
+            base = (J ? across_j<kBig>(i, col >> 3) : across_m<kBig>(i, col >> 3)) * 16 + (col & 4) * 2;
+        } else {
+            const int r = first + (J ? (l >> 2) * 16 + (l & 3) : l);
+            base = (J ? along_j(r, q) : along_m(r, q)) * 16;
+        }
+    }
+
+    static __device__ __forceinline__ void read(Frag &to, uint32_t at, int t, int h) {
+        if (!ACROSS) {
+            to = *(__attribute__((address_space(3))) const Frag *)(uintptr_t)((at ^ (h * 64)) + t * (J ? 512 : 2048));
+            return;
+        }
+        union {
+            Frag f;
+            s16x4 half[2];
+        } u;
+        const uint32_t col = J ? (at ^ ((t >> 1) * 16)) + (t & 1) * 8 : at ^ (t * 32);
+#pragma unroll
+        for (int s = 0; s < 2; s++)
+            u.half[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4 *)(uintptr_t)(col + (h * 32 + s * 4) * (kBig * 2)));
+        to = u.f;
+    }
+};
+
 template <typename F> __device__ __forceinline__ void mask_frag(F &f, int left) {
     union {
         F f;
@@ -408,13 +444,10 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         // it multiplies.  Before the last one everything of the step has been read and
         // the next step has arrived, so one barrier a step is enough: after it the
         // step after next is loaded into this step's half of LDS.
-        Frag f[2][4], g[2][4];
-        const auto read_a = [&](Frag &to, const char *at, int h, int m) {
-            to = frag<T, A_ACROSS, false, kBig>(reinterpret_cast<const Pack<T> *>(at), wm, m, h);
-        };
-        const auto read_b = [&](Frag &to, const char *at, int h, int j) {
-            to = frag<T, B_ACROSS, true, kBig>(reinterpret_cast<const Pack<T> *>(at + kStage / 2), wj, j, h);
-        };
+        Frag f[3][4], g[2][4];
+        const Reader<T, A_ACROSS, false> ra(wm);
+        const Reader<T, B_ACROSS, true> rb(wj);
+        const uint32_t stage0 = lds_address(lds[0]);
         // four products, and what is issued behind them
         const auto multiply = [&](const Frag &fm, const Frag(&gj)[4], int m) {
 #pragma unroll
@@ -430,29 +463,31 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         fb.load(lds[1] + kStage / 2);
         asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
         barrier();
+        // this step's and the next step's places, each operand's; the compiler would
+        // keep every fragment's address of both in registers, more than there are
+        uint32_t at_a = stage0 + ra.base, at_b = stage0 + kStage / 2 + rb.base;
+        uint32_t other_a = at_a + kStage, other_b = at_b + kStage;
 #pragma unroll
-        for (int j = 0; j < 4; j++) read_b(g[0][j], lds[0], 0, j);
-#pragma unroll
-        for (int m = 0; m < 4; m++) read_a(f[0][m], lds[0], 0, m);
+        for (int m = 0; m < 4; m++) rb.read(g[0][m], at_b, m, 0), ra.read(f[0][m], at_a, m, 0);
         for (int t = 0; t + 1 < steps; t++) {
-            char *cur = lds[t & 1], *next = lds[(t & 1) ^ 1];
+            char *cur = lds[t & 1];
+            asm volatile("" : "+v"(at_a), "+v"(at_b), "+v"(other_a), "+v"(other_b));
 #pragma unroll
             for (int m = 0; m < 4; m++) {
                 multiply(f[0][m], g[0], m);
-                read_a(f[1][m], cur, 0, 4 + m);
+                __builtin_amdgcn_sched_barrier(0);
+                ra.read(f[1][m], at_a, 4 + m, 0);
+                ra.read(f[2][m], at_a, m, 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int m = 0; m < 4; m++) {
                 multiply(f[1][m], g[0], 4 + m);
-                read_b(g[1][m], cur, 1, m);
-                read_a(f[0][m], cur, 1, m);
                 __builtin_amdgcn_sched_barrier(0);
-            }
+                if (m < 2) {
 #pragma unroll
-            for (int m = 0; m < 4; m++) {
-                multiply(f[0][m], g[1], m);
-                read_a(f[1][m], cur, 1, 4 + m);
+                    for (int k = 2 * m; k < 2 * m + 2; k++) rb.read(g[1][k], at_b, k, 1), ra.read(f[0][k], at_a, 4 + k, 1);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             fa.next(cur);
@@ -461,28 +496,32 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
             barrier();
 #pragma unroll
             for (int m = 0; m < 4; m++) {
-                multiply(f[1][m], g[1], 4 + m);
+                multiply(f[2][m], g[1], m);
                 __builtin_amdgcn_sched_barrier(0);
-                read_b(g[0][m], next, 0, m);
-                read_a(f[0][m], next, 0, m);
                 fa.issue(m);
+                rb.read(g[0][m], other_b, m, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                multiply(f[0][m], g[1], 4 + m);
+                __builtin_amdgcn_sched_barrier(0);
+                ra.read(f[0][m], other_a, m, 0);
                 fb.issue(m);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            const uint32_t ta = at_a, tb = at_b;
+            at_a = other_a, at_b = other_b, other_a = ta, other_b = tb;
         }
-        const char *cur = lds[(steps - 1) & 1];
         const int left = (int)(p.depth - (int64_t)(steps - 1) * 64);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
 #pragma unroll
             for (int m = 0; m < 4; m++) {
-                if (h) {
-                    read_b(g[0][m], cur, 1, m);
-                    read_a(f[0][m], cur, 1, m);
-                }
-                read_a(f[1][m], cur, h, 4 + m);
+                if (h) rb.read(g[0][m], at_b, m, 1), ra.read(f[0][m], at_a, m, 1);
+                ra.read(f[1][m], at_a, 4 + m, h);
             }
-            if (D != kWeights) {
+            if (D != kWeights) {   // along i, what lies past the end is not 0; across, it is
                 mask(f[0], left, h);
                 mask(f[1], left, h);
                 if (!B_ACROSS) mask(g[0], left, h);
