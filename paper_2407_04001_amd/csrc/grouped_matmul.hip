@@ -37,89 +37,110 @@ template <> struct Mfma<_Float16> {
     }
 };
 
-__device__ __forceinline__ int64_t offset_at(const GroupedProduct &a, int e) {
-    int64_t o = a.offsets_64 ? static_cast<const int64_t *>(a.offsets)[e]
-                             : (int64_t) static_cast<const int32_t *>(a.offsets)[e];
-    return o < 0 ? 0 : o > a.rows ? a.rows : o;
-}
+// 64 virtual groups from `first` on, one a lane: virtual group 0 is the rows before
+// offsets[0], 1 .. groups the groups, groups + 1 the rows from offsets[groups] on.
+// `before` is where the one before `first` ends.  Offsets are kept within 0 .. rows
+// and not below any earlier one, so that every row has one virtual group whatever
+// they hold.
+struct Ranges {
+    int lo, hi;
+    int tiles, upto;   // of BM rows: this group's, and those up to and with it
 
-// Rows of virtual group v: 0 is the rows before offsets[0], 1 .. groups the
-// groups, groups + 1 the rows from offsets[groups] on.
-__device__ __forceinline__ void group_rows(const GroupedProduct &a, int v, int64_t &lo, int64_t &hi) {
-    lo = v == 0 ? 0 : offset_at(a, v - 1);
-    hi = v == a.groups + 1 ? a.rows : offset_at(a, v);
-    if (hi < lo) hi = lo;
-}
-
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
-    return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
-struct Tile {
-    int group;         // -1: rows of no group
-    int64_t row, end;  // first row, end of its group's rows
-    int col;           // column tile
-    bool none;
-};
-
-// The tile of this workgroup among the row tiles (BM rows; every virtual group
-// begins a new one) x `cols` column tiles.  How many row tiles there are is
-// known on the device only: the grid is an upper bound, and what is left over
-// returns.  Workgroups go round the 8 XCDs by their number, so the tiles are
-// dealt such that each XCD has one contiguous run of them, and within a run
-// kBand row tiles go through all column tiles together: their A rows stay in
-// that XCD's L2 while B passes once per band.
-constexpr int kXcds = 8, kBand = 8;
-
-template <int BM> __device__ Tile find_tile(const GroupedProduct &a, int cols) {
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int v0 = 0; v0 < a.groups + 2; v0 += 64) {
-        const int v = v0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (v < a.groups + 2) group_rows(a, v, lo, hi);
-        int t = (int)((hi - lo + BM - 1) / BM);
+    __device__ __forceinline__ Ranges(const GroupedProduct &a, int first, int before, int bm) {
+        const int lane = threadIdx.x & 63, v = first + lane;
+        int64_t o = a.rows;
+        if (v <= a.groups)
+            o = a.offsets_64 ? static_cast<const int64_t *>(a.offsets)[v]
+                             : (int64_t) static_cast<const int32_t *>(a.offsets)[v];
+        o = o > a.rows ? a.rows : o;
+        hi = o < before ? before : (int)o;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d, 64);
-        total += t;
-    }
-    total = __builtin_amdgcn_readfirstlane((int)total);
-    const int64_t tiles = total * cols, per = (tiles + kXcds - 1) / kXcds;
-    const int64_t i = blockIdx.x / kXcds, at = (int64_t)(blockIdx.x % kXcds) * per + i;
-    Tile out;
-    out.none = i >= per || at >= tiles;
-    if (out.none) return out;
-    const int64_t band = at / (kBand * (int64_t)cols), in = at - band * kBand * cols;
-    const int high = (int)(total - band * kBand < kBand ? total - band * kBand : kBand);
-    int64_t rest = band * kBand + in % high;
-    out.col = (int)(in / high);
-    for (int v0 = 0; v0 < a.groups + 2; v0 += 64) {
-        const int v = v0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (v < a.groups + 2) group_rows(a, v, lo, hi);
-        const int t = (int)((hi - lo + BM - 1) / BM);
-        int upto = t;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(hi, d, 64);
+            if (lane >= d && o > hi) hi = o;
+        }
+        lo = __shfl_up(hi, 1, 64);
+        if (lane == 0) lo = before;
+        upto = tiles = (int)(((uint32_t)(hi - lo) + bm - 1) / bm);
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int o = __shfl_up(upto, d, 64);
             if (lane >= d) upto += o;
         }
-        const uint64_t found = __ballot(rest < upto);
-        if (found) {
-            const int src = __builtin_ctzll(found);
-            const int before = __shfl(upto, src, 64) - __shfl(t, src, 64);
-            out.row = __shfl(lo, src, 64) + (rest - before) * BM;
-            out.end = __shfl(hi, src, 64);
-            out.group = v0 + src - 1;
-            if (out.group == a.groups) out.group = -1;
-            break;
-        }
-        rest -= __shfl(upto, 63, 64);
     }
-    out.group = __builtin_amdgcn_readfirstlane(out.group);
-    out.row = uniform64(out.row), out.end = uniform64(out.end);
-    return out;
+    __device__ __forceinline__ int end() const { return __builtin_amdgcn_readlane(hi, 63); }
+    __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
+};
+
+struct Tile {
+    int group;         // -1: rows of no group
+    int row, end;      // first row, end of its group's rows
+    int col;           // column tile
+    bool none;
+};
+
+// The tiles of BM rows (every virtual group begins a new one) x `cols` columns of
+// tiles, dealt to the workgroups.  How many row tiles there are is known on the
+// device only: the grid is an upper bound, or as many workgroups as run at once,
+// each taking every (grid)-th.  Workgroups go round the 8 XCDs by their number,
+// so each XCD gets one contiguous run of the tiles, and within a run kBand row
+// tiles go through all column tiles together: their A rows stay in that XCD's L2
+// while B passes once per band.
+constexpr int kXcds = 8, kBand = 8;
+
+template <int BM> struct Deal {
+    uint32_t cols, total, per;   // row tiles; tiles of an XCD's run
+
+    __device__ __forceinline__ Deal(const GroupedProduct &a, int cols_) {
+        cols = cols_, total = 0;
+        int before = 0;
+        for (int v = 0; v < a.groups + 2; v += 64) {
+            const Ranges r(a, v, before, BM);
+            total += r.all();
+            before = r.end();
+        }
+        per = (total * cols + kXcds - 1) / kXcds;
+    }
+
+    // The i-th tile of this workgroup's run.
+    __device__ __forceinline__ Tile get(const GroupedProduct &a, uint32_t i) const {
+        Tile out;
+        const uint32_t at = blockIdx.x % kXcds * per + i;
+        out.none = i >= per || at >= total * cols;
+        if (out.none) return out;
+        const uint32_t band = at / (kBand * cols), in = at - band * kBand * cols;
+        const uint32_t high = total - band * kBand < kBand ? total - band * kBand : kBand;
+        // (quotients are formed in vector registers)
+        out.col = __builtin_amdgcn_readfirstlane(in / high);
+        int rest = __builtin_amdgcn_readfirstlane(band * kBand + in % high);
+        int before = 0;
+        for (int v = 0;; v += 64) {
+            const Ranges r(a, v, before, BM);
+            const uint64_t found = __ballot(rest < r.upto);
+            if (found) {
+                const int src = __builtin_ctzll(found), first = __builtin_amdgcn_readlane(r.upto - r.tiles, src);
+                out.row = __builtin_amdgcn_readlane(r.lo, src) + (rest - first) * BM;
+                out.end = __builtin_amdgcn_readlane(r.hi, src);
+                out.group = v + src - 1 == a.groups ? -1 : v + src - 1;
+                return out;
+            }
+            rest -= r.all();
+            before = r.end();
+        }
+    }
+};
+
+// Rows of group e.
+__device__ __forceinline__ void group_rows(const GroupedProduct &a, int e, int &lo, int &hi) {
+    int before = 0;
+    for (int v = 0;; v += 64) {
+        const Ranges r(a, v, before, 1 << 30);
+        if (e + 1 < v + 64) {
+            lo = __builtin_amdgcn_readlane(r.lo, e + 1 - v), hi = __builtin_amdgcn_readlane(r.hi, e + 1 - v);
+            return;
+        }
+        before = r.end();
+    }
 }
 
 // LDS places, in 16-byte chunks.  "Along": row r, chunk c (8 i) of a row of 8
@@ -137,46 +158,43 @@ template <int R> __device__ __forceinline__ int across_j(int i, int c) {
     return i * (R / 8) + (c ^ ((i & 1) | ((i & 2) << 2)));
 }
 
-// What one workgroup computes: m_rows x j_rows of c (at most a tile of them)
-// from `depth` of the contraction.
+// What one workgroup computes at a time: m_rows x j_rows of c (at most a tile of
+// them) from `depth` of the contraction.
 template <typename T, typename O> struct Part {
     const T *a, *b;
     O *c;
-    int64_t lda, ldb, m_rows, j_rows, depth;
+    int lda, ldb, m_rows, j_rows, depth;
 
-    template <Direction D, int BM, int BN> __device__ __forceinline__ bool find(const GroupedProduct &g) {
+    // One tile of the forward product or the rows' gradient.
+    template <Direction D, int BM, int BN> __device__ __forceinline__ void rows(const GroupedProduct &g, const Tile &t) {
         const T *x = static_cast<const T *>(g.x), *w = static_cast<const T *>(g.w), *dy = static_cast<const T *>(g.dy);
-        c = static_cast<O *>(g.out);
-        if (D == kWeights) {
-            const int nt = (g.n + BM - 1) / BM, kt = (g.k + BN - 1) / BN;
-            const int e = blockIdx.x / (nt * kt), t = blockIdx.x % (nt * kt), m0 = t / kt * BM, j0 = t % kt * BN;
-            int64_t lo, hi;
-            group_rows(g, e + 1, lo, hi);
-            lo = uniform64(lo), hi = uniform64(hi);
-            a = dy + lo * g.lddy + m0, lda = g.lddy, m_rows = g.n - m0;
-            b = x + lo * g.ldx + j0, ldb = g.ldx, j_rows = g.k - j0;
-            depth = hi - lo;
-            c += ((int64_t)e * g.n + m0) * g.k + j0;
-            return true;
-        }
-        const int cols = D == kForward ? g.n : g.k;
-        const Tile t = find_tile<BM>(g, (cols + BN - 1) / BN);
-        if (t.none) return false;
         const int j0 = t.col * BN;
         const int64_t e = t.group < 0 ? 0 : t.group;
-        m_rows = t.end - t.row, j_rows = cols - j0;
+        m_rows = t.end - t.row, j_rows = (D == kForward ? g.n : g.k) - j0;
         if (D == kForward) {
-            a = x + t.row * g.ldx, lda = g.ldx;
+            a = x + t.row * g.ldx, lda = (int)g.ldx;
             b = w + (e * g.n + j0) * g.k, ldb = g.k;
             depth = g.k;
         } else {
-            a = dy + t.row * g.lddy, lda = g.lddy;
+            a = dy + t.row * g.lddy, lda = (int)g.lddy;
             b = w + e * g.n * g.k + j0, ldb = g.k;
             depth = g.n;
         }
         if (t.group < 0) depth = 0;
-        c += t.row * g.ldo + j0;
-        return true;
+        c = static_cast<O *>(g.out) + t.row * g.ldo + j0;
+    }
+
+    // This workgroup's tile of the weights' gradient.
+    template <int BM, int BN> __device__ __forceinline__ void weights(const GroupedProduct &g) {
+        const int nt = (g.n + BM - 1) / BM, kt = (g.k + BN - 1) / BN;
+        const int e = __builtin_amdgcn_readfirstlane(blockIdx.x / (nt * kt)), t = blockIdx.x % (nt * kt);
+        const int m0 = __builtin_amdgcn_readfirstlane(t / kt * BM), j0 = __builtin_amdgcn_readfirstlane(t % kt * BN);
+        int lo, hi;
+        group_rows(g, e, lo, hi);
+        a = static_cast<const T *>(g.dy) + lo * g.lddy + m0, lda = (int)g.lddy, m_rows = g.n - m0;
+        b = static_cast<const T *>(g.x) + lo * g.ldx + j0, ldb = (int)g.ldx, j_rows = g.k - j0;
+        depth = hi - lo;
+        c = static_cast<O *>(g.out) + ((int64_t)e * g.n + m0) * g.k + j0;
     }
 };
 
@@ -253,7 +271,13 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
     constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
     __shared__ Pack<T> lds[2][2][kTile * 8];
     Part<T, O> p;
-    if (!p.template find<D, kTile, kTile>(a)) return;
+    if (D == kWeights) {
+        p.template weights<kTile, kTile>(a);
+    } else {
+        const Tile t = Deal<kTile>(a, ((D == kForward ? a.n : a.k) + kTile - 1) / kTile).get(a, blockIdx.x / kXcds);
+        if (t.none) return;
+        p.template rows<D, kTile, kTile>(a, t);
+    }
     const T *A = p.a, *B = p.b;
     const int64_t lda = p.lda, ldb = p.ldb, m_rows = p.m_rows, j_rows = p.j_rows, depth = p.depth;
     O *c = p.c;
@@ -322,39 +346,42 @@ __device__ __forceinline__ void load_to_lds(u32x4 r, int at, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(r) : "memory");
 }
 
-// One operand's loads: 4 of 16 bytes a lane and step.
+// One operand's loads: 4 of 16 bytes a lane and step, each 64 rows (along) or 16 i
+// (across) on from the one before.
 template <typename T, bool ACROSS, bool J> struct Feed {
-    const char *base;     // of the current step
-    int64_t left;         // i from this step on
-    int64_t ld;           // bytes
+    const char *base;     // of the step to load next
+    int left;             // i from that step on
+    int ld;               // bytes
     int rows, at[4];      // rows (along) or columns (across) that exist; the lane's byte offsets
-
-    __device__ __forceinline__ void begin(const T *p, int64_t ld_elems, int64_t have, int64_t depth) {
-        base = reinterpret_cast<const char *>(p), ld = ld_elems * 2, left = depth;
-        rows = (int)(have < kBig ? have : kBig);
-#pragma unroll
-        for (int s = 0; s < 4; s++) {
-            const int q = threadIdx.x + s * 512;   // LDS chunk this lane's load fills; the permutation is its own inverse
-            if (ACROSS) {
-                const int i = q >> 5, c = (J ? across_j<kBig>(i, q & 31) : across_m<kBig>(i, q & 31)) - i * 32;
-                at[s] = i * (int)ld + c * 16;
-            } else {
-                const int r = q >> 3, c = (J ? along_j(r, q & 7) : along_m(r, q & 7)) - r * 8;
-                at[s] = r * (int)ld + c * 16;
-            }
-        }
-    }
-
-    u32x4 range;      // buffer descriptor of the step being loaded
+    u32x4 range;          // buffer descriptor of the step being loaded; empty past the last
     uint32_t dst;
 
+    __device__ __forceinline__ explicit Feed(int ld_elems) {
+        ld = ld_elems * 2;
+        const int q = threadIdx.x;   // LDS chunk the lane's first load fills; the permutation is its own inverse
+        if (ACROSS)
+            at[0] = (q >> 5) * ld + ((J ? across_j<kBig>(q >> 5, q & 31) : across_m<kBig>(q >> 5, q & 31)) & 31) * 16;
+        else
+            at[0] = (q >> 3) * ld + ((J ? along_j(q >> 3, q & 7) : along_m(q >> 3, q & 7)) & 7) * 16;
+#pragma unroll
+        for (int s = 1; s < 4; s++) at[s] = at[0] + s * (ACROSS ? 16 : 64) * ld;
+    }
+
+    __device__ __forceinline__ void turn_to(const T *p, int have, int depth) {
+        base = reinterpret_cast<const char *>(p), left = depth;
+        rows = have < kBig ? have : kBig;
+    }
+
     __device__ __forceinline__ void next(const char *lds) {
-        const int64_t bytes = ACROSS ? ((left < 64 ? left : 64) - 1) * ld + rows * 2 : (rows - 1) * ld + left * 2;
-        // the range is checked by words of 4 bytes: the last element's own word has to be inside
+        // below 2^31, as 256 rows are; checked by words of 4 bytes, so the last element's own word has to be inside
+        uint32_t bytes = ACROSS ? ((left < 64 ? left : 64) - 1) * ld + rows * 2 : (rows - 1) * ld + left * 2;
+        bytes = left > 0 ? (bytes + 3) & ~3u : 0;
         const uint64_t at0 = reinterpret_cast<uint64_t>(base);
-        range = u32x4{(uint32_t)at0, (uint32_t)(at0 >> 32) & 0xffff, left > 0 ? (uint32_t)((bytes + 3) & ~3ll) : 0, 0x00020000};
+        range = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)at0),
+                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(at0 >> 32) & 0xffff),
+                      (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000};
         dst = lds_address(lds) + (__builtin_amdgcn_readfirstlane(threadIdx.x) >> 6) * 1024;
-        base += ACROSS ? 64 * ld : 128;
+        base += ACROSS ? 64 * (int64_t)ld : 128;
         left -= 64;
     }
 
@@ -367,7 +394,10 @@ template <typename T, bool ACROSS, bool J> struct Feed {
     }
 };
 
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All but the last N loads (and stores) of this wave have ended, and its LDS reads.
+template <int N> __device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 
 // A barrier alone: what it orders is waited for where it is needed.
 __device__ __forceinline__ void barrier() {
@@ -427,41 +457,70 @@ template <typename F> __device__ __forceinline__ void mask_frag(F &f, int left) 
 
 template <typename T, typename O, Direction D> __global__ __launch_bounds__(512) void k_product_big(GroupedProduct a) {
     constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
+    constexpr int kStores = 8 * 16 / kVec<O>;   // of a wave that stores a whole tile
     typedef typename Mfma<T>::Frag Frag;
     __shared__ __attribute__((aligned(1024))) char lds[2][kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = (wave >> 2) * 128, wj = (wave & 3) * 64;
+    // A step is four groups of 16 products: i halves h, and for each the wave's upper
+    // and lower rows of A.  Each group's fragments are read while the group before
+    // it multiplies.  By the middle of a step all of it has been read and the next
+    // step has arrived, so one barrier a step is enough: after it the step after next
+    // is loaded into this step's half of LDS.
+    Frag f[3][4], g[2][4];
+    f32x4 acc[8][4];
+    const Reader<T, A_ACROSS, false> ra(wm);
+    const Reader<T, B_ACROSS, true> rb(wj);
+    const uint32_t stage0 = lds_address(lds[0]);
+    // four products, and what is issued behind them
+    const auto multiply = [&](const Frag &fm, const Frag(&gj)[4], int m) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[m][j] = Mfma<T>::go(gj[j], fm, acc[m][j]);
+    };
+    const auto mask = [&](Frag(&of)[4], int left, int h) {
+#pragma unroll
+        for (int m = 0; m < 4; m++) mask_frag(of[m], left - h * 32 - ((threadIdx.x & 63) >> 4) * 8);
+    };
+
     Part<T, O> p;
-    if (!p.template find<D, kBig, kBig>(a)) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = (wave >> 2) * 128, wj = (wave & 3) * 64;
-    f32x4 acc[8][4] = {};
-    if (p.depth > 0) {
-        Feed<T, A_ACROSS, false> fa;
-        Feed<T, B_ACROSS, true> fb;
-        fa.begin(p.a, p.lda, p.m_rows, p.depth);
-        fb.begin(p.b, p.ldb, p.j_rows, p.depth);
-        const int steps = (int)((p.depth + 63) >> 6);
-        // A step is four groups of 16 products: i halves h, and for each the wave's upper
-        // and lower rows of A.  Each group's fragments are read while the group before
-        // it multiplies.  Before the last one everything of the step has been read and
-        // the next step has arrived, so one barrier a step is enough: after it the
-        // step after next is loaded into this step's half of LDS.
-        Frag f[3][4], g[2][4];
-        const Reader<T, A_ACROSS, false> ra(wm);
-        const Reader<T, B_ACROSS, true> rb(wj);
-        const uint32_t stage0 = lds_address(lds[0]);
-        // four products, and what is issued behind them
-        const auto multiply = [&](const Frag &fm, const Frag(&gj)[4], int m) {
+    const Deal<kBig> deal(a, D == kWeights ? 1 : ((D == kForward ? a.n : a.k) + kBig - 1) / kBig);
+    uint32_t turn = blockIdx.x / kXcds;
+    if (D == kWeights) {
+        p.template weights<kBig, kBig>(a);
+    } else {
+        const Tile t = deal.get(a, turn);
+        if (t.none) return;
+        p.template rows<D, kBig, kBig>(a, t);
+    }
+    Feed<T, A_ACROSS, false> fa(p.lda);
+    Feed<T, B_ACROSS, true> fb(p.ldb);
+    // the first two steps of a tile; the second may be past its end
+    const auto feed = [&]() {
+        if (p.depth <= 0) return;
+        fa.turn_to(p.a, p.m_rows, p.depth);
+        fb.turn_to(p.b, p.j_rows, p.depth);
 #pragma unroll
-            for (int j = 0; j < 4; j++) acc[m][j] = Mfma<T>::go(gj[j], fm, acc[m][j]);
-        };
-        const auto mask = [&](Frag(&of)[4], int left, int h) {
+        for (int u = 0; u < 2; u++) {
+            fa.load(lds[u]);
+            fb.load(lds[u] + kStage / 2);
+        }
+    };
+    feed();
+    bool stored = false;   // kStores stores of the tile before are in flight behind this tile's first loads
+    for (;;) {
+        Tile after;
+        after.none = true;
+        if (D != kWeights) after = deal.get(a, turn += gridDim.x / kXcds);
 #pragma unroll
-            for (int m = 0; m < 4; m++) mask_frag(of[m], left - h * 32 - ((threadIdx.x & 63) >> 4) * 8);
-        };
-        fa.load(lds[0]);
-        fb.load(lds[0] + kStage / 2);
-        fa.load(lds[1]);
-        fb.load(lds[1] + kStage / 2);
-        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        for (int m = 0; m < 8; m++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[m][j] = 0.0f;
+        if (p.depth > 0) {
+        const int steps = (p.depth + 63) >> 6;
+        if (stored)
+            wait_loads<8 + kStores>();
+        else
+            wait_loads<8>();
         barrier();
         // this step's and the next step's places, each operand's; the compiler would
         // keep every fragment's address of both in registers, more than there are
@@ -492,7 +551,11 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
             }
             fa.next(cur);
             fb.next(cur + kStage / 2);
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            // all loads are the next step's; in a tile's first step the stores follow them
+            if (t == 0 && stored)
+                wait_loads<kStores>();
+            else
+                wait_loads<0>();
             barrier();
 #pragma unroll
             for (int m = 0; m < 4; m++) {
@@ -513,7 +576,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
             const uint32_t ta = at_a, tb = at_b;
             at_a = other_a, at_b = other_b, other_a = ta, other_b = tb;
         }
-        const int left = (int)(p.depth - (int64_t)(steps - 1) * 64);
+        const int left = p.depth - (steps - 1) * 64;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
 #pragma unroll
@@ -529,13 +592,28 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
 #pragma unroll
             for (int m = 0; m < 8; m++) multiply(f[m >> 2][m & 3], g[0], m);
         }
-        wait_loads();   // of nothing but zeros, yet into this workgroup's LDS
-    }
-    const int lane = threadIdx.x & 63;
+        }
+        // the last loads, past the end, filled LDS with 0; nobody reads LDS any more
+        wait_loads<0>();
+        barrier();
+        O *c = p.c;
+        const int m_rows = p.m_rows, j_rows = p.j_rows;
+        if (!after.none) {   // the next tile's loads go before this one's stores
+            p.template rows<D, kBig, kBig>(a, after);
+            feed();
+        }
+        stored = m_rows >= kBig && j_rows >= kBig;
+        c += (wm + (lane & 15)) * a.ldo + wj + (lane >> 4) * 16;
+        if (stored) {
 #pragma unroll
-    for (int m = 0; m < 8; m++) {
-        const int row = wm + m * 16 + (lane & 15), col = wj + (lane >> 4) * 16;
-        if (row < p.m_rows && col < p.j_rows) store16<T, O>(p.c + row * a.ldo + col, p.j_rows - col, acc[m]);
+            for (int m = 0; m < 8; m++) store16<T, O>(c + m * 16 * a.ldo, 16, acc[m]);
+        } else {
+            const int row = wm + (lane & 15), col = wj + (lane >> 4) * 16;
+#pragma unroll
+            for (int m = 0; m < 8; m++)
+                if (row + m * 16 < m_rows && col < j_rows) store16<T, O>(c + m * 16 * a.ldo, j_rows - col, acc[m]);
+        }
+        if (after.none) return;
     }
 }
 
@@ -553,9 +631,14 @@ template <int BM, int BN, Direction D> int64_t blocks_for(const GroupedProduct &
     return (tiles + kXcds - 1) / kXcds * kXcds;
 }
 
+constexpr int kCus = 256;
+
 template <typename T, typename O, Direction D> int go(const GroupedProduct &a, void *stream) {
-    if (feeds_big<D>(a) && (D == kWeights || a.rows / a.groups >= 128))
-        return launch(k_product_big<T, O, D>, blocks_for<kBig, kBig, D>(a), 512, stream, a);
+    if (feeds_big<D>(a) && (D == kWeights || a.rows / a.groups >= 128)) {
+        int64_t blocks = blocks_for<kBig, kBig, D>(a);
+        if (D != kWeights && blocks > kCus) blocks = kCus;   // one a CU: LDS holds no second
+        return launch(k_product_big<T, O, D>, blocks, 512, stream, a);
+    }
     return launch(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
 }
 
