@@ -146,17 +146,15 @@ __device__ __forceinline__ void group_rows(const GroupedProduct &a, int e, int &
 // LDS places, in 16-byte chunks.  "Along": row r, chunk c (8 i) of a row of 8
 // chunks; "across": i row, chunk c (8 columns) of a row of R / 8.  The chunk is
 // permuted by a function of the row so that the 16 lanes that read together
-// reach different banks.  On the j side a lane's 16 MFMA rows are j = 16 q + 4 t + r
-// (q = lane / 4 % 4, r = lane % 4, t the fragment), so that the four fragments
-// of a lane end as 16 consecutive columns of c, stored together.
+// reach different banks.  On the j side fragment t's MFMA rows are j = 32 (t / 2) +
+// 8 q + 4 (t % 2) + r (q = lane / 4 % 4, r = lane % 4), so that two fragments of a lane
+// end as 8 consecutive columns of c, and four lanes' stores as 64 adjacent bytes.
 __device__ __forceinline__ int along_m(int r, int c) { return r * 8 + (c ^ ((r >> 1) & 7)); }
-__device__ __forceinline__ int along_j(int r, int c) { return r * 8 + (c ^ (((r >> 1) & 1) | ((r >> 3) & 6))); }
+__device__ __forceinline__ int along_j(int r, int c) { return r * 8 + (c ^ (((r >> 1) & 1) | ((r >> 2) & 6))); }
 template <int R> __device__ __forceinline__ int across_m(int i, int c) {
     return i * (R / 8) + (c ^ (2 * ((i & 3) | ((i >> 1) & 4))));
 }
-template <int R> __device__ __forceinline__ int across_j(int i, int c) {
-    return i * (R / 8) + (c ^ ((i & 1) | ((i & 2) << 2)));
-}
+template <int R> __device__ __forceinline__ int across_j(int i, int c) { return i * (R / 8) + (c ^ ((i & 3) << 2)); }
 
 // What one workgroup computes at a time: m_rows x j_rows of c (at most a tile of
 // them) from `depth` of the contraction.
@@ -234,12 +232,12 @@ __device__ __forceinline__ typename Mfma<T>::Frag frag(const Pack<T> *lds, int f
     typedef typename Mfma<T>::Frag Frag;
     const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
     if (!ACROSS) {
-        const int r = first + (J ? (l >> 2) * 16 + t * 4 + (l & 3) : t * 16 + l);
+        const int r = first + (J ? (t >> 1) * 32 + (l >> 2) * 8 + (t & 1) * 4 + (l & 3) : t * 16 + l);
         const int c = h * 4 + q;
         return *reinterpret_cast<const Frag *>(lds + (J ? along_j(r, c) : along_m(r, c)));
     }
     // 4 rows of i x 16 columns a transposing read: a lane gives 4 columns of one row, and gets one column's 4 rows
-    const int col = first + (J ? (l & 3) * 16 + t * 4 : t * 16 + (l & 3) * 4);
+    const int col = first + (J ? (t >> 1) * 32 + (l & 3) * 8 + (t & 1) * 4 : t * 16 + (l & 3) * 4);
     union {
         Frag f;
         s16x4 half[2];
@@ -255,15 +253,16 @@ __device__ __forceinline__ typename Mfma<T>::Frag frag(const Pack<T> *lds, int f
     return u.f;
 }
 
-// A lane's 16 consecutive columns of one row of c.
-template <typename T, typename O> __device__ __forceinline__ void store16(O *p, int64_t n, const f32x4 (&v)[4]) {
+// A lane's columns of one row of c: 8 from p on and 8 from p + 32 on, of the n that exist.
+template <typename O> __device__ __forceinline__ void store_row(O *p, int n, const f32x4 (&v)[4]) {
     constexpr int V = kVec<O>;
 #pragma unroll
     for (int s = 0; s < 16; s += V) {
+        const int at = (s & 7) + (s >> 3) * 32;
         Pack<O> o;
 #pragma unroll
         for (int j = 0; j < V; j++) o.e[j] = (O)v[(s + j) >> 2][(s + j) & 3];
-        if (n > s) store_pack(p + s, n - s, o);
+        if (n > at) store_pack(p + at, n - at, o);
     }
 }
 
@@ -319,8 +318,8 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int m = 0; m < 4; m++) {
-        const int row = wm + m * 16 + (lane & 15), col = wj + (lane >> 4) * 16;
-        if (row < m_rows && col < j_rows) store16<T, O>(c + row * a.ldo + col, j_rows - col, acc[m]);
+        const int row = wm + m * 16 + (lane & 15), col = wj + (lane >> 4) * 8;
+        if (row < m_rows && col < j_rows) store_row(c + row * a.ldo + col, (int)(j_rows - col), acc[m]);
     }
 }
 
@@ -418,24 +417,24 @@ template <typename T, bool ACROSS, bool J> struct Reader {
     __device__ __forceinline__ explicit Reader(int first) {
         const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
         if (ACROSS) {
-            const int i = q * 8 + (l >> 2), col = first + (J ? (l & 3) * 16 : (l & 3) * 4);
+            const int i = q * 8 + (l >> 2), col = first + (J ? (l & 3) * 8 : (l & 3) * 4);
             base = (J ? across_j<kBig>(i, col >> 3) : across_m<kBig>(i, col >> 3)) * 16 + (col & 4) * 2;
         } else {
-            const int r = first + (J ? (l >> 2) * 16 + (l & 3) : l);
+            const int r = first + (J ? (l >> 2) * 8 + (l & 3) : l);
             base = (J ? along_j(r, q) : along_m(r, q)) * 16;
         }
     }
 
     static __device__ __forceinline__ void read(Frag &to, uint32_t at, int t, int h) {
         if (!ACROSS) {
-            to = *(__attribute__((address_space(3))) const Frag *)(uintptr_t)((at ^ (h * 64)) + t * (J ? 512 : 2048));
+            to = *(__attribute__((address_space(3))) const Frag *)(uintptr_t)((at ^ (h * 64)) + (J ? (t >> 1) * 4096 + (t & 1) * 512 : t * 2048));
             return;
         }
         union {
             Frag f;
             s16x4 half[2];
         } u;
-        const uint32_t col = J ? (at ^ ((t >> 1) * 16)) + (t & 1) * 8 : at ^ (t * 32);
+        const uint32_t col = J ? (at ^ ((t >> 1) * 64)) + (t & 1) * 8 : at ^ (t * 32);
 #pragma unroll
         for (int s = 0; s < 2; s++)
             u.half[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -603,15 +602,15 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
             feed();
         }
         stored = m_rows >= kBig && j_rows >= kBig;
-        c += (wm + (lane & 15)) * a.ldo + wj + (lane >> 4) * 16;
+        c += (wm + (lane & 15)) * a.ldo + wj + (lane >> 4) * 8;
         if (stored) {
 #pragma unroll
-            for (int m = 0; m < 8; m++) store16<T, O>(c + m * 16 * a.ldo, 16, acc[m]);
+            for (int m = 0; m < 8; m++) store_row(c + m * 16 * a.ldo, 64, acc[m]);
         } else {
-            const int row = wm + (lane & 15), col = wj + (lane >> 4) * 16;
+            const int row = wm + (lane & 15), col = wj + (lane >> 4) * 8;
 #pragma unroll
             for (int m = 0; m < 8; m++)
-                if (row + m * 16 < m_rows && col < j_rows) store16<T, O>(c + m * 16 * a.ldo, j_rows - col, acc[m]);
+                if (row + m * 16 < m_rows && col < j_rows) store_row(c + m * 16 * a.ldo, j_rows - col, acc[m]);
         }
         if (after.none) return;
     }
