@@ -143,6 +143,22 @@ __device__ __forceinline__ void group_rows(const GroupedProduct &a, int e, int &
     }
 }
 
+// The group with the `rank`-th most rows (ties to the lower one): the weights' gradient
+// begins with the longest groups, so that the workgroups that start last have the
+// least to do.  More groups than lanes keep their own order; their lengths even out.
+__device__ __forceinline__ int longest(const GroupedProduct &a, int rank) {
+    if (a.groups == 1 || a.groups > 62) return rank;
+    const Ranges r(a, 0, 0, 1 << 30);
+    const int lane = threadIdx.x & 63;
+    const int mine = lane >= 1 && lane <= a.groups ? r.hi - r.lo : -1;
+    int above = 0;
+    for (int l = 1; l <= a.groups; l++) {
+        const int other = __builtin_amdgcn_readlane(mine, l);
+        above += other > mine || (other == mine && l < lane);
+    }
+    return __builtin_ctzll(__ballot(mine >= 0 && above == rank)) - 1;
+}
+
 // LDS places, in 16-byte chunks.  "Along": row r, chunk c (8 i) of a row of 8
 // chunks; "across": i row, chunk c (8 columns) of a row of R / 8.  The chunk is
 // permuted by a function of the row so that the 16 lanes that read together
@@ -182,17 +198,30 @@ template <typename T, typename O> struct Part {
         c = static_cast<O *>(g.out) + t.row * g.ldo + j0;
     }
 
-    // This workgroup's tile of the weights' gradient.
+    // This workgroup's tile of the weights' gradient: of one group, or of one of the
+    // a.splits equal runs of 64-row steps that the group's rows are cut into (each
+    // run's sums are a matrix of their own).
     template <int BM, int BN> __device__ __forceinline__ void weights(const GroupedProduct &g) {
-        const int nt = (g.n + BM - 1) / BM, kt = (g.k + BN - 1) / BN;
-        const int e = __builtin_amdgcn_readfirstlane(blockIdx.x / (nt * kt)), t = blockIdx.x % (nt * kt);
+        const uint32_t nt = (g.n + BM - 1) / BM, kt = (g.k + BN - 1) / BN, tiles = nt * kt;
+        const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles);
+        // workgroups go round the XCDs: an XCD gets neighbouring tiles of a group
+        uint32_t t = blockIdx.x - item * tiles;
+        if (tiles % kXcds == 0) t = t % kXcds * (tiles / kXcds) + t / kXcds;
         const int m0 = __builtin_amdgcn_readfirstlane(t / kt * BM), j0 = __builtin_amdgcn_readfirstlane(t % kt * BN);
+        const int part = __builtin_amdgcn_readfirstlane(item / g.groups), e = longest(g, item - part * g.groups);
         int lo, hi;
         group_rows(g, e, lo, hi);
+        if (g.splits > 1) {
+            const uint32_t steps = (hi - lo + 63) >> 6;
+            const int from = __builtin_amdgcn_readfirstlane((uint64_t)steps * part / g.splits) * 64;
+            const int to = __builtin_amdgcn_readfirstlane((uint64_t)steps * (part + 1) / g.splits) * 64;
+            hi = lo + to < hi ? lo + to : hi;
+            lo += from;
+        }
         a = static_cast<const T *>(g.dy) + lo * g.lddy + m0, lda = (int)g.lddy, m_rows = g.n - m0;
         b = static_cast<const T *>(g.x) + lo * g.ldx + j0, ldb = (int)g.ldx, j_rows = g.k - j0;
         depth = hi - lo;
-        c = static_cast<O *>(g.out) + ((int64_t)e * g.n + m0) * g.k + j0;
+        c = static_cast<O *>(g.out) + (((int64_t)part * g.groups + e) * g.n + m0) * g.k + j0;
     }
 };
 
@@ -329,7 +358,6 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
 // lane): the buffer's range ends at the operand's last element, so what a tile
 // overhangs reads as 0.  Only what lies past i = depth in a row along i is
 // inside that range; the fragments of the last step are masked there.
-constexpr int kBig = 256;
 constexpr int kStage = 2 * kBig * 8 * 16;   // bytes of one step's two operands in LDS
 
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
@@ -624,13 +652,28 @@ template <Direction D> bool feeds_big(const GroupedProduct &a) {
 }
 
 template <int BM, int BN, Direction D> int64_t blocks_for(const GroupedProduct &a) {
-    if (D == kWeights) return (int64_t)a.groups * ((a.n + BM - 1) / BM) * ((a.k + BN - 1) / BN);
+    if (D == kWeights) return (int64_t)a.splits * a.groups * ((a.n + BM - 1) / BM) * ((a.k + BN - 1) / BN);
     const int cols = D == kForward ? a.n : a.k;
     const int64_t tiles = (a.rows / BM + a.groups + 2) * ((cols + BN - 1) / BN);
     return (tiles + kXcds - 1) / kXcds * kXcds;
 }
 
-constexpr int kCus = 256;
+// The sum of a.splits matrices of `count` elements, in order.
+template <typename O> __global__ __launch_bounds__(256) void k_join(GroupedProduct a, int64_t count) {
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t n = count - at;
+    if (n <= 0) return;
+    f32x4 sum = 0.0f;
+    for (int p = 0; p < a.splits; p++) {
+        const Pack<float> v = load_pack(a.partial + p * count + at, n, 0.0f);
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum[j] += v.e[j];
+    }
+    O *out = static_cast<O *>(a.out) + at;
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+        if (j < n) out[j] = (O)sum[j];
+}
 
 template <typename T, typename O, Direction D> int go(const GroupedProduct &a, void *stream) {
     if (feeds_big<D>(a) && (D == kWeights || a.rows / a.groups >= 128)) {
@@ -639,6 +682,16 @@ template <typename T, typename O, Direction D> int go(const GroupedProduct &a, v
         return launch(k_product_big<T, O, D>, blocks, 512, stream, a);
     }
     return launch(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
+}
+
+template <typename T> int weights(const GroupedProduct &a, void *stream) {
+    const bool narrow = a.out_dtype != PASE_FP32;
+    if (a.splits == 1) return narrow ? go<T, T, kWeights>(a, stream) : go<T, float, kWeights>(a, stream);
+    GroupedProduct parts = a;
+    parts.out = a.partial;
+    if (const int e = go<T, float, kWeights>(parts, stream)) return e;
+    const int64_t count = (int64_t)a.groups * a.n * a.k, blocks = (count + 1023) / 1024;
+    return narrow ? launch(k_join<T>, blocks, 256, stream, a, count) : launch(k_join<float>, blocks, 256, stream, a, count);
 }
 
 template <Direction D> int by_type(const GroupedProduct &a, void *stream) {
@@ -651,6 +704,8 @@ template <Direction D> int by_type(const GroupedProduct &a, void *stream) {
 
 int launch_product_forward(const GroupedProduct &a, void *stream) { return by_type<kForward>(a, stream); }
 int launch_product_rows_grad(const GroupedProduct &a, void *stream) { return by_type<kRowsGrad>(a, stream); }
-int launch_product_weights_grad(const GroupedProduct &a, void *stream) { return by_type<kWeights>(a, stream); }
+int launch_product_weights_grad(const GroupedProduct &a, void *stream) {
+    return a.dtype == PASE_BF16 ? weights<__bf16>(a, stream) : weights<_Float16>(a, stream);
+}
 
 }  // namespace pase

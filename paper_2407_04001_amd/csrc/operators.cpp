@@ -165,7 +165,13 @@ int norm_backward_blocks(int dtype, int64_t rows, int width) {
 
 int softmax_loss_splits(int, int64_t, int64_t) { return 1; }
 
-int grouped_matmul_splits(int64_t, int, int, int) { return 1; }
+// A part a CU, while parts of an average group keep 512 rows: with fewer tiles than
+// CUs the rest would be idle, and a part's sums are written and read once more.
+int grouped_matmul_splits(int64_t rows, int groups, int n, int k) {
+    const int64_t tiles = (int64_t)groups * ((n + kBig - 1) / kBig) * ((k + kBig - 1) / kBig);
+    const int64_t idle = kCus / tiles, deep = rows / groups / 512, most = idle < deep ? idle : deep;
+    return (int)(most < 1 ? 1 : most > 32 ? 32 : most);
+}
 
 }  // namespace pase
 

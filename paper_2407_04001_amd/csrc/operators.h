@@ -65,6 +65,8 @@ int softmax_loss_splits(int dtype, int64_t rows, int64_t classes);
 // parts each group's rows are cut into by the weights' gradient
 int grouped_matmul_splits(int64_t rows, int groups, int n, int k);
 
+constexpr int kCus = 256;          // compute units of an MI355X
+constexpr int kBig = 256;          // rows and columns of a tile of the grouped products
 constexpr int kGradVecs = 1024;   // 16-byte vectors of a row that one workgroup of the loss gradient takes
 
 // Launches: 0 or a hipError_t.
