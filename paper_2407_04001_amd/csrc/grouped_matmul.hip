@@ -644,6 +644,157 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
     }
 }
 
+// ---------------------------------------------------------------- few rows
+// Forward with few rows a group: what counts is reading each weight once.  A
+// workgroup takes 16 MT rows and 32 columns; its four waves take every fourth 32 of
+// the contraction, straight from HBM to the matrix unit (a lane's 16 bytes are its
+// part of a fragment), and add up through LDS.
+template <typename T, typename O, int MT> __global__ __launch_bounds__(256) void k_product_thin(GroupedProduct a) {
+    typedef typename Mfma<T>::Frag Frag;
+    union Piece {
+        Pack<T> p;
+        Frag f;
+    };
+    constexpr int JT = 2, BM = 16 * MT, BN = 16 * JT;
+    __shared__ f32x4 join[3][MT * JT][64];
+    const Tile tile = Deal<BM>(a, (a.n + BN - 1) / BN).get(a, blockIdx.x / kXcds);
+    if (tile.none) return;
+    Part<T, O> p;
+    p.template rows<kForward, BM, BN>(a, tile);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
+    f32x4 acc[MT][JT] = {};
+    // rows past the end read the last one again; they are not stored
+    const T *pa[MT], *pb[JT];
+#pragma unroll
+    for (int m = 0; m < MT; m++) {
+        const int r = m * 16 + l;
+        pa[m] = p.a + (int64_t)(r < p.m_rows ? r : p.m_rows - 1) * p.lda;
+    }
+#pragma unroll
+    for (int j = 0; j < JT; j++) {   // MFMA row 4 h + r of fragment j is column 8 h + 4 j + r, as in frag()
+        const int r = (l >> 2) * 8 + j * 4 + (l & 3);
+        pb[j] = p.b + (int64_t)(r < p.j_rows ? r : p.j_rows - 1) * p.ldb;
+    }
+    // (Holding the next pieces in registers as well was no faster: 12-24 rows a group
+    // 20.7-26.2 us against 18.7-22.7, 8 groups of 1024 x 4096.)
+    for (int i = wave * 32 + q * 8; i - q * 8 < p.depth; i += 128) {   // past the end 0
+        const int n = p.depth - i;
+        Piece fa[MT], fb[JT];
+#pragma unroll
+        for (int j = 0; j < JT; j++) fb[j].p = load_pack(pb[j] + i, n, (T)0.0f);
+#pragma unroll
+        for (int m = 0; m < MT; m++) fa[m].p = load_pack(pa[m] + i, n, (T)0.0f);
+#pragma unroll
+        for (int m = 0; m < MT; m++)
+#pragma unroll
+            for (int j = 0; j < JT; j++) acc[m][j] = Mfma<T>::go(fb[j].f, fa[m].f, acc[m][j]);
+    }
+    if (wave)
+#pragma unroll
+        for (int t = 0; t < MT * JT; t++) join[wave - 1][t][lane] = acc[t / JT][t % JT];
+    __syncthreads();
+    if (wave) return;
+    const int col = q * 8;
+    constexpr int V = kVec<O>;
+#pragma unroll
+    for (int m = 0; m < MT; m++) {
+#pragma unroll
+        for (int j = 0; j < JT; j++)
+#pragma unroll
+            for (int w = 0; w < 3; w++) acc[m][j] += join[w][m * JT + j][lane];
+        const int r = m * 16 + l;
+        if (r >= p.m_rows) continue;
+        O *c = p.c + r * a.ldo + col;
+#pragma unroll
+        for (int s = 0; s < 8; s += V) {
+            Pack<O> o;
+#pragma unroll
+            for (int j = 0; j < V; j++) o.e[j] = (O)acc[m][(s + j) >> 2][(s + j) & 3];
+            if (p.j_rows > col + s) store_pack(c + s, p.j_rows - col - s, o);
+        }
+    }
+}
+
+// The rows' gradient with few rows a group: as above with 64 columns a workgroup, but
+// w's rows run across, so each wave passes its 32 x 64 of w through LDS of its own
+// (no barriers) for the transposing reads.  The next 32 are loaded meanwhile.
+template <typename T, int MT> __global__ __launch_bounds__(256) void k_rows_grad_thin(GroupedProduct a) {
+    typedef typename Mfma<T>::Frag Frag;
+    union Piece {
+        Pack<T> p;
+        Frag f;
+    };
+    constexpr int JT = 4, BM = 16 * MT, BN = 16 * JT, kRow = BN * 2 + 16;   // LDS bytes of a row: 16 more, for the banks
+    __shared__ __attribute__((aligned(16))) char lds[4 * 32 * kRow > 3 * MT * JT * 1024 ? 4 * 32 * kRow : 3 * MT * JT * 1024];
+    const Tile tile = Deal<BM>(a, (a.k + BN - 1) / BN).get(a, blockIdx.x / kXcds);
+    if (tile.none) return;
+    Part<T, T> p;
+    p.template rows<kRowsGrad, BM, BN>(a, tile);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
+    char *mine = lds + wave * 32 * kRow;
+    f32x4 acc[MT][JT] = {};
+    const T *pa[MT];
+#pragma unroll
+    for (int m = 0; m < MT; m++) {
+        const int r = m * 16 + l;
+        pa[m] = p.a + (int64_t)(r < p.m_rows ? r : p.m_rows - 1) * p.lda;
+    }
+    Pack<T> w[4];
+    Piece fa[MT];
+    const auto fetch = [&](int i) {   // i .. i + 31 of the contraction; past its end 0
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            const int r = s * 8 + (lane >> 3), c = (lane & 7) * 8;
+            w[s] = load_pack(p.b + (int64_t)(i + r) * p.ldb + c, i + r < p.depth ? p.j_rows - c : 0, (T)0.0f);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; m++) fa[m].p = load_pack(pa[m] + i + q * 8, p.depth - i - q * 8, (T)0.0f);
+    };
+    int i = wave * 32;
+    if (i < p.depth) fetch(i);
+    while (i < p.depth) {
+        Piece f[MT];
+#pragma unroll
+        for (int m = 0; m < MT; m++) f[m] = fa[m];
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+            reinterpret_cast<Pack<T> *>(mine + (s * 8 + (lane >> 3)) * kRow)[lane & 7] = w[s];
+        i += 128;
+        if (i < p.depth) fetch(i);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < JT; j++) {
+            union {
+                Frag f;
+                s16x4 half[2];
+            } u;
+#pragma unroll
+            for (int s = 0; s < 2; s++)   // columns as in frag(): two fragments end as 8 consecutive ones
+                u.half[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(
+                    mine + (q * 8 + s * 4 + (l >> 2)) * kRow + ((j >> 1) * 32 + (l & 3) * 8 + (j & 1) * 4) * 2));
+#pragma unroll
+            for (int m = 0; m < MT; m++) acc[m][j] = Mfma<T>::go(u.f, f[m].f, acc[m][j]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    f32x4 *join = reinterpret_cast<f32x4 *>(lds);
+    if (wave)
+#pragma unroll
+        for (int t = 0; t < MT * JT; t++) join[((wave - 1) * MT * JT + t) * 64 + lane] = acc[t / JT][t % JT];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int m = 0; m < MT; m++) {
+#pragma unroll
+        for (int j = 0; j < JT; j++)
+#pragma unroll
+            for (int o = 0; o < 3; o++) acc[m][j] += join[(o * MT * JT + m * JT + j) * 64 + lane];
+        const int r = m * 16 + l;
+        if (r < p.m_rows) store_row(p.c + r * a.ldo + q * 8, p.j_rows - q * 8, acc[m]);
+    }
+}
+
 template <Direction D> bool feeds_big(const GroupedProduct &a) {
     const auto even = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 2 == 0; };
     if (D == kForward) return even(a.x, a.ldx) && even(a.w, a.k);
@@ -675,13 +826,44 @@ template <typename O> __global__ __launch_bounds__(256) void k_join(GroupedProdu
         if (j < n) out[j] = (O)sum[j];
 }
 
+// Whether the kernels for few rows a group are the faster ones, by what bounds each
+// (microseconds; measured with 8 and 64 groups of 1024 x 4096, 4096 x 1024 and 1024 x
+// 1024).  They read the weights of the groups that have rows, once for every 64 of
+// these, at 3.6-4.6 (forward) and 5 TB/s (gradient, and 4 ns for each of its
+// contraction): 12, 48 and 200 rows a group of 8 x 1024 x 4096 forward 18, 32 and 79,
+// gradient 27, 32 and 43.  Big tiles take a time for each 64 of the contraction,
+// whatever rows are in them, and use no more CUs than there are tiles: the same
+// forward 24, 26 and 31 (128 tiles of 16 steps), gradient 73, 74 and 78 (32 tiles of 64
+// steps).  Where rows are not 4-byte aligned a tile takes 2.5 times as long.
+template <Direction D> bool few_rows(const GroupedProduct &a, bool big) {
+    const double some = (double)a.rows / a.groups, live = a.groups * (1 - __builtin_exp(-some));
+    const double reads = 2.0 * live * a.n * a.k * (some < 16 ? 1 : 0.75 + some / 64);
+    const double thin = D == kForward ? 4 + reads / (some < 16 ? 4.6e6 : 3.6e6) : 5 + reads / 5.0e6 + a.n * 0.004;
+    const int cols = ((D == kForward ? a.n : a.k) + kBig - 1) / kBig, steps = ((D == kForward ? a.k : a.n) + 63) / 64;
+    const double rounds = __builtin_ceil((some / kBig + 0.9) * a.groups * cols / kCus);
+    return thin < (7 + rounds * steps * 1.05) * (big ? 1 : 2.5);
+}
+
 template <typename T, typename O, Direction D> int go(const GroupedProduct &a, void *stream) {
-    if (feeds_big<D>(a) && (D == kWeights || a.rows / a.groups >= 128)) {
-        int64_t blocks = blocks_for<kBig, kBig, D>(a);
-        if (D != kWeights && blocks > kCus) blocks = kCus;   // one a CU: LDS holds no second
-        return launch(k_product_big<T, O, D>, blocks, 512, stream, a);
+    const bool big = feeds_big<D>(a);
+    if constexpr (D != kWeights) {
+        if (few_rows<D>(a, big)) {
+            const int64_t some = a.rows / a.groups;
+            if constexpr (D == kForward) {
+                if (some < 8) return launch(k_product_thin<T, O, 1>, blocks_for<16, 32, D>(a), 256, stream, a);
+                if (some < 16) return launch(k_product_thin<T, O, 2>, blocks_for<32, 32, D>(a), 256, stream, a);
+                return launch(k_product_thin<T, O, 4>, blocks_for<64, 32, D>(a), 256, stream, a);
+            } else {
+                if (some < 8) return launch(k_rows_grad_thin<T, 1>, blocks_for<16, 64, D>(a), 256, stream, a);
+                if (some < 16) return launch(k_rows_grad_thin<T, 2>, blocks_for<32, 64, D>(a), 256, stream, a);
+                return launch(k_rows_grad_thin<T, 4>, blocks_for<64, 64, D>(a), 256, stream, a);
+            }
+        }
     }
-    return launch(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
+    if (!big) return launch(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
+    int64_t blocks = blocks_for<kBig, kBig, D>(a);
+    if (D != kWeights && blocks > kCus) blocks = kCus;   // one a CU: LDS holds no second
+    return launch(k_product_big<T, O, D>, blocks, 512, stream, a);
 }
 
 template <typename T> int weights(const GroupedProduct &a, void *stream) {
