@@ -677,8 +677,7 @@ template <typename T, typename O, int MT> __global__ __launch_bounds__(256) void
     }
     // (Holding the next pieces in registers as well was no faster: 12-24 rows a group
     // 20.7-26.2 us against 18.7-22.7, 8 groups of 1024 x 4096.)
-    for (int i = wave * 32 + q * 8; i - q * 8 < p.depth; i += 128) {   // past the end 0
-        const int n = p.depth - i;
+    const auto step = [&](int i, int n) {   // n: how many of this lane's 8 exist; the rest are 0
         Piece fa[MT], fb[JT];
 #pragma unroll
         for (int j = 0; j < JT; j++) fb[j].p = load_pack(pb[j] + i, n, (T)0.0f);
@@ -688,7 +687,10 @@ template <typename T, typename O, int MT> __global__ __launch_bounds__(256) void
         for (int m = 0; m < MT; m++)
 #pragma unroll
             for (int j = 0; j < JT; j++) acc[m][j] = Mfma<T>::go(fb[j].f, fa[m].f, acc[m][j]);
-    }
+    };
+    const int whole = p.depth & ~127, tail = whole + wave * 32;
+    for (int i = wave * 32; i < whole; i += 128) step(i + q * 8, 8);
+    if (tail < p.depth) step(tail + q * 8, p.depth - tail - q * 8);
     if (wave)
 #pragma unroll
         for (int t = 0; t < MT * JT; t++) join[wave - 1][t][lane] = acc[t / JT][t % JT];

@@ -1,7 +1,7 @@
 // Residual add + layer norm, forward and backward (pase_operators.h).
 //
-// A row is held in registers by one team of WAVES waves, NV 16-byte vectors a
-// lane, so that it is read once although the mean, the sum of squared
+// A row is held in registers by one team of lanes (8 to 1024 of them), NV 16-byte
+// vectors a lane, so that it is read once although the mean, the sum of squared
 // deviations and the output each need all of it.  The variance is summed over
 // (z - mean)^2, not z^2 - mean^2, whose difference loses digits where the mean
 // is large.  Both passes are bound by HBM: they read and write each operand
@@ -14,23 +14,30 @@ namespace {
 
 constexpr int kThreads = 256;   // of a workgroup, unless one team is larger
 
-template <int WAVES> constexpr int kBlock = WAVES * 64 > kThreads ? WAVES * 64 : kThreads;
-template <int WAVES> constexpr int kTeams = kBlock<WAVES> / (WAVES * 64);
+template <int LANES> constexpr int kBlock = LANES > kThreads ? LANES : kThreads;
+template <int LANES> constexpr int kTeams = kBlock<LANES> / LANES;
 
-// Sum over one team.  A team of several waves that is not the whole workgroup
-// does not occur, so its barriers are the workgroup's.
-template <int WAVES, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float *lds) {
-    group_sum<WAVES>(v, lds);
+// Sums over one team, the same in each of its lanes.  A team of several waves is a
+// workgroup; `lds` holds N floats a wave.
+template <int LANES, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float *lds) {
+    if constexpr (LANES > 64) {
+        group_sum<LANES / 64>(v, lds);
+    } else {
+#pragma unroll
+        for (int d = LANES / 2; d; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; i++) v[i] += __shfl_xor(v[i], d, 64);
+    }
 }
 
-template <typename T, typename P, int NV, int WAVES>
-__global__ __launch_bounds__(kBlock<WAVES>) void k_norm_forward(NormForward a) {
-    constexpr int V = kVec<T>, kTeam = WAVES * 64;
-    static_assert(WAVES == 1 || kTeams<WAVES> == 1, "a team of several waves is a workgroup");
+template <typename T, typename P, int NV, int LANES>
+__global__ __launch_bounds__(kBlock<LANES>) void k_norm_forward(NormForward a) {
+    constexpr int V = kVec<T>, kTeam = LANES, WAVES = LANES > 64 ? LANES / 64 : 1;
+    static_assert(LANES <= 64 || kTeams<LANES> == 1, "a team of several waves is a workgroup");
     __shared__ float lds[2 * WAVES];
     const int lane = threadIdx.x % kTeam;
-    const int64_t row = (int64_t)blockIdx.x * kTeams<WAVES> + threadIdx.x / kTeam;
-    if (row >= a.rows) return;   // whole waves; with several waves a team, whole workgroups
+    const int64_t row = (int64_t)blockIdx.x * kTeams<LANES> + threadIdx.x / kTeam;
+    if (row >= a.rows) return;   // whole teams
     const T *x = static_cast<const T *>(a.x) + row * a.ldx;
     const T *r = static_cast<const T *>(a.residual) + row * a.ldr;
     const float count = (float)a.width;
@@ -57,7 +64,7 @@ __global__ __launch_bounds__(kBlock<WAVES>) void k_norm_forward(NormForward a) {
     for (int i = 0; i < NV; i++)
 #pragma unroll
         for (int j = 0; j < V; j++) s[0] += z[i][j];
-    team_sum<WAVES>(s, lds);
+    team_sum<LANES>(s, lds);
     const float mean = s[0] / count;
     float q[1] = {0};
 #pragma unroll
@@ -69,7 +76,7 @@ __global__ __launch_bounds__(kBlock<WAVES>) void k_norm_forward(NormForward a) {
             q[0] += d * d;
         }
     }
-    team_sum<WAVES>(q, lds + WAVES);
+    team_sum<LANES>(q, lds + WAVES);
     const float rstd = 1.0f / sqrtf(q[0] / count + a.eps);
     if (lane == 0) a.mean[row] = mean, a.rstd[row] = rstd;
 
@@ -104,11 +111,11 @@ __global__ __launch_bounds__(kBlock<WAVES>) void k_norm_forward(NormForward a) {
 // dx row by row, a team taking every (teams in the grid)-th row; its lanes keep
 // the sums of dy * h and dy over those rows for their own columns, which the
 // workgroup adds up and leaves as one row of `partial`.
-template <typename T, typename P, int NV, int WAVES>
-__global__ __launch_bounds__(kBlock<WAVES>) void k_norm_backward(NormBackward a) {
-    constexpr int V = kVec<T>, kTeam = WAVES * 64, TEAMS = kTeams<WAVES>;
+template <typename T, typename P, int NV, int LANES>
+__global__ __launch_bounds__(kBlock<LANES>) void k_norm_backward(NormBackward a) {
+    constexpr int V = kVec<T>, kTeam = LANES, TEAMS = kTeams<LANES>, WAVES = LANES > 64 ? LANES / 64 : 1;
     __shared__ float lds[2 * 2 * WAVES];
-    __shared__ float join[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? V * 64 + 4 : 1];
+    __shared__ float join[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? V * LANES + 4 : 1];
     const int lane = threadIdx.x % kTeam, team = threadIdx.x / kTeam;
     const P *gain = static_cast<const P *>(a.gain);
     const float inv = 1.0f / (float)a.width;
@@ -150,7 +157,7 @@ __global__ __launch_bounds__(kBlock<WAVES>) void k_norm_backward(NormBackward a)
                 s[1] += dh * h;
             }
         }
-        team_sum<WAVES>(s, lds + odd * 2 * WAVES);
+        team_sum<LANES>(s, lds + odd * 2 * WAVES);
         const float m0 = s[0] * inv, m1 = s[1] * inv;
         const T *dz = static_cast<const T *>(a.dz) + row * a.lddz;
         T *dx = static_cast<T *>(a.dx) + row * a.lddx;
@@ -179,15 +186,15 @@ __global__ __launch_bounds__(kBlock<WAVES>) void k_norm_backward(NormBackward a)
 #pragma unroll
             for (int j = 0; j < V; j++)
                 if (at + j < a.width) out[at + j] = dg[i][j], out[a.width + at + j] = db[i][j];
-        } else {   // a team is a wave: its 64 V columns of this i, one after the other
+        } else {   // the teams' LANES V columns of this i, one team after the other
 #pragma unroll
             for (int which = 0; which < 2; which++) {
                 __syncthreads();
 #pragma unroll
-                for (int j = 0; j < V; j++) join[team][j * 64 + lane] = which ? db[i][j] : dg[i][j];
+                for (int j = 0; j < V; j++) join[team][j * LANES + lane] = which ? db[i][j] : dg[i][j];
                 __syncthreads();
-                for (int c = threadIdx.x; c < V * 64; c += kBlock<WAVES>) {
-                    const int col = i * 64 * V + c, slot = (c % V) * 64 + c / V;
+                for (int c = threadIdx.x; c < V * LANES; c += kBlock<LANES>) {
+                    const int col = i * LANES * V + c, slot = (c % V) * LANES + c / V;
                     float s = 0;
 #pragma unroll
                     for (int t = 0; t < TEAMS; t++) s += join[t][slot];
@@ -218,17 +225,21 @@ template <typename P> __global__ __launch_bounds__(1024) void k_norm_sums(NormBa
     if (out) out[col < a.width ? col : col - a.width] = (P)s;
 }
 
-// Teams by row length: a wave while four vectors a lane hold the row, then a
-// workgroup of four, then of sixteen.
+// Teams by row length: the fewest lanes that hold the row in up to four vectors each
+// (two in teams below a wave, which keeps the rows of a wave's loads close).
 template <typename T, typename P, typename F> int by_width(int width, F &&f) {
-    const int vecs = (width + kVec<T> - 1) / kVec<T>;
-    if (vecs <= 64) return f.template operator()<T, P, 1, 1>();
-    if (vecs <= 128) return f.template operator()<T, P, 2, 1>();
-    if (vecs <= 256) return f.template operator()<T, P, 4, 1>();
-    if (vecs <= 1024) return f.template operator()<T, P, 4, 4>();
-    if (vecs <= 2048) return f.template operator()<T, P, 2, 16>();
-    if constexpr (sizeof(T) == 4) return f.template operator()<T, P, 4, 16>();
-    return (int)hipErrorInvalidValue;   // wider than PASE_NORM_MAX_WIDTH: refused before
+    const int vecs = norm_vectors(width, sizeof(T));
+    switch (norm_lanes(vecs)) {
+    case 8: return vecs <= 8 ? f.template operator()<T, P, 1, 8>() : f.template operator()<T, P, 2, 8>();
+    case 16: return f.template operator()<T, P, 2, 16>();
+    case 32: return f.template operator()<T, P, 2, 32>();
+    case 64: return vecs <= 128 ? f.template operator()<T, P, 2, 64>() : f.template operator()<T, P, 4, 64>();
+    case 256: return f.template operator()<T, P, 4, 256>();
+    default:
+        if (vecs <= 2048) return f.template operator()<T, P, 2, 1024>();
+        if constexpr (sizeof(T) == 4) return f.template operator()<T, P, 4, 1024>();
+        return (int)hipErrorInvalidValue;   // wider than PASE_NORM_MAX_WIDTH: refused before
+    }
 }
 
 template <typename F> int by_type(int dtype, int param_dtype, int width, F &&f) {
@@ -241,17 +252,17 @@ template <typename F> int by_type(int dtype, int param_dtype, int width, F &&f) 
 struct Forward {
     const NormForward &a;
     void *stream;
-    template <typename T, typename P, int NV, int WAVES> int operator()() {
-        return launch(k_norm_forward<T, P, NV, WAVES>, (a.rows + kTeams<WAVES> - 1) / kTeams<WAVES>, kBlock<WAVES>, stream, a);
+    template <typename T, typename P, int NV, int LANES> int operator()() {
+        return launch(k_norm_forward<T, P, NV, LANES>, (a.rows + kTeams<LANES> - 1) / kTeams<LANES>, kBlock<LANES>, stream, a);
     }
 };
 
 struct Backward {
     const NormBackward &a;
     void *stream;
-    template <typename T, typename P, int NV, int WAVES> int operator()() {
+    template <typename T, typename P, int NV, int LANES> int operator()() {
         if (a.blocks)
-            if (const int e = launch(k_norm_backward<T, P, NV, WAVES>, a.blocks, kBlock<WAVES>, stream, a)) return e;
+            if (const int e = launch(k_norm_backward<T, P, NV, LANES>, a.blocks, kBlock<LANES>, stream, a)) return e;
         if (!a.dgain && !a.dbias) return 0;
         return launch(k_norm_sums<P>, (2 * (int64_t)a.width + 63) / 64, 1024, stream, a);
     }

@@ -158,8 +158,8 @@ pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void 
 }  // namespace
 
 int norm_backward_blocks(int dtype, int64_t rows, int width) {
-    const int64_t vecs = ((int64_t)width * element_bytes(dtype) + 15) / 16;
-    const int64_t teams = vecs <= 256 ? 4 : 1, want = (rows + teams - 1) / teams;
+    const int lanes = norm_lanes(norm_vectors(width, element_bytes(dtype)));
+    const int64_t teams = lanes < 256 ? 256 / lanes : 1, want = (rows + teams - 1) / teams;
     return (int)(want < 512 ? want : 512);
 }
 

@@ -58,6 +58,11 @@ struct GroupedProduct {
     int splits;
 };
 
+// 16-byte vectors of a layer norm's row, and the lanes of the team that holds it
+inline int norm_vectors(int width, int element) { return (int)(((int64_t)width * element + 15) / 16); }
+inline int norm_lanes(int vecs) {
+    return vecs <= 16 ? 8 : vecs <= 32 ? 16 : vecs <= 64 ? 32 : vecs <= 256 ? 64 : vecs <= 1024 ? 256 : 1024;
+}
 // blocks of the layer norm's backward pass (one row of partial sums each)
 int norm_backward_blocks(int dtype, int64_t rows, int width);
 // workgroups that share a row of the softmax loss
