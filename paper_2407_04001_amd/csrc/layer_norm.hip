@@ -125,17 +125,28 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_norm_backward(NormBackward a)
 #pragma unroll
         for (int j = 0; j < V; j++) dg[i][j] = db[i][j] = 0;
 
-    int odd = 0;
-    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS, odd ^= 1) {
+    // the next row is on its way while this one is reduced
+    Pack<T> ny[NV], nz[NV];
+    float next_mean = 0, next_rstd = 0;
+    const auto fetch = [&](int64_t row) {
         const T *dy = static_cast<const T *>(a.dy) + row * a.lddy, *z = static_cast<const T *>(a.z) + row * a.ldz;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        Pack<T> py[NV], pz[NV];
+        next_mean = a.mean[row], next_rstd = a.rstd[row];
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int at = (lane + i * kTeam) * V, n = a.width - at;
-            py[i] = load_pack(dy + at, n, (T)0.0f);
-            pz[i] = load_pack(z + at, n, (T)0.0f);
+            ny[i] = load_pack(dy + at, n, (T)0.0f);
+            nz[i] = load_pack(z + at, n, (T)0.0f);
         }
+    };
+    const int64_t first = (int64_t)blockIdx.x * TEAMS + team, stride = (int64_t)gridDim.x * TEAMS;
+    if (first < a.rows) fetch(first);
+    int odd = 0;
+    for (int64_t row = first; row < a.rows; row += stride, odd ^= 1) {
+        const float mean = next_mean, rstd = next_rstd;
+        Pack<T> py[NV], pz[NV];
+#pragma unroll
+        for (int i = 0; i < NV; i++) py[i] = ny[i], pz[i] = nz[i];
+        if (row + stride < a.rows) fetch(row + stride);
         float g[NV][V];
         float s[2] = {0, 0};
 #pragma unroll
@@ -184,8 +195,13 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_norm_backward(NormBackward a)
         const int at = (lane + i * kTeam) * V;
         if (TEAMS == 1) {
 #pragma unroll
-            for (int j = 0; j < V; j++)
-                if (at + j < a.width) out[at + j] = dg[i][j], out[a.width + at + j] = db[i][j];
+            for (int h = 0; h < V; h += 4) {
+                Pack<float> g, b;
+#pragma unroll
+                for (int j = 0; j < 4; j++) g.e[j] = dg[i][h + j], b.e[j] = db[i][h + j];
+                store_pack(out + at + h, a.width - at - h, g);
+                store_pack(out + a.width + at + h, a.width - at - h, b);
+            }
         } else {   // the teams' LANES V columns of this i, one team after the other
 #pragma unroll
             for (int which = 0; which < 2; which++) {

@@ -187,7 +187,6 @@ template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *strea
     if (vecs <= 256) return launch(k_loss_row<T, 4, 1, GRAD>, a.rows, 64, stream, a);
     if (vecs <= 1024) return launch(k_loss_row<T, 4, 4, GRAD>, a.rows, 256, stream, a);
     if (vecs <= 4096) return launch(k_loss_row<T, 8, 8, GRAD>, a.rows, 512, stream, a);
-    if (vecs <= 16384) return launch(k_loss_row<T, 16, 16, GRAD>, a.rows, 1024, stream, a);
     return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
 }
 

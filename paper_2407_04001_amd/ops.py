@@ -13,6 +13,7 @@ nothing waits for it.  A refused argument raises `PaseError`.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -68,62 +69,60 @@ def _check(rc: int):
         raise PaseError(rc, load().pase_operator_error().decode())
 
 
-class _On:
-    """The device of the tensors as the current one, and its current stream."""
-
-    __slots__ = ("stream", "guard")
-
-    def __init__(self, device):
-        self.guard = None
-        if device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        self.stream = torch.cuda.current_stream().cuda_stream
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _matrix(name, t, rows=None, cols=None, dtype=None, device=None):
-    """Checks a [rows, cols] argument and gives its row stride."""
+def _on_device(which):
+    """Runs an operator with the device of its argument number `which` as the
+    current one; the operator enqueues on that device's current stream."""
+    def wrap(fn):
+        @functools.wraps(fn)
+        def run(*args, **kw):
+            index = args[which].get_device()
+            if index < 0 or index == torch.cuda.current_device():   # a host tensor is refused by the checks
+                return fn(*args, **kw)
+            with torch.cuda.device(index):
+                return fn(*args, **kw)
+        return run
+    return wrap
+
+
+def _matrix(name, t, like=None, rows=None, cols=None):
+    """Checks a [rows, cols] argument, of the type and device of `like`, and gives its row stride."""
     if t.dim() != 2:
         _refuse(f"{name} has {t.dim()} dimensions, 2 are wanted")
-    shape = t.shape
-    if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
-        _refuse(f"{name} is {tuple(shape)}, ({rows}, {cols}) is wanted")
-    _device(name, t, dtype, device)
+    have_rows, have_cols = t.shape
+    if like is not None:
+        if have_rows != rows or have_cols != cols:
+            _refuse(f"{name} is {tuple(t.shape)}, ({rows}, {cols}) is wanted")
+        _same(name, t, like.dtype, like)
+    elif t.get_device() < 0:
+        _refuse(f"{name} is not on a GPU")
     ld, step = t.stride()
-    if shape[1] > 1 and step != 1:
+    if step != 1 and have_cols > 1:
         _refuse(f"the elements of a row of {name} are {step} apart, not adjacent")
-    if shape[0] > 1:
-        if ld < shape[1]:
+    if ld < have_cols:
+        if have_rows > 1:
             _refuse(f"the rows of {name} overlap")
-        return ld
-    return max(ld, shape[1])
+        return have_cols
+    return ld
 
 
-def _vector(name, t, n, dtype=None, device=None):
+def _same(name, t, dtype, like):
+    if dtype is not None and t.dtype is not dtype:
+        _refuse(f"{name} is {t.dtype}, {dtype} is wanted")
+    if t.get_device() != like.get_device():
+        _refuse(f"{name} is on {t.device}, not on {like.device}")
+
+
+def _vector(name, t, n, dtype, like):
     if t.dim() != 1 or t.shape[0] != n:
         _refuse(f"{name} is {tuple(t.shape)}, ({n},) is wanted")
-    _device(name, t, dtype, device)
+    _same(name, t, dtype, like)
     if n > 1 and t.stride(0) != 1:
         _refuse(f"{name} is not contiguous")
     return t.data_ptr()
-
-
-def _device(name, t, dtype, device):
-    if dtype is not None and t.dtype is not dtype:
-        _refuse(f"{name} is {t.dtype}, {dtype} is wanted")
-    if device is None:
-        if not t.is_cuda:
-            _refuse(f"{name} is not on a GPU")
-    elif t.device != device:
-        _refuse(f"{name} is on {t.device}, not on {device}")
 
 
 def _dtype(name, dtype):
@@ -133,79 +132,81 @@ def _dtype(name, dtype):
     return d
 
 
-def _index(name, t, n, device):
+def _index(name, t, n, like):
     """Checks a vector of n int32 or int64 and gives (pointer, is 64 bits)."""
-    if t.dtype is not torch.int64 and t.dtype is not torch.int32:
+    wide = t.dtype is torch.int64
+    if not wide and t.dtype is not torch.int32:
         _refuse(f"{name} is {t.dtype}: int32 or int64 is wanted")
-    return _vector(name, t, n, None, device), 1 if t.dtype is torch.int64 else 0
+    return _vector(name, t, n, None, like), 1 if wide else 0
 
 
-def _workspace(need: int, device):
-    if not need:
-        return None, 0
-    return torch.empty(need, dtype=torch.uint8, device=device), need
+def _workspace(size, like):
+    """A workspace of the bytes that `size`, a call with an output pointer last, reports: (tensor, pointer, bytes)."""
+    need = C.c_uint64()
+    _check(size(C.byref(need)))
+    if not need.value:
+        return None, None, 0
+    ws = like.new_empty(need.value, dtype=torch.uint8)
+    return ws, ws.data_ptr(), need.value
 
 
 # ------------------------------------------------------------------ layer norm
 def _params(gain, bias, width, x):
     if gain.dtype is not x.dtype and gain.dtype is not torch.float32:
         _refuse(f"gain is {gain.dtype}: {x.dtype} or torch.float32 is wanted")
-    g = _vector("gain", gain, width, None, x.device)
-    return g, _vector("bias", bias, width, gain.dtype, x.device) if bias is not None else None
+    g = _vector("gain", gain, width, None, x)
+    return g, _vector("bias", bias, width, gain.dtype, x) if bias is not None else None
 
 
+@_on_device(0)
 def layer_norm_forward(x, gain, bias=None, residual=None, eps: float = 1e-5):
     """(y, z, mean, rstd) of the rows of z = x + residual [rows, width]; without
     a residual z is x itself.  gain, bias: [width], in x's type or float32."""
     d = _dtype("x", x.dtype)
     ldx = _matrix("x", x)
     rows, width = x.shape
-    ldr = _matrix("residual", residual, rows, width, x.dtype, x.device) if residual is not None else 0
     g, b = _params(gain, bias, width, x)
-    with _On(x.device) as stream:
-        y = torch.empty(rows, width, dtype=x.dtype, device=x.device)
-        z = torch.empty_like(y) if residual is not None else x
-        stats = torch.empty(2, rows, dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
-        _check(load().pase_layer_norm_forward(
-            d, _DTYPES[gain.dtype], rows, width, x.data_ptr(), ldx,
-            residual.data_ptr() if residual is not None else None, ldr, g, b, eps, y.data_ptr(), width,
-            z.data_ptr() if residual is not None else None, width, mean.data_ptr(), rstd.data_ptr(), stream))
+    y = x.new_empty((rows, width))
+    mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind()
+    z, r, ldr, zp = x, None, 0, None
+    if residual is not None:
+        ldr, r = _matrix("residual", residual, x, rows, width), residual.data_ptr()
+        z = x.new_empty((rows, width))
+        zp = z.data_ptr()
+    _check(load().pase_layer_norm_forward(
+        d, _DTYPES[gain.dtype], rows, width, x.data_ptr(), ldx, r, ldr, g, b, eps, y.data_ptr(), width, zp, width,
+        mean.data_ptr(), rstd.data_ptr(), _raw_stream(x.get_device())))
     return y, z, mean, rstd
 
 
+@_on_device(0)
 def layer_norm_backward(dy, z, gain, mean, rstd, dz=None):
     """(dx, dgain, dbias): dx is the gradient of x and of the residual alike.
     dz: the gradient that reaches z other than through the norm."""
     d = _dtype("dy", dy.dtype)
     lddy = _matrix("dy", dy)
     rows, width = dy.shape
-    device = dy.device
-    ldz = _matrix("z", z, rows, width, dy.dtype, device)
-    lddz = _matrix("dz", dz, rows, width, dy.dtype, device) if dz is not None else 0
+    ldz = _matrix("z", z, dy, rows, width)
+    lddz = _matrix("dz", dz, dy, rows, width) if dz is not None else 0
     g, _ = _params(gain, None, width, dy)
-    m = _vector("mean", mean, rows, torch.float32, device)
-    r = _vector("rstd", rstd, rows, torch.float32, device)
+    m = _vector("mean", mean, rows, torch.float32, dy)
+    r = _vector("rstd", rstd, rows, torch.float32, dy)
     L = load()
-    with _On(device) as stream:
-        need = C.c_uint64()
-        _check(L.pase_layer_norm_workspace(d, rows, width, C.byref(need)))
-        ws, have = _workspace(need.value, device)
-        dx = torch.empty(rows, width, dtype=dy.dtype, device=device)
-        dparams = torch.empty(2, width, dtype=gain.dtype, device=device)
-        dgain, dbias = dparams[0], dparams[1]
-        _check(L.pase_layer_norm_backward(
-            d, _DTYPES[gain.dtype], rows, width, dy.data_ptr(), lddy, z.data_ptr(), ldz,
-            dz.data_ptr() if dz is not None else None, lddz, g, m, r, dx.data_ptr(), width, dgain.data_ptr(),
-            dbias.data_ptr(), ws.data_ptr() if ws is not None else None, have, stream))
+    ws, wp, have = _workspace(lambda out: L.pase_layer_norm_workspace(d, rows, width, out), dy)
+    dx = dy.new_empty((rows, width))
+    dgain, dbias = dy.new_empty((2, width), dtype=gain.dtype).unbind()
+    _check(L.pase_layer_norm_backward(
+        d, _DTYPES[gain.dtype], rows, width, dy.data_ptr(), lddy, z.data_ptr(), ldz,
+        dz.data_ptr() if dz is not None else None, lddz, g, m, r, dx.data_ptr(), width, dgain.data_ptr(),
+        dbias.data_ptr(), wp, have, _raw_stream(dy.get_device())))
     return dx, dgain, dbias
 
 
 # ------------------------------------------------------------------ grouped products
-def _groups(w, offsets, dtype, device):
+def _groups(w, like):
     if w.dim() != 3:
         _refuse(f"w has {w.dim()} dimensions, (groups, n, k) is wanted")
-    _device("w", w, dtype, device)
+    _same("w", w, like.dtype, like)
     if not w.is_contiguous():
         _refuse("w is not contiguous")
     return w.shape
@@ -218,6 +219,7 @@ def _out_dtype(name, want, dtype):
     return want
 
 
+@_on_device(0)
 def grouped_matmul_forward(x, w, offsets, out_dtype=None):
     """y[t] = w[e] x[t] for the rows t of each group e, offsets[e] .. offsets[e + 1] - 1.
 
@@ -226,46 +228,42 @@ def grouped_matmul_forward(x, w, offsets, out_dtype=None):
     x's type, or float32 on request."""
     d = _dtype("x", x.dtype)
     ldx = _matrix("x", x)
-    device = x.device
-    groups, n, k = _groups(w, offsets, x.dtype, device)
-    rows = x.shape[0]
-    if x.shape[1] != k:
-        _refuse(f"x has rows of {x.shape[1]}, w of {k}")
-    off, off64 = _index("offsets", offsets, groups + 1, device)
+    groups, n, k = _groups(w, x)
+    rows, width = x.shape
+    if width != k:
+        _refuse(f"x has rows of {width}, w of {k}")
+    off, off64 = _index("offsets", offsets, groups + 1, x)
     out = _out_dtype("out_dtype", out_dtype, x.dtype)
-    with _On(device) as stream:
-        y = torch.empty(rows, n, dtype=out, device=device)
-        _check(load().pase_grouped_matmul_forward(d, _DTYPES[out], rows, groups, n, k, x.data_ptr(), ldx,
-                                                  w.data_ptr(), off, off64, y.data_ptr(), n, stream))
+    y = x.new_empty((rows, n), dtype=out)
+    _check(load().pase_grouped_matmul_forward(d, _DTYPES[out], rows, groups, n, k, x.data_ptr(), ldx, w.data_ptr(), off,
+                                              off64, y.data_ptr(), n, _raw_stream(x.get_device())))
     return y
 
 
+@_on_device(0)
 def grouped_matmul_backward(dy, x, w, offsets, grad_dtype=None, need_dx: bool = True, need_dw: bool = True):
     """(dx, dw) of `grouped_matmul_forward`: dx in dy's type, dw [groups, n, k] in
     dy's type or float32 (grad_dtype).  One that is not needed is None."""
     d = _dtype("dy", dy.dtype)
     lddy = _matrix("dy", dy)
-    device = dy.device
-    groups, n, k = _groups(w, offsets, dy.dtype, device)
-    rows = dy.shape[0]
-    if dy.shape[1] != n:
-        _refuse(f"dy has rows of {dy.shape[1]}, w gives rows of {n}")
-    ldx = _matrix("x", x, rows, k, dy.dtype, device)
-    off, off64 = _index("offsets", offsets, groups + 1, device)
+    groups, n, k = _groups(w, dy)
+    rows, width = dy.shape
+    if width != n:
+        _refuse(f"dy has rows of {width}, w gives rows of {n}")
+    ldx = _matrix("x", x, dy, rows, k)
+    off, off64 = _index("offsets", offsets, groups + 1, dy)
     grad = _out_dtype("grad_dtype", grad_dtype, dy.dtype)
     L = load()
-    with _On(device) as stream:
-        dx = torch.empty(rows, k, dtype=dy.dtype, device=device) if need_dx else None
-        dw = ws = None
-        need = C.c_uint64()
-        if need_dw:
-            dw = torch.empty(groups, n, k, dtype=grad, device=device)
-            _check(L.pase_grouped_matmul_workspace(d, _DTYPES[grad], rows, groups, n, k, C.byref(need)))
-            ws, _ = _workspace(need.value, device)
-        _check(L.pase_grouped_matmul_backward(
-            d, _DTYPES[grad], rows, groups, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), off, off64,
-            dx.data_ptr() if need_dx else None, k, dw.data_ptr() if need_dw else None,
-            ws.data_ptr() if ws is not None else None, need.value, stream))
+    dx = dy.new_empty((rows, k)) if need_dx else None
+    dw, ws, wp, have = None, None, None, 0
+    if need_dw:
+        dw = dy.new_empty((groups, n, k), dtype=grad)
+        ws, wp, have = _workspace(
+            lambda out: L.pase_grouped_matmul_workspace(d, _DTYPES[grad], rows, groups, n, k, out), dy)
+    _check(L.pase_grouped_matmul_backward(
+        d, _DTYPES[grad], rows, groups, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), off, off64,
+        dx.data_ptr() if need_dx else None, k, dw.data_ptr() if need_dw else None, wp, have,
+        _raw_stream(dy.get_device())))
     return dx, dw
 
 
@@ -274,13 +272,13 @@ def _loss_args(logits, targets):
     d = _dtype("logits", logits.dtype)
     ldl = _matrix("logits", logits)
     rows, classes = logits.shape
-    t, t64 = _index("targets", targets, rows, logits.device)
+    t, t64 = _index("targets", targets, rows, logits)
     return d, ldl, rows, classes, t, t64
 
 
-def _row_gradient(dloss, rows, device):
+def _row_gradient(dloss, rows, like):
     """Pointer and stride of dloss: one a row, or one for all (a 0-d tensor, or expanded)."""
-    _device("dloss", dloss, torch.float32, device)
+    _same("dloss", dloss, torch.float32, like)
     if dloss.dim() == 0:
         return dloss.data_ptr(), 0
     if dloss.dim() != 1 or dloss.shape[0] != rows:
@@ -291,58 +289,51 @@ def _row_gradient(dloss, rows, device):
     return dloss.data_ptr(), step if rows > 1 else 0
 
 
-def _loss(logits, targets, ignore_index, dloss, out):
-    d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
-    device = logits.device
-    L = load()
-    with _On(device) as stream:
-        need = C.c_uint64()
-        _check(L.pase_softmax_loss_workspace(d, rows, classes, C.byref(need)))
-        ws, have = _workspace(need.value, device)
-        wp = ws.data_ptr() if ws is not None else None
-        both = torch.empty(2, rows, dtype=torch.float32, device=device)
-        loss, lse = both[0], both[1]
-        if dloss is None:
-            _check(L.pase_softmax_loss_forward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index,
-                                               loss.data_ptr(), lse.data_ptr(), wp, have, stream))
-            return loss, lse
-        g, step = _row_gradient(dloss, rows, device)
-        dlogits, lddl = _gradient_out(logits, out)
-        _check(L.pase_softmax_loss_grad(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, g, step,
-                                        loss.data_ptr(), lse.data_ptr(), dlogits.data_ptr(), lddl, wp, have, stream))
-        return loss, lse, dlogits
-
-
 def _gradient_out(logits, out):
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        return out, logits.shape[1]
-    return out, _matrix("out", out, *logits.shape, logits.dtype, logits.device)
+        return logits.new_empty(logits.shape), logits.shape[1]
+    return out, _matrix("out", out, logits, *logits.shape)
 
 
+@_on_device(0)
 def softmax_loss_forward(logits, targets, ignore_index: int = -100):
     """(loss, lse) per row of logits [rows, classes], float32.  targets: [rows],
     int32 or int64; a row whose target is ignore_index has loss 0."""
-    return _loss(logits, targets, ignore_index, None, None)
+    d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
+    L = load()
+    ws, wp, have = _workspace(lambda out: L.pase_softmax_loss_workspace(d, rows, classes, out), logits)
+    loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
+    _check(L.pase_softmax_loss_forward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, loss.data_ptr(),
+                                       lse.data_ptr(), wp, have, _raw_stream(logits.get_device())))
+    return loss, lse
 
 
+@_on_device(0)
 def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None):
     """(loss, lse, dlogits) in one pass over the logits, for a gradient of the
     rows' losses that is known beforehand (dloss: float32 [rows], or one value
     for all), as where the loss is their mean.  out may be logits."""
-    return _loss(logits, targets, ignore_index, dloss, out)
+    d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
+    g, step = _row_gradient(dloss, rows, logits)
+    L = load()
+    ws, wp, have = _workspace(lambda out: L.pase_softmax_loss_workspace(d, rows, classes, out), logits)
+    loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
+    dlogits, lddl = _gradient_out(logits, out)
+    _check(L.pase_softmax_loss_grad(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, g, step,
+                                    loss.data_ptr(), lse.data_ptr(), dlogits.data_ptr(), lddl, wp, have,
+                                    _raw_stream(logits.get_device())))
+    return loss, lse, dlogits
 
 
+@_on_device(1)
 def softmax_loss_backward(dloss, logits, targets, lse, ignore_index: int = -100, out=None):
     """dlogits from the lse of `softmax_loss_forward`.  out may be logits."""
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
-    device = logits.device
-    g, step = _row_gradient(dloss, rows, device)
-    s = _vector("lse", lse, rows, torch.float32, device)
-    with _On(device) as stream:
-        dlogits, lddl = _gradient_out(logits, out)
-        _check(load().pase_softmax_loss_backward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, s, g,
-                                                 step, dlogits.data_ptr(), lddl, stream))
+    g, step = _row_gradient(dloss, rows, logits)
+    s = _vector("lse", lse, rows, torch.float32, logits)
+    dlogits, lddl = _gradient_out(logits, out)
+    _check(load().pase_softmax_loss_backward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, s, g, step,
+                                             dlogits.data_ptr(), lddl, _raw_stream(logits.get_device())))
     return dlogits
 
 
