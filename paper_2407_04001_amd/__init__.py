@@ -2,6 +2,8 @@
 
 The search runs in ``libpase.so`` (host planner in C++, DP-table fill in HIP
 kernels for gfx950); this package only loads it and marshals arguments.
+``ops`` runs a graph's layers as operators on device tensors, ``measure`` makes
+layer costs of their times; both need torch.
 """
 from .pase import (EXPORTS, LIB_PATH, OPT_BULK_US, OPT_C_SPLITS, OPT_CONFIG_SET,  # noqa: F401
                    OPT_DIRECT_CELLS, OPT_FUSED_MIN, OPT_GRAD_SYNC, OPT_HALO, OPT_KEEP_TABLES, OPT_KERNEL,
