@@ -282,12 +282,13 @@ __device__ __forceinline__ typename Mfma<T>::Frag frag(const Pack<T> *lds, int f
     return u.f;
 }
 
-// A lane's columns of one row of c: 8 from p on and 8 from p + 32 on, of the n that exist.
-template <typename O> __device__ __forceinline__ void store_row(O *p, int n, const f32x4 (&v)[4]) {
+// A lane's columns of one row of c, of the n that exist from p on: 8 and, 32 on, 8
+// (PAIRED fragments), or four times 4, 16 apart.
+template <bool PAIRED, typename O> __device__ __forceinline__ void store_row(O *p, int n, const f32x4 (&v)[4]) {
     constexpr int V = kVec<O>;
 #pragma unroll
     for (int s = 0; s < 16; s += V) {
-        const int at = (s & 7) + (s >> 3) * 32;
+        const int at = PAIRED ? (s & 7) + (s >> 3) * 32 : s * 4;
         Pack<O> o;
 #pragma unroll
         for (int j = 0; j < V; j++) o.e[j] = (O)v[(s + j) >> 2][(s + j) & 3];
@@ -348,7 +349,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
 #pragma unroll
     for (int m = 0; m < 4; m++) {
         const int row = wm + m * 16 + (lane & 15), col = wj + (lane >> 4) * 8;
-        if (row < m_rows && col < j_rows) store_row(c + row * a.ldo + col, (int)(j_rows - col), acc[m]);
+        if (row < m_rows && col < j_rows) store_row<true>(c + row * a.ldo + col, (int)(j_rows - col), acc[m]);
     }
 }
 
@@ -485,6 +486,9 @@ template <typename F> __device__ __forceinline__ void mask_frag(F &f, int left) 
 template <typename T, typename O, Direction D> __global__ __launch_bounds__(512) void k_product_big(GroupedProduct a) {
     constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
     constexpr int kStores = 8 * 16 / kVec<O>;   // of a wave that stores a whole tile
+    // A lane's 16 bytes of c are one fragment's 4 columns in fp32 and two fragments' 8
+    // in 16 bits: the j side's rows are in order in the first case, paired in the second.
+    constexpr bool PAIRED = sizeof(O) == 2;
     typedef typename Mfma<T>::Frag Frag;
     __shared__ __attribute__((aligned(1024))) char lds[2][kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -497,7 +501,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
     Frag f[3][4], g[2][4];
     f32x4 acc[8][4];
     const Reader<T, A_ACROSS, false> ra(wm);
-    const Reader<T, B_ACROSS, true> rb(wj);
+    const Reader<T, B_ACROSS, PAIRED> rb(wj);
     const uint32_t stage0 = lds_address(lds[0]);
     // four products, and what is issued behind them
     const auto multiply = [&](const Frag &fm, const Frag(&gj)[4], int m) {
@@ -520,7 +524,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         p.template rows<D, kBig, kBig>(a, t);
     }
     Feed<T, A_ACROSS, false> fa(p.lda);
-    Feed<T, B_ACROSS, true> fb(p.ldb);
+    Feed<T, B_ACROSS, PAIRED> fb(p.ldb);
     // the first two steps of a tile; the second may be past its end
     const auto feed = [&]() {
         if (p.depth <= 0) return;
@@ -630,15 +634,15 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
             feed();
         }
         stored = m_rows >= kBig && j_rows >= kBig;
-        c += (wm + (lane & 15)) * a.ldo + wj + (lane >> 4) * 8;
+        const int row = wm + (lane & 15), col = wj + (lane >> 4) * kVec<O>;
+        c += row * a.ldo + col;
         if (stored) {
 #pragma unroll
-            for (int m = 0; m < 8; m++) store_row(c + m * 16 * a.ldo, 64, acc[m]);
+            for (int m = 0; m < 8; m++) store_row<PAIRED>(c + m * 16 * a.ldo, 64, acc[m]);
         } else {
-            const int row = wm + (lane & 15), col = wj + (lane >> 4) * 8;
 #pragma unroll
             for (int m = 0; m < 8; m++)
-                if (row + m * 16 < m_rows && col < j_rows) store_row(c + m * 16 * a.ldo, j_rows - col, acc[m]);
+                if (row + m * 16 < m_rows && col < j_rows) store_row<PAIRED>(c + m * 16 * a.ldo, j_rows - col, acc[m]);
         }
         if (after.none) return;
     }
@@ -793,7 +797,7 @@ template <typename T, int MT> __global__ __launch_bounds__(256) void k_rows_grad
 #pragma unroll
             for (int o = 0; o < 3; o++) acc[m][j] += join[(o * MT * JT + m * JT + j) * 64 + lane];
         const int r = m * 16 + l;
-        if (r < p.m_rows) store_row(p.c + r * a.ldo + q * 8, p.j_rows - q * 8, acc[m]);
+        if (r < p.m_rows) store_row<true>(p.c + r * a.ldo + q * 8, p.j_rows - q * 8, acc[m]);
     }
 }
 

@@ -140,14 +140,21 @@ def _index(name, t, n, like):
     return _vector(name, t, n, None, like), 1 if wide else 0
 
 
-def _workspace(size, like):
-    """A workspace of the bytes that `size`, a call with an output pointer last, reports: (tensor, pointer, bytes)."""
+@functools.lru_cache(maxsize=4096)
+def _bytes(name, *sizes):
+    """Workspace that the library asks for at these types and sizes."""
     need = C.c_uint64()
-    _check(size(C.byref(need)))
-    if not need.value:
+    _check(getattr(load(), name)(*sizes, C.byref(need)))
+    return need.value
+
+
+def _workspace(like, name, *sizes):
+    """A workspace for one call: (tensor, pointer, bytes)."""
+    need = _bytes(name, *sizes)
+    if not need:
         return None, None, 0
-    ws = like.new_empty(need.value, dtype=torch.uint8)
-    return ws, ws.data_ptr(), need.value
+    ws = like.new_empty(need, dtype=torch.uint8)
+    return ws, ws.data_ptr(), need
 
 
 # ------------------------------------------------------------------ layer norm
@@ -192,7 +199,7 @@ def layer_norm_backward(dy, z, gain, mean, rstd, dz=None):
     m = _vector("mean", mean, rows, torch.float32, dy)
     r = _vector("rstd", rstd, rows, torch.float32, dy)
     L = load()
-    ws, wp, have = _workspace(lambda out: L.pase_layer_norm_workspace(d, rows, width, out), dy)
+    ws, wp, have = _workspace(dy, "pase_layer_norm_workspace", d, rows, width)
     dx = dy.new_empty((rows, width))
     dgain, dbias = dy.new_empty((2, width), dtype=gain.dtype).unbind()
     _check(L.pase_layer_norm_backward(
@@ -258,8 +265,7 @@ def grouped_matmul_backward(dy, x, w, offsets, grad_dtype=None, need_dx: bool = 
     dw, ws, wp, have = None, None, None, 0
     if need_dw:
         dw = dy.new_empty((groups, n, k), dtype=grad)
-        ws, wp, have = _workspace(
-            lambda out: L.pase_grouped_matmul_workspace(d, _DTYPES[grad], rows, groups, n, k, out), dy)
+        ws, wp, have = _workspace(dy, "pase_grouped_matmul_workspace", d, _DTYPES[grad], rows, groups, n, k)
     _check(L.pase_grouped_matmul_backward(
         d, _DTYPES[grad], rows, groups, n, k, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), off, off64,
         dx.data_ptr() if need_dx else None, k, dw.data_ptr() if need_dw else None, wp, have,
@@ -301,7 +307,7 @@ def softmax_loss_forward(logits, targets, ignore_index: int = -100):
     int32 or int64; a row whose target is ignore_index has loss 0."""
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
     L = load()
-    ws, wp, have = _workspace(lambda out: L.pase_softmax_loss_workspace(d, rows, classes, out), logits)
+    ws, wp, have = _workspace(logits, "pase_softmax_loss_workspace", d, rows, classes)
     loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
     _check(L.pase_softmax_loss_forward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, loss.data_ptr(),
                                        lse.data_ptr(), wp, have, _raw_stream(logits.get_device())))
@@ -316,7 +322,7 @@ def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
     g, step = _row_gradient(dloss, rows, logits)
     L = load()
-    ws, wp, have = _workspace(lambda out: L.pase_softmax_loss_workspace(d, rows, classes, out), logits)
+    ws, wp, have = _workspace(logits, "pase_softmax_loss_workspace", d, rows, classes)
     loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
     dlogits, lddl = _gradient_out(logits, out)
     _check(L.pase_softmax_loss_grad(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, g, step,
