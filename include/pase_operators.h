@@ -107,11 +107,7 @@ pase_status pase_grouped_matmul_backward(int dtype, int grad_dtype, uint64_t row
  * 0..classes-1 that is not ignore_index gives loss NaN. */
 pase_status pase_softmax_loss_forward(int dtype, uint64_t rows, uint64_t classes, const void *logits,
                                       uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
-                                      float *loss, float *lse, void *workspace, uint64_t workspace_bytes,
-                                      void *stream);
-
-/* Bytes of workspace the two calls around it need (0 is possible). */
-pase_status pase_softmax_loss_workspace(int dtype, uint64_t rows, uint64_t classes, uint64_t *bytes);
+                                      float *loss, float *lse, void *stream);
 
 /* Loss and gradient in one pass over the logits, for a loss gradient that is
  * known beforehand: dlogits[j] = (exp(logits[j] - lse) - [j = target]) * dloss.
@@ -121,8 +117,7 @@ pase_status pase_softmax_loss_workspace(int dtype, uint64_t rows, uint64_t class
 pase_status pase_softmax_loss_grad(int dtype, uint64_t rows, uint64_t classes, const void *logits,
                                    uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
                                    const float *dloss, uint64_t dloss_stride, float *loss, float *lse,
-                                   void *dlogits, uint64_t lddl, void *workspace, uint64_t workspace_bytes,
-                                   void *stream);
+                                   void *dlogits, uint64_t lddl, void *stream);
 
 /* The gradient alone, from the lse of pase_softmax_loss_forward; same rules. */
 pase_status pase_softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, const void *logits,

@@ -226,8 +226,9 @@ template <typename T, typename O> struct Part {
 };
 
 // ---------------------------------------------------------------- any alignment
-// 128 x 128 tiles, 64 of i at a time; four waves, 64 x 64 each.  Operands go
-// through registers, where what lies past an edge becomes 0.
+// Where a row may begin at an odd element.  128 x 128 tiles, 64 of i at a time; four waves, 64 x 64 each.  Operands go
+// through registers, where what lies past an edge becomes 0.  Bound by the latency of
+// those loads, one step ahead: 16384 x 4096 x 1024 in 8 groups 427 us (322 TFLOP/s).
 constexpr int kTile = 128, kDepth = 64;
 
 template <typename T, bool ACROSS>
@@ -359,6 +360,15 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256)
 // lane): the buffer's range ends at the operand's last element, so what a tile
 // overhangs reads as 0.  Only what lies past i = depth in a row along i is
 // inside that range; the fragments of the last step are masked there.
+// 16384 x 4096 x 4096 in bf16 402-412 us (1.34 PFLOP/s; the library's own 1.3-1.68 on
+// like shapes): the matrix units are busy for 60 % of the cycles at the 1.96 GHz the
+// card holds.  Without its loads the loop takes 360 us, without its LDS reads 377,
+// without both 303: it is bound by neither alone.  Tried and slower: 128 x 256 tiles,
+// two workgroups a CU (522); stages of 32 i, four deep (455-482); two groups of waves
+// a barrier apart, one reading while the other multiplies (446).
+// 16384 x 1024 -> 4096 in 8 even groups 122 us (1.12 PFLOP/s), in ragged ones 142-163:
+// the last round of tiles is then nearly empty, and bound by latency (halving its
+// tiles changed nothing).
 constexpr int kStage = 2 * kBig * 8 * 16;   // bytes of one step's two operands in LDS
 
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
@@ -369,7 +379,7 @@ __device__ __forceinline__ uint32_t lds_address(const void *p) {
 // the same for the wave, through M0, which nothing else here uses).  The load has no register result; whoever reads the
 // LDS bytes waits for it by wait_loads().  The builtin of the same instruction
 // makes the compiler wait for every such load before each transposing LDS read,
-// a step too early: 16384 x 4096 x 4096 rows gradient 510 us with it, XXX without.
+// a step too early: 16384 x 4096 x 4096 rows gradient 510 us with it, 436 without.
 __device__ __forceinline__ void load_to_lds(u32x4 r, int at, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(r) : "memory");
 }
@@ -652,7 +662,8 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
 // Forward with few rows a group: what counts is reading each weight once.  A
 // workgroup takes 16 MT rows and 32 columns; its four waves take every fourth 32 of
 // the contraction, straight from HBM to the matrix unit (a lane's 16 bytes are its
-// part of a fragment), and add up through LDS.
+// part of a fragment), and add up through LDS.  Bound by HBM and latency: 64 rows in 8
+// groups of 1024 x 4096 (67 MB) 16-18 us, 3.7-4.2 TB/s.
 template <typename T, typename O, int MT> __global__ __launch_bounds__(256) void k_product_thin(GroupedProduct a) {
     typedef typename Mfma<T>::Frag Frag;
     union Piece {
@@ -723,7 +734,8 @@ template <typename T, typename O, int MT> __global__ __launch_bounds__(256) void
 
 // The rows' gradient with few rows a group: as above with 64 columns a workgroup, but
 // w's rows run across, so each wave passes its 32 x 64 of w through LDS of its own
-// (no barriers) for the transposing reads.  The next 32 are loaded meanwhile.
+// (no barriers) for the transposing reads.  The next 32 are loaded meanwhile.  The
+// same 64 rows: 27 us (32 turns of a load's latency), 16 us with n and k exchanged.
 template <typename T, int MT> __global__ __launch_bounds__(256) void k_rows_grad_thin(GroupedProduct a) {
     typedef typename Mfma<T>::Frag Frag;
     union Piece {

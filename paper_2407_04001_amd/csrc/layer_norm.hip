@@ -5,7 +5,9 @@
 // deviations and the output each need all of it.  The variance is summed over
 // (z - mean)^2, not z^2 - mean^2, whose difference loses digits where the mean
 // is large.  Both passes are bound by HBM: they read and write each operand
-// once.
+// once.  16384 x 1024 in bf16 with a residual: forward 26 us for 134 MB (5.1 TB/s),
+// backward 36 us (3.7 TB/s; the sums of dgain and dbias, 2 x 4 MB and a second launch,
+// are 5 us of it).  200000 x 64: 16 and 24 us; a wave a row there took 77 and 172.
 #include "operators.h"
 #include "vectors.h"
 
@@ -110,7 +112,9 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_norm_forward(NormForward a) {
 
 // dx row by row, a team taking every (teams in the grid)-th row; its lanes keep
 // the sums of dy * h and dy over those rows for their own columns, which the
-// workgroup adds up and leaves as one row of `partial`.
+// workgroup adds up and leaves as one row of `partial`.  512 workgroups: 16384 x 1024
+// 30.4 us (operands in cache), with 256 of them 40.5, with 1024 35.2 (more sums to
+// write and read).
 template <typename T, typename P, int NV, int LANES>
 __global__ __launch_bounds__(kBlock<LANES>) void k_norm_backward(NormBackward a) {
     constexpr int V = kVec<T>, kTeam = LANES, TEAMS = kTeams<LANES>, WAVES = LANES > 64 ? LANES / 64 : 1;

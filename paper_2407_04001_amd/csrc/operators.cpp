@@ -110,11 +110,6 @@ uint64_t norm_bytes(int dtype, uint64_t rows, uint64_t width) {
     return (uint64_t)norm_backward_blocks(dtype, (int64_t)rows, (int)width) * 2 * width * sizeof(float);
 }
 
-uint64_t loss_bytes(int dtype, uint64_t rows, uint64_t classes) {
-    const int splits = softmax_loss_splits(dtype, (int64_t)rows, (int64_t)classes);
-    return splits > 1 ? rows * (uint64_t)splits * 2 * sizeof(float) : 0;
-}
-
 uint64_t product_bytes(uint64_t rows, uint32_t groups, uint64_t n, uint64_t k) {
     const int splits = grouped_matmul_splits((int64_t)rows, (int)groups, (int)n, (int)k);
     return splits > 1 ? (uint64_t)splits * groups * n * k * sizeof(float) : 0;
@@ -129,7 +124,7 @@ uint64_t product_bytes(uint64_t rows, uint32_t groups, uint64_t n, uint64_t k) {
 pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
                          const void *targets, int targets_64, int64_t ignore_index, const float *dloss,
                          uint64_t dloss_stride, float *loss, float *lse, void *dlogits, uint64_t lddl,
-                         void *workspace, uint64_t workspace_bytes, bool grad, void *stream) {
+                         bool grad, void *stream) {
     CHECK(check_loss(dtype, rows, classes, targets, targets_64));
     if (!rows) return PASE_OK;
     REQUIRE_MATRIX(logits, ldl, classes, dtype);
@@ -141,7 +136,6 @@ pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void 
         REQUIRE(dloss_stride <= 1, "dloss_stride is neither 0 nor 1");
         REQUIRE(dlogits != logits || ldl == lddl, "dlogits is logits with another row stride");
     }
-    CHECK(check_workspace(workspace, workspace_bytes, loss_bytes(dtype, rows, classes)));
     SoftmaxLoss a{};
     a.dtype = dtype, a.targets_64 = targets_64;
     a.rows = (int64_t)rows, a.classes = (int64_t)classes;
@@ -150,8 +144,6 @@ pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void 
     a.dloss = dloss, a.dloss_stride = (int64_t)dloss_stride;
     a.loss = loss, a.lse = lse;
     a.dlogits = grad ? dlogits : nullptr, a.lddl = (int64_t)lddl;
-    a.partial = static_cast<float *>(workspace);
-    a.splits = softmax_loss_splits(dtype, a.rows, a.classes);
     return launched(launch_softmax_loss(a, stream));
 }
 
@@ -162,8 +154,6 @@ int norm_backward_blocks(int dtype, int64_t rows, int width) {
     const int64_t teams = lanes < 256 ? 256 / lanes : 1, want = (rows + teams - 1) / teams;
     return (int)(want < 512 ? want : 512);
 }
-
-int softmax_loss_splits(int, int64_t, int64_t) { return 1; }
 
 // A part a CU, while parts of an average group keep 512 rows: with fewer tiles than
 // CUs the rest would be idle, and a part's sums are written and read once more.
@@ -321,27 +311,19 @@ pase_status pase_grouped_matmul_backward(int dtype, int grad_dtype, uint64_t row
     return PASE_OK;
 }
 
-pase_status pase_softmax_loss_workspace(int dtype, uint64_t rows, uint64_t classes, uint64_t *bytes) {
-    REQUIRE(bytes, "bytes is null");
-    CHECK(check_loss(dtype, 0, classes, nullptr, 0));
-    if (rows > (1ull << 31) - 1) return refuse(PASE_ERR_TOO_LARGE, "too many rows");
-    *bytes = loss_bytes(dtype, rows, classes);
-    return PASE_OK;
-}
-
 pase_status pase_softmax_loss_forward(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
                                       const void *targets, int targets_64, int64_t ignore_index, float *loss,
-                                      float *lse, void *workspace, uint64_t workspace_bytes, void *stream) {
+                                      float *lse, void *stream) {
     return softmax_loss(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, nullptr, 0, loss, lse,
-                        nullptr, 0, workspace, workspace_bytes, false, stream);
+                        nullptr, 0, false, stream);
 }
 
 pase_status pase_softmax_loss_grad(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
                                    const void *targets, int targets_64, int64_t ignore_index, const float *dloss,
                                    uint64_t dloss_stride, float *loss, float *lse, void *dlogits, uint64_t lddl,
-                                   void *workspace, uint64_t workspace_bytes, void *stream) {
+                                   void *stream) {
     return softmax_loss(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, dloss, dloss_stride,
-                        loss, lse, dlogits, lddl, workspace, workspace_bytes, true, stream);
+                        loss, lse, dlogits, lddl, true, stream);
 }
 
 pase_status pase_softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
@@ -367,7 +349,6 @@ pase_status pase_softmax_loss_backward(int dtype, uint64_t rows, uint64_t classe
     a.dloss = dloss, a.dloss_stride = (int64_t)dloss_stride;
     a.lse = const_cast<float *>(lse);
     a.dlogits = dlogits, a.lddl = (int64_t)lddl;
-    a.splits = 1;
     return launched(launch_softmax_loss_backward(a, stream));
 }
 

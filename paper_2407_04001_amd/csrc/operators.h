@@ -41,8 +41,6 @@ struct SoftmaxLoss {
     float *loss, *lse;
     void *dlogits;
     int64_t lddl;
-    float *partial;      // [rows][splits][2]: the chunks' maxima and sums
-    int splits;          // workgroups sharing a row (1: a row is one workgroup's)
 };
 
 // c[m][j] = sum over the contraction of a and b; see grouped_matmul.hip for
@@ -54,7 +52,7 @@ struct GroupedProduct {
     const void *x, *w, *dy, *offsets;
     void *out;
     int64_t ldx, lddy, ldo;
-    float *partial;      // weight gradient: [splits][groups][n][k] when splits > 1
+    float *partial;      // weights gradient: [splits][groups][n][k] when splits > 1
     int splits;
 };
 
@@ -65,8 +63,6 @@ inline int norm_lanes(int vecs) {
 }
 // blocks of the layer norm's backward pass (one row of partial sums each)
 int norm_backward_blocks(int dtype, int64_t rows, int width);
-// workgroups that share a row of the softmax loss
-int softmax_loss_splits(int dtype, int64_t rows, int64_t classes);
 // parts each group's rows are cut into by the weights' gradient
 int grouped_matmul_splits(int64_t rows, int groups, int n, int k);
 

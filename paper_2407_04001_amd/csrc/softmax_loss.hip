@@ -71,7 +71,10 @@ template <typename T> __device__ __forceinline__ void zero_row(T *out, int64_t c
         store_pack(out + at, classes - at, zero);
 }
 
-// One row a workgroup of WAVES waves, NV vectors a lane.
+// One row a workgroup of WAVES waves, NV vectors a lane.  Bound by HBM: 16384 x 32768 in
+// bf16, loss and gradient, 380 us for 2.15 GB (5.7 TB/s).  Sixteen waves with sixteen
+// vectors a lane (rows of 131072 in bf16) would leave one workgroup on a CU, which loads,
+// sums and stores by turns: 1608 us against 501 for k_loss_long.
 template <typename T, int NV, int WAVES, bool GRAD>
 __global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
     constexpr int V = kVec<T>, THREADS = WAVES * 64;
@@ -118,7 +121,12 @@ __global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
     }
 }
 
-// A row longer than the registers of a workgroup hold.
+// A longer row: read by kAhead vectors a lane in flight, and for the gradient again,
+// one by one (that pass also writes; with 8 in flight 1280 x 65536 in fp32 took 210 us
+// against 161).  4096 x 131072 in bf16: loss 188 us (1.07 GB, 5.7 TB/s), loss and
+// gradient 501 us; 1 x 131072 loss 9 us.
+constexpr int kAhead = 8;
+
 template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_long(SoftmaxLoss a) {
     constexpr int V = kVec<T>, WAVES = 16, THREADS = 1024;
     __shared__ float lds[2 * WAVES];
@@ -131,18 +139,26 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_
         if (GRAD) zero_row(out, a.classes, THREADS);
         return;
     }
+    const int64_t first = (int64_t)threadIdx.x * V, stride = (int64_t)THREADS * V;
     float top = -__builtin_inff(), from = 0.0f, sum = 0.0f;
-    for (int64_t at = (int64_t)threadIdx.x * V; at < a.classes; at += (int64_t)THREADS * V) {
-        const Pack<T> l = load_pack(logits + at, a.classes - at, masked<T>());
+    for (int64_t at = first; at < a.classes; at += kAhead * stride) {
+        Pack<T> l[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; i++)
+            l[i] = load_pack(logits + at + i * stride, a.classes - at - i * stride, masked<T>());
         float t = top;
 #pragma unroll
-        for (int j = 0; j < V; j++) t = fmaxf(t, (float)l.e[j]);
+        for (int i = 0; i < kAhead; i++)
+#pragma unroll
+            for (int j = 0; j < V; j++) t = fmaxf(t, (float)l[i].e[j]);
         if (t > top) {
             sum *= __expf(top - t);   // top is -inf only while the sum is 0 or NaN
             top = from = t;
         }
 #pragma unroll
-        for (int j = 0; j < V; j++) sum += __expf((float)l.e[j] - from);
+        for (int i = 0; i < kAhead; i++)
+#pragma unroll
+            for (int j = 0; j < V; j++) sum += __expf((float)l[i].e[j] - from);
     }
     const float all = group_max<WAVES>(top, lds);
     float s[1] = {top == -__builtin_inff() ? sum : sum * __expf(top - all)};
@@ -152,10 +168,8 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_
     if (GRAD) {
         __syncthreads();
         const RowGrad g = row_grad(a, row, target, lse);
-        for (int64_t at = (int64_t)threadIdx.x * V; at < a.classes; at += (int64_t)THREADS * V) {
-            const Pack<T> l = load_pack(logits + at, a.classes - at, masked<T>());
-            grad_pack(out, at, a.classes - at, l, g.lse, target, g.scale);
-        }
+        for (int64_t at = first; at < a.classes; at += stride)
+            grad_pack(out, at, a.classes - at, load_pack(logits + at, a.classes - at, masked<T>()), g.lse, target, g.scale);
     }
 }
 
@@ -182,21 +196,25 @@ template <typename T> __global__ __launch_bounds__(256) void k_loss_grad(Softmax
     }
 }
 
+template <typename T> int grad_typed(const SoftmaxLoss &a, void *stream) {
+    const int chunks = (int)((a.classes + kGradVecs * kVec<T> - 1) / (kGradVecs * kVec<T>));
+    return launch(k_loss_grad<T>, a.rows * chunks, 256, stream, a, chunks);
+}
+
 template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *stream) {
     const int64_t vecs = (a.classes + kVec<T> - 1) / kVec<T>;
     if (vecs <= 256) return launch(k_loss_row<T, 4, 1, GRAD>, a.rows, 64, stream, a);
     if (vecs <= 1024) return launch(k_loss_row<T, 4, 4, GRAD>, a.rows, 256, stream, a);
     if (vecs <= 4096) return launch(k_loss_row<T, 8, 8, GRAD>, a.rows, 512, stream, a);
-    return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
+    if (!GRAD || a.rows >= 2 * kCus) return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
+    // fewer rows than fill the chip: the gradient from the lse, by workgroups that share rows
+    // (1 x 131072 in fp32: 28 us in one kernel, 13 in two)
+    if (const int e = launch(k_loss_long<T, false>, a.rows, 1024, stream, a)) return e;
+    return grad_typed<T>(a, stream);
 }
 
 template <typename T> int loss_typed(const SoftmaxLoss &a, void *stream) {
     return a.dlogits ? loss_rows<T, true>(a, stream) : loss_rows<T, false>(a, stream);
-}
-
-template <typename T> int grad_typed(const SoftmaxLoss &a, void *stream) {
-    const int chunks = (int)((a.classes + kGradVecs * kVec<T> - 1) / (kGradVecs * kVec<T>));
-    return launch(k_loss_grad<T>, a.rows * chunks, 256, stream, a, chunks);
 }
 
 }  // namespace

@@ -46,9 +46,6 @@ template <typename T> __device__ __forceinline__ void store_pack(T *p, int64_t n
     }
 }
 
-template <int N> struct Sums {
-    float v[N];
-};
 
 template <int N> __device__ __forceinline__ void wave_sum(float (&v)[N]) {
 #pragma unroll

@@ -27,7 +27,7 @@ MAX_GROUPS = 65536
 
 EXPORTS = ["pase_operator_error", "pase_layer_norm_forward", "pase_layer_norm_workspace",
            "pase_layer_norm_backward", "pase_grouped_matmul_forward", "pase_grouped_matmul_workspace",
-           "pase_grouped_matmul_backward", "pase_softmax_loss_workspace", "pase_softmax_loss_forward",
+           "pase_grouped_matmul_backward", "pase_softmax_loss_forward",
            "pase_softmax_loss_grad", "pase_softmax_loss_backward"]
 
 _lib = None
@@ -47,9 +47,8 @@ def load():
         "pase_grouped_matmul_forward": [I, I, U64, U32, U64, U64, P, U64, P, P, I, P, U64, P],
         "pase_grouped_matmul_workspace": [I, I, U64, U32, U64, U64, P],
         "pase_grouped_matmul_backward": [I, I, U64, U32, U64, U64, P, U64, P, U64, P, P, I, P, U64, P, P, U64, P],
-        "pase_softmax_loss_workspace": [I, U64, U64, P],
-        "pase_softmax_loss_forward": [I, U64, U64, P, U64, P, I, I64, P, P, P, U64, P],
-        "pase_softmax_loss_grad": [I, U64, U64, P, U64, P, I, I64, P, U64, P, P, P, U64, P, U64, P],
+        "pase_softmax_loss_forward": [I, U64, U64, P, U64, P, I, I64, P, P, P],
+        "pase_softmax_loss_grad": [I, U64, U64, P, U64, P, I, I64, P, U64, P, P, P, U64, P],
         "pase_softmax_loss_backward": [I, U64, U64, P, U64, P, I, I64, P, P, U64, P, U64, P],
     }
     for name, args in sig.items():
@@ -306,11 +305,9 @@ def softmax_loss_forward(logits, targets, ignore_index: int = -100):
     """(loss, lse) per row of logits [rows, classes], float32.  targets: [rows],
     int32 or int64; a row whose target is ignore_index has loss 0."""
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
-    L = load()
-    ws, wp, have = _workspace(logits, "pase_softmax_loss_workspace", d, rows, classes)
     loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
-    _check(L.pase_softmax_loss_forward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, loss.data_ptr(),
-                                       lse.data_ptr(), wp, have, _raw_stream(logits.get_device())))
+    _check(load().pase_softmax_loss_forward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index,
+                                            loss.data_ptr(), lse.data_ptr(), _raw_stream(logits.get_device())))
     return loss, lse
 
 
@@ -321,13 +318,11 @@ def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None
     for all), as where the loss is their mean.  out may be logits."""
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
     g, step = _row_gradient(dloss, rows, logits)
-    L = load()
-    ws, wp, have = _workspace(logits, "pase_softmax_loss_workspace", d, rows, classes)
     loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
     dlogits, lddl = _gradient_out(logits, out)
-    _check(L.pase_softmax_loss_grad(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, g, step,
-                                    loss.data_ptr(), lse.data_ptr(), dlogits.data_ptr(), lddl, wp, have,
-                                    _raw_stream(logits.get_device())))
+    _check(load().pase_softmax_loss_grad(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, g, step,
+                                         loss.data_ptr(), lse.data_ptr(), dlogits.data_ptr(), lddl,
+                                         _raw_stream(logits.get_device())))
     return loss, lse, dlogits
 
 

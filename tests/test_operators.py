@@ -37,10 +37,9 @@ PROD_F = dict(dtype=BF16, out=BF16, rows=4, groups=2, n=8, k=8, x=P, ldx=8, w=P,
               stream=None)
 PROD_B = dict(dtype=BF16, grad=BF16, rows=4, groups=2, n=8, k=8, dy=P, lddy=8, x=P, ldx=8, w=P, offsets=P, off64=0,
               dx=P, lddx=8, dw=P, ws=P, ws_bytes=1 << 20, stream=None)
-LOSS_F = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, loss=P, lse=P, ws=P,
-              ws_bytes=1 << 20, stream=None)
+LOSS_F = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, loss=P, lse=P, stream=None)
 LOSS_G = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, dloss=P, step=1, loss=P,
-              lse=P, dlogits=2 * P, lddl=8, ws=P, ws_bytes=1 << 20, stream=None)
+              lse=P, dlogits=2 * P, lddl=8, stream=None)
 LOSS_B = dict(dtype=BF16, rows=4, classes=8, logits=P, ldl=8, targets=P, t64=1, ignore=-100, lse=P, dloss=P, step=1,
               dlogits=2 * P, lddl=8, stream=None)
 
@@ -91,8 +90,7 @@ def test_refusals(lib, name, good, status, change):
 
 
 @pytest.mark.parametrize("name,args", [
-    ("pase_layer_norm_workspace", (BF16, 4, 8)), ("pase_grouped_matmul_workspace", (BF16, BF16, 4, 2, 8, 8)),
-    ("pase_softmax_loss_workspace", (BF16, 4, 8))])
+    ("pase_layer_norm_workspace", (BF16, 4, 8)), ("pase_grouped_matmul_workspace", (BF16, BF16, 4, 2, 8, 8))])
 def test_workspace_sizes(lib, name, args):
     need = C.c_uint64(12345)
     assert getattr(lib, name)(*args, C.byref(need)) == OK

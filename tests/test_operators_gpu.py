@@ -659,8 +659,7 @@ def test_outputs_keep_to_their_rows(ops):
     t, dloss = torch.randint(0, n, (rows,), generator=g, device="cuda"), torch.ones((), device="cuda")
     d, ll = room(rows, n), torch.empty(2, rows, device="cuda")
     assert L.pase_softmax_loss_grad(0, rows, n, out[1:].data_ptr(), out.stride(0), t.data_ptr(), 1, -100, dloss.data_ptr(), 0,
-                                    ll[0].data_ptr(), ll[1].data_ptr(), d[1:].data_ptr(), d.stride(0), ws.data_ptr(),
-                                    ws.numel(), stream) == 0
+                                    ll[0].data_ptr(), ll[1].data_ptr(), d[1:].data_ptr(), d.stride(0), stream) == 0
     assert torch.equal(d[1:-1, :n], ops.softmax_loss_grad(out[1:-1, :n], t, dloss)[2]) and untouched(d, n)
 
 
