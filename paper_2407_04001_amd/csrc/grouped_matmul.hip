@@ -228,11 +228,21 @@ template <typename T, typename O> struct Part {
 // ---------------------------------------------------------------- any alignment
 // Where a row may begin at an odd element.  128 x 128 tiles, 64 of i at a time; four waves, 64 x 64 each.  Operands go
 // through registers, where what lies past an edge becomes 0.  Bound by the latency of
-// those loads, one step ahead: 16384 x 4096 x 1024 in 8 groups 427 us (322 TFLOP/s).
+// those loads, one step ahead: 16384 x 1023 -> 4095 in 8 ragged groups 317 us (433
+// TFLOP/s), 487 with one workgroup a CU and every load tested against the edges.
 constexpr int kTile = 128, kDepth = 64;
 
 template <typename T, bool ACROSS>
 __device__ __forceinline__ void fetch(Pack<T> (&r)[4], const T *base, int64_t ld, int64_t rows, int64_t depth, int64_t i0) {
+    if (rows >= kTile && i0 + kDepth <= depth) {   // nothing past an edge: four loads in flight, no tests between
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            const int p = threadIdx.x + s * 256;
+            const T *from = ACROSS ? base + (i0 + (p >> 4)) * ld + (p & 15) * 8 : base + (p >> 3) * ld + i0 + (p & 7) * 8;
+            r[s].v = reinterpret_cast<const Unaligned16<T> *>(from)->v;
+        }
+        return;
+    }
 #pragma unroll
     for (int s = 0; s < 4; s++) {
         const int p = threadIdx.x + s * 256;
@@ -297,7 +307,7 @@ template <bool PAIRED, typename O> __device__ __forceinline__ void store_row(O *
     }
 }
 
-template <typename T, typename O, Direction D> __global__ __launch_bounds__(256) void k_product(GroupedProduct a) {
+template <typename T, typename O, Direction D> __global__ __launch_bounds__(256, 2) void k_product(GroupedProduct a) {
     constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
     __shared__ Pack<T> lds[2][2][kTile * 8];
     Part<T, O> p;
@@ -852,14 +862,17 @@ template <typename O> __global__ __launch_bounds__(256) void k_join(GroupedProdu
 // gradient 27, 32 and 43.  Big tiles take a time for each 64 of the contraction,
 // whatever rows are in them, and use no more CUs than there are tiles: the same
 // forward 24, 26 and 31 (128 tiles of 16 steps), gradient 73, 74 and 78 (32 tiles of 64
-// steps).  Where rows are not 4-byte aligned a tile takes 2.5 times as long.
+// steps).  Where rows are not 4-byte aligned a tile takes 2.2 times as long (16384 x
+// 1023 -> 4095 in 8 groups 317 us), and these kernels read at 1.0 and 2.7 TB/s (176 rows
+// a group of 32 x 1023 x 1365: 325 and 122 us).
 template <Direction D> bool few_rows(const GroupedProduct &a, bool big) {
     const double some = (double)a.rows / a.groups, live = a.groups * (1 - __builtin_exp(-some));
     const double reads = 2.0 * live * a.n * a.k * (some < 16 ? 1 : 0.75 + some / 64);
-    const double thin = D == kForward ? 4 + reads / (some < 16 ? 4.6e6 : 3.6e6) : 5 + reads / 5.0e6 + a.n * 0.004;
+    const double rate = D == kForward ? (!big ? 1.0e6 : some < 16 ? 4.6e6 : 3.6e6) : big ? 5.0e6 : 2.7e6;
+    const double thin = 4 + reads / rate + (D == kForward ? 0 : 1 + a.n * 0.004);
     const int cols = ((D == kForward ? a.n : a.k) + kBig - 1) / kBig, steps = ((D == kForward ? a.k : a.n) + 63) / 64;
     const double rounds = __builtin_ceil((some / kBig + 0.9) * a.groups * cols / kCus);
-    return thin < (7 + rounds * steps * 1.05) * (big ? 1 : 2.5);
+    return thin < (7 + rounds * steps * 1.05) * (big ? 1 : 2.2);
 }
 
 template <typename T, typename O, Direction D> int go(const GroupedProduct &a, void *stream) {
