@@ -77,8 +77,8 @@ pase_status pase_layer_norm_backward(int dtype, int param_dtype, uint64_t rows, 
  * w; out_dtype: dtype or PASE_FP32.  offsets: device array of groups + 1 entries,
  * int32 (offsets_64 = 0) or int64 (1), not decreasing, within 0..rows.  They are
  * read on the device only: rows below offsets[0] and from offsets[groups] on
- * belong to no group and get y = 0.  Offsets that break the rule are clamped into
- * 0..rows; which group's product a contested row gets is then unspecified. */
+ * belong to no group and get y = 0.  An offset outside 0..rows or below an earlier
+ * one is taken as the nearest that keeps the rule. */
 pase_status pase_grouped_matmul_forward(int dtype, int out_dtype, uint64_t rows, uint32_t groups,
                                         uint64_t n, uint64_t k, const void *x, uint64_t ldx, const void *w,
                                         const void *offsets, int offsets_64, void *y, uint64_t ldy,
