@@ -567,82 +567,82 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
 #pragma unroll
             for (int j = 0; j < 4; j++) acc[m][j] = 0.0f;
         if (p.depth > 0) {
-        const int steps = (p.depth + 63) >> 6;
-        if (stored)
-            wait_loads<8 + kStores>();
-        else
-            wait_loads<8>();
-        barrier();
-        // this step's and the next step's places, each operand's; the compiler would
-        // keep every fragment's address of both in registers, more than there are
-        uint32_t at_a = stage0 + ra.base, at_b = stage0 + kStage / 2 + rb.base;
-        uint32_t other_a = at_a + kStage, other_b = at_b + kStage;
-#pragma unroll
-        for (int m = 0; m < 4; m++) rb.read(g[0][m], at_b, m, 0), ra.read(f[0][m], at_a, m, 0);
-        for (int t = 0; t + 1 < steps; t++) {
-            char *cur = lds[t & 1];
-            asm volatile("" : "+v"(at_a), "+v"(at_b), "+v"(other_a), "+v"(other_b));
-#pragma unroll
-            for (int m = 0; m < 4; m++) {
-                multiply(f[0][m], g[0], m);
-                __builtin_amdgcn_sched_barrier(0);
-                ra.read(f[1][m], at_a, 4 + m, 0);
-                ra.read(f[2][m], at_a, m, 1);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int m = 0; m < 4; m++) {
-                multiply(f[1][m], g[0], 4 + m);
-                __builtin_amdgcn_sched_barrier(0);
-                if (m < 2) {
-#pragma unroll
-                    for (int k = 2 * m; k < 2 * m + 2; k++) rb.read(g[1][k], at_b, k, 1), ra.read(f[0][k], at_a, 4 + k, 1);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            fa.next(cur);
-            fb.next(cur + kStage / 2);
-            // all loads are the next step's; in a tile's first step the stores follow them
-            if (t == 0 && stored)
-                wait_loads<kStores>();
+            const int steps = (p.depth + 63) >> 6;
+            if (stored)
+                wait_loads<8 + kStores>();
             else
-                wait_loads<0>();
+                wait_loads<8>();
             barrier();
+            // this step's and the next step's places, each operand's; the compiler would
+            // keep every fragment's address of both in registers, more than there are
+            uint32_t at_a = stage0 + ra.base, at_b = stage0 + kStage / 2 + rb.base;
+            uint32_t other_a = at_a + kStage, other_b = at_b + kStage;
 #pragma unroll
-            for (int m = 0; m < 4; m++) {
-                multiply(f[2][m], g[1], m);
-                __builtin_amdgcn_sched_barrier(0);
-                fa.issue(m);
-                rb.read(g[0][m], other_b, m, 0);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int m = 0; m < 4; m++) rb.read(g[0][m], at_b, m, 0), ra.read(f[0][m], at_a, m, 0);
+            for (int t = 0; t + 1 < steps; t++) {
+                char *cur = lds[t & 1];
+                asm volatile("" : "+v"(at_a), "+v"(at_b), "+v"(other_a), "+v"(other_b));
+#pragma unroll
+                for (int m = 0; m < 4; m++) {
+                    multiply(f[0][m], g[0], m);
+                    __builtin_amdgcn_sched_barrier(0);
+                    ra.read(f[1][m], at_a, 4 + m, 0);
+                    ra.read(f[2][m], at_a, m, 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; m++) {
+                    multiply(f[1][m], g[0], 4 + m);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (m < 2) {
+#pragma unroll
+                        for (int k = 2 * m; k < 2 * m + 2; k++) rb.read(g[1][k], at_b, k, 1), ra.read(f[0][k], at_a, 4 + k, 1);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                fa.next(cur);
+                fb.next(cur + kStage / 2);
+                // all loads are the next step's; in a tile's first step the stores follow them
+                if (t == 0 && stored)
+                    wait_loads<kStores>();
+                else
+                    wait_loads<0>();
+                barrier();
+#pragma unroll
+                for (int m = 0; m < 4; m++) {
+                    multiply(f[2][m], g[1], m);
+                    __builtin_amdgcn_sched_barrier(0);
+                    fa.issue(m);
+                    rb.read(g[0][m], other_b, m, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; m++) {
+                    multiply(f[0][m], g[1], 4 + m);
+                    __builtin_amdgcn_sched_barrier(0);
+                    ra.read(f[0][m], other_a, m, 0);
+                    fb.issue(m);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const uint32_t ta = at_a, tb = at_b;
+                at_a = other_a, at_b = other_b, other_a = ta, other_b = tb;
             }
+            const int left = p.depth - (steps - 1) * 64;
 #pragma unroll
-            for (int m = 0; m < 4; m++) {
-                multiply(f[0][m], g[1], 4 + m);
-                __builtin_amdgcn_sched_barrier(0);
-                ra.read(f[0][m], other_a, m, 0);
-                fb.issue(m);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int h = 0; h < 2; h++) {
+#pragma unroll
+                for (int m = 0; m < 4; m++) {
+                    if (h) rb.read(g[0][m], at_b, m, 1), ra.read(f[0][m], at_a, m, 1);
+                    ra.read(f[1][m], at_a, 4 + m, h);
+                }
+                if (D != kWeights) {   // along i, what lies past the end is not 0; across, it is
+                    mask(f[0], left, h);
+                    mask(f[1], left, h);
+                    if (!B_ACROSS) mask(g[0], left, h);
+                }
+#pragma unroll
+                for (int m = 0; m < 8; m++) multiply(f[m >> 2][m & 3], g[0], m);
             }
-            const uint32_t ta = at_a, tb = at_b;
-            at_a = other_a, at_b = other_b, other_a = ta, other_b = tb;
-        }
-        const int left = p.depth - (steps - 1) * 64;
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-#pragma unroll
-            for (int m = 0; m < 4; m++) {
-                if (h) rb.read(g[0][m], at_b, m, 1), ra.read(f[0][m], at_a, m, 1);
-                ra.read(f[1][m], at_a, 4 + m, h);
-            }
-            if (D != kWeights) {   // along i, what lies past the end is not 0; across, it is
-                mask(f[0], left, h);
-                mask(f[1], left, h);
-                if (!B_ACROSS) mask(g[0], left, h);
-            }
-#pragma unroll
-            for (int m = 0; m < 8; m++) multiply(f[m >> 2][m & 3], g[0], m);
-        }
         }
         // the last loads, past the end, filled LDS with 0; nobody reads LDS any more
         wait_loads<0>();

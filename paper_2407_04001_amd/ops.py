@@ -7,8 +7,8 @@ what each computes.  The functions here check their arguments, allocate the
 outputs and enqueue the work on the current stream of the tensors' device;
 nothing waits for it.  A refused argument raises `PaseError`.
 
-``layer_norm``, ``grouped_matmul`` and ``softmax_loss`` are differentiable
-(`torch.autograd`); the others are the passes they are made of.
+``layer_norm``, ``grouped_matmul`` and ``softmax_loss`` are differentiable, once
+(`torch.autograd`; a second derivative raises); the others are the passes they are made of.
 """
 from __future__ import annotations
 
@@ -16,6 +16,7 @@ import ctypes as C
 import functools
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import pase
 from .pase import INVALID_ARGUMENT, PaseError
@@ -357,6 +358,7 @@ class _LayerNorm(torch.autograd.Function):
         return y, z
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dz):
         z, gain, mean, rstd = ctx.saved_tensors
         bias, residual = ctx.has
@@ -380,6 +382,7 @@ class _GroupedMatmul(torch.autograd.Function):
         return grouped_matmul_forward(x, w, offsets)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, w, offsets = ctx.saved_tensors
         dx, dw = grouped_matmul_backward(_rows_adjacent(dy), x, w, offsets, need_dx=ctx.needs_input_grad[0],
@@ -401,6 +404,7 @@ class _SoftmaxLoss(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         logits, targets, lse = ctx.saved_tensors
         if dloss.dim() == 1 and dloss.stride(0) not in (0, 1):

@@ -581,6 +581,15 @@ def test_autograd_matches_plain_gradients(ops):
         assert (m.grad.float() - p.grad).norm() <= 16 * U[HF] * p.grad.norm() + 1e-6
 
 
+def test_second_derivatives_are_refused(ops):
+    x = torch.randn(4, 8, device="cuda", requires_grad=True)
+    gain = torch.ones(8, device="cuda", requires_grad=True)
+    for y in (ops.layer_norm(x, gain).square().sum(), ops.softmax_loss(x, torch.arange(4, device="cuda")).square().sum()):
+        grad, = torch.autograd.grad(y, x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            grad.sum().backward()
+
+
 def test_another_stream_and_graph_replays(ops):
     """The same results on a side stream, and from every replay of a captured graph."""
     g = gen(22)
