@@ -299,6 +299,23 @@ def test_product_against_64_bits(ops, case, dtype):
         close(gw, dw, 2 * (max(lengths) + 8) * E * mw, "dw")
 
 
+@pytest.mark.parametrize("n,k", [(512, 512), (264, 511), (1000, 520)])
+@pytest.mark.parametrize("groups,around", [(80, 100), (150, 90), (70, 300)])
+def test_product_many_groups_exact(ops, groups, around, n, k):
+    """More groups than a wave has lanes, with enough rows for the tiled kernels."""
+    g = gen(groups + n)
+    lengths = torch.randint(0, 2 * around, (groups,), generator=g, device="cuda").tolist()
+    lengths[3] = lengths[groups - 1] = 0
+    rows = 5 + sum(lengths) + 9
+    x, dy, w = whole(g, rows, k, dtype=BF), whole(g, rows, n, dtype=BF), whole(g, groups, n, k, dtype=BF)
+    offsets = ranges(lengths, 5)
+    y, _ = product64(x, w, offsets)
+    assert torch.equal(ops.grouped_matmul_forward(x, w, offsets, out_dtype=SF), y.float())
+    dx, dw, _, _ = product_grad64(dy, x, w, offsets)
+    gx, gw = ops.grouped_matmul_backward(dy, x, w, offsets, grad_dtype=SF)
+    assert torch.equal(gx, dx.to(BF)) and torch.equal(gw, dw.float())
+
+
 def test_product_infinities_stay_in_their_rows(ops):
     """NaN and infinities of rows of other groups, of no group and past a row's end reach no other row."""
     g = gen(3)
