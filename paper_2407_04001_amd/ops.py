@@ -301,6 +301,13 @@ def _gradient_out(logits, out):
     return out, _matrix("out", out, logits, *logits.shape)
 
 
+def _written(out):
+    """Tells autograd that a caller's tensor was written, as an in-place torch
+    operation does: what had saved it for its backward pass raises there."""
+    if out is not None and not out.is_inference():   # an inference tensor has no version
+        torch.autograd.graph.increment_version(out)
+
+
 @_on_device(0)
 def softmax_loss_forward(logits, targets, ignore_index: int = -100):
     """(loss, lse) per row of logits [rows, classes], float32.  targets: [rows],
@@ -324,6 +331,7 @@ def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None
     _check(load().pase_softmax_loss_grad(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, g, step,
                                          loss.data_ptr(), lse.data_ptr(), dlogits.data_ptr(), lddl,
                                          _raw_stream(logits.get_device())))
+    _written(out)
     return loss, lse, dlogits
 
 
@@ -336,6 +344,7 @@ def softmax_loss_backward(dloss, logits, targets, lse, ignore_index: int = -100,
     dlogits, lddl = _gradient_out(logits, out)
     _check(load().pase_softmax_loss_backward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, s, g, step,
                                              dlogits.data_ptr(), lddl, _raw_stream(logits.get_device())))
+    _written(out)
     return dlogits
 
 

@@ -717,3 +717,29 @@ def test_refused_tensors(ops):
             lambda: ops.softmax_loss_grad(x, t, stat.double()), lambda: ops.softmax_loss_grad(x, t, stat[:2]),
             lambda: ops.softmax_loss_grad(x, t, stat, out=x.float()), lambda: ops.softmax_loss_backward(stat, x, t, stat[:2])):
         assert refused(ops, call)
+
+
+@pytest.mark.parametrize("saved_by", ["softmax_loss", "tanh"])
+@pytest.mark.parametrize("form", ["grad", "backward"])
+def test_gradient_in_place_is_known_to_autograd(ops, form, saved_by):
+    """A gradient written over logits that another node saved for its backward pass: that pass raises."""
+    g = gen(31)
+    base = rand(g, 6, 40).requires_grad_()
+    targets = torch.randint(0, 40, (6,), generator=g, device="cuda")
+    logits = torch.tanh(base)
+    y = ops.softmax_loss(logits, targets).sum() if saved_by == "softmax_loss" else logits.sum()
+    over, dloss = logits.detach(), torch.ones((), device="cuda")
+    if form == "grad":
+        ops.softmax_loss_grad(over, targets, dloss, out=over)
+    else:
+        ops.softmax_loss_backward(dloss, over, targets, ops.softmax_loss_forward(over, targets)[1], out=over)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_gradient_into_an_inference_tensor(ops):
+    """These have no version to raise."""
+    with torch.inference_mode():
+        out = torch.empty(3, 10, device="cuda")
+    logits, targets, dloss = torch.randn(3, 10, device="cuda"), torch.arange(3, device="cuda"), torch.ones((), device="cuda")
+    assert torch.equal(ops.softmax_loss_grad(logits, targets, dloss, out=out)[2], ops.softmax_loss_grad(logits, targets, dloss)[2])
