@@ -743,3 +743,23 @@ def test_gradient_into_an_inference_tensor(ops):
         out = torch.empty(3, 10, device="cuda")
     logits, targets, dloss = torch.randn(3, 10, device="cuda"), torch.arange(3, device="cuda"), torch.ones((), device="cuda")
     assert torch.equal(ops.softmax_loss_grad(logits, targets, dloss, out=out)[2], ops.softmax_loss_grad(logits, targets, dloss)[2])
+
+
+@pytest.mark.parametrize("dtype,param", [(BF, BF), (BF, SF), (SF, SF)])
+@pytest.mark.parametrize("width", [5, 61, 342, 1022, 2050, 8193])
+def test_norm_backward_where_mean_over_deviation_overflows(ops, width, dtype, param):
+    """Constant rows of 2e36: their deviations are 0, mean * rstd is past fp32's range."""
+    g = gen(width)
+    z = torch.full((3, width), 2e36, dtype=dtype, device="cuda")
+    mean = z[:, 0].float().contiguous()
+    rstd = torch.full((3,), 1e-5 ** -0.5, device="cuda")
+    dy, gain = rand(g, 3, width, dtype=dtype), rand(g, width, dtype=param, scale=0.3, shift=1.0)
+    dx, dgain, dbias = ops.layer_norm_backward(dy, z, gain, mean, rstd)
+    # h is 0, so that dx is rstd (dh - avg(dh)); the sum's and the products' roundings, as in the definition's bound
+    dh = dy.double() * gain.double()
+    r = rstd.double()[:, None]
+    want = r * (dh - dh.mean(1, keepdim=True))
+    tol = r * ((width + 8) * E * dh.abs().mean(1, keepdim=True) + 6 * E * (dh.abs() + dh.mean(1, keepdim=True).abs())) + 2 * E * want.abs()
+    close(dx, want, tol, "dx")
+    assert not dgain.any()
+    close(dbias, dy.double().sum(0), 11 * E * dy.double().abs().sum(0), "dbias")
