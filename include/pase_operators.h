@@ -104,10 +104,17 @@ pase_status pase_grouped_matmul_backward(int dtype, int grad_dtype, uint64_t row
  * (targets_64 = 0) or int64 (1).  A row whose target is ignore_index has loss 0
  * and lse 0, and its logits are not read.  A logit of -inf masks its class.  A
  * row with every class masked has lse -inf and loss +inf.  A target outside
- * 0..classes-1 that is not ignore_index gives loss NaN. */
+ * 0..classes-1 that is not ignore_index gives loss NaN.  The loss is formed from the
+ * differences to the row's maximum: it does not carry the rounding of lse. */
 pase_status pase_softmax_loss_forward(int dtype, uint64_t rows, uint64_t classes, const void *logits,
                                       uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
                                       float *loss, float *lse, void *stream);
+
+/* The same, with lse_low [rows]: what the rounding of lse to fp32 left of it (lse + lse_low
+ * is the log-sum-exp; 0 for ignored rows and rows with every class masked). */
+pase_status pase_softmax_loss_forward_parts(int dtype, uint64_t rows, uint64_t classes, const void *logits,
+                                            uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
+                                            float *loss, float *lse, float *lse_low, void *stream);
 
 /* Loss and gradient in one pass over the logits, for a loss gradient that is
  * known beforehand: dlogits[j] = (exp(logits[j] - lse) - [j = target]) * dloss.
@@ -119,11 +126,18 @@ pase_status pase_softmax_loss_grad(int dtype, uint64_t rows, uint64_t classes, c
                                    const float *dloss, uint64_t dloss_stride, float *loss, float *lse,
                                    void *dlogits, uint64_t lddl, void *stream);
 
-/* The gradient alone, from the lse of pase_softmax_loss_forward; same rules. */
+/* The gradient alone, from the lse of pase_softmax_loss_forward; same rules.  It carries
+ * the rounding of lse: exp(logits[j] - lse) is off by up to 2^-24 |lse| of itself. */
 pase_status pase_softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, const void *logits,
                                        uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
                                        const float *lse, const float *dloss, uint64_t dloss_stride,
                                        void *dlogits, uint64_t lddl, void *stream);
+
+/* The same without that rounding, from the lse and lse_low of pase_softmax_loss_forward_parts. */
+pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t classes, const void *logits,
+                                             uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
+                                             const float *lse, const float *lse_low, const float *dloss,
+                                             uint64_t dloss_stride, void *dlogits, uint64_t lddl, void *stream);
 
 #ifdef __cplusplus
 }

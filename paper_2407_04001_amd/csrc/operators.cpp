@@ -123,13 +123,14 @@ uint64_t product_bytes(uint64_t rows, uint32_t groups, uint64_t n, uint64_t k) {
 
 pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
                          const void *targets, int targets_64, int64_t ignore_index, const float *dloss,
-                         uint64_t dloss_stride, float *loss, float *lse, void *dlogits, uint64_t lddl,
+                         uint64_t dloss_stride, float *loss, float *lse, float *low, void *dlogits, uint64_t lddl,
                          bool grad, void *stream) {
     CHECK(check_loss(dtype, rows, classes, targets, targets_64));
     if (!rows) return PASE_OK;
     REQUIRE_MATRIX(logits, ldl, classes, dtype);
     REQUIRE(loss && lse, "loss or lse is null");
     REQUIRE(aligned(loss, 4) && aligned(lse, 4), "loss or lse is not aligned to its element");
+    REQUIRE(!low || aligned(low, 4), "lse_low is not aligned to its element");
     if (grad) {
         REQUIRE_MATRIX(dlogits, lddl, classes, dtype);
         REQUIRE(dloss && aligned(dloss, 4), "dloss is null or not aligned to its element");
@@ -142,9 +143,36 @@ pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void 
     a.logits = logits, a.ldl = (int64_t)ldl;
     a.targets = targets, a.ignore = ignore_index;
     a.dloss = dloss, a.dloss_stride = (int64_t)dloss_stride;
-    a.loss = loss, a.lse = lse;
+    a.loss = loss, a.lse = lse, a.low = low;
     a.dlogits = grad ? dlogits : nullptr, a.lddl = (int64_t)lddl;
     return launched(launch_softmax_loss(a, stream));
+}
+
+pase_status softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
+                                  const void *targets, int targets_64, int64_t ignore_index, const float *lse,
+                                  const float *low, const float *dloss, uint64_t dloss_stride, void *dlogits,
+                                  uint64_t lddl, void *stream) {
+    CHECK(check_loss(dtype, rows, classes, targets, targets_64));
+    if (!rows) return PASE_OK;
+    REQUIRE_MATRIX(logits, ldl, classes, dtype);
+    REQUIRE_MATRIX(dlogits, lddl, classes, dtype);
+    REQUIRE(lse && aligned(lse, 4), "lse is null or not aligned to its element");
+    REQUIRE(!low || aligned(low, 4), "lse_low is not aligned to its element");
+    REQUIRE(dloss && aligned(dloss, 4), "dloss is null or not aligned to its element");
+    REQUIRE(dloss_stride <= 1, "dloss_stride is neither 0 nor 1");
+    REQUIRE(dlogits != logits || ldl == lddl, "dlogits is logits with another row stride");
+    const uint64_t span = (uint64_t)kGradVecs * (16 / element_bytes(dtype));
+    if (rows > ((1ull << 31) - 1) / ((classes + span - 1) / span))
+        return refuse(PASE_ERR_TOO_LARGE, "the logits have too many elements for one call");
+    SoftmaxLoss a{};
+    a.dtype = dtype, a.targets_64 = targets_64;
+    a.rows = (int64_t)rows, a.classes = (int64_t)classes;
+    a.logits = logits, a.ldl = (int64_t)ldl;
+    a.targets = targets, a.ignore = ignore_index;
+    a.dloss = dloss, a.dloss_stride = (int64_t)dloss_stride;
+    a.lse = const_cast<float *>(lse), a.low = const_cast<float *>(low);
+    a.dlogits = dlogits, a.lddl = (int64_t)lddl;
+    return launched(launch_softmax_loss_backward(a, stream));
 }
 
 }  // namespace
@@ -315,7 +343,15 @@ pase_status pase_softmax_loss_forward(int dtype, uint64_t rows, uint64_t classes
                                       const void *targets, int targets_64, int64_t ignore_index, float *loss,
                                       float *lse, void *stream) {
     return softmax_loss(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, nullptr, 0, loss, lse,
-                        nullptr, 0, false, stream);
+                        nullptr, nullptr, 0, false, stream);
+}
+
+pase_status pase_softmax_loss_forward_parts(int dtype, uint64_t rows, uint64_t classes, const void *logits,
+                                            uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
+                                            float *loss, float *lse, float *lse_low, void *stream) {
+    if (rows) REQUIRE(lse_low, "lse_low is null");
+    return softmax_loss(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, nullptr, 0, loss, lse,
+                        lse_low, nullptr, 0, false, stream);
 }
 
 pase_status pase_softmax_loss_grad(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
@@ -323,33 +359,24 @@ pase_status pase_softmax_loss_grad(int dtype, uint64_t rows, uint64_t classes, c
                                    uint64_t dloss_stride, float *loss, float *lse, void *dlogits, uint64_t lddl,
                                    void *stream) {
     return softmax_loss(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, dloss, dloss_stride,
-                        loss, lse, dlogits, lddl, true, stream);
+                        loss, lse, nullptr, dlogits, lddl, true, stream);
 }
 
 pase_status pase_softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
                                        const void *targets, int targets_64, int64_t ignore_index, const float *lse,
                                        const float *dloss, uint64_t dloss_stride, void *dlogits, uint64_t lddl,
                                        void *stream) {
-    CHECK(check_loss(dtype, rows, classes, targets, targets_64));
-    if (!rows) return PASE_OK;
-    REQUIRE_MATRIX(logits, ldl, classes, dtype);
-    REQUIRE_MATRIX(dlogits, lddl, classes, dtype);
-    REQUIRE(lse && aligned(lse, 4), "lse is null or not aligned to its element");
-    REQUIRE(dloss && aligned(dloss, 4), "dloss is null or not aligned to its element");
-    REQUIRE(dloss_stride <= 1, "dloss_stride is neither 0 nor 1");
-    REQUIRE(dlogits != logits || ldl == lddl, "dlogits is logits with another row stride");
-    const uint64_t span = (uint64_t)kGradVecs * (16 / element_bytes(dtype));
-    if (rows > ((1ull << 31) - 1) / ((classes + span - 1) / span))
-        return refuse(PASE_ERR_TOO_LARGE, "the logits have too many elements for one call");
-    SoftmaxLoss a{};
-    a.dtype = dtype, a.targets_64 = targets_64;
-    a.rows = (int64_t)rows, a.classes = (int64_t)classes;
-    a.logits = logits, a.ldl = (int64_t)ldl;
-    a.targets = targets, a.ignore = ignore_index;
-    a.dloss = dloss, a.dloss_stride = (int64_t)dloss_stride;
-    a.lse = const_cast<float *>(lse);
-    a.dlogits = dlogits, a.lddl = (int64_t)lddl;
-    return launched(launch_softmax_loss_backward(a, stream));
+    return softmax_loss_backward(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, lse, nullptr,
+                                 dloss, dloss_stride, dlogits, lddl, stream);
+}
+
+pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t classes, const void *logits,
+                                             uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
+                                             const float *lse, const float *lse_low, const float *dloss,
+                                             uint64_t dloss_stride, void *dlogits, uint64_t lddl, void *stream) {
+    if (rows) REQUIRE(lse_low, "lse_low is null");
+    return softmax_loss_backward(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, lse, lse_low,
+                                 dloss, dloss_stride, dlogits, lddl, stream);
 }
 
 }  // extern "C"

@@ -41,6 +41,7 @@ struct SoftmaxLoss {
     float *loss, *lse;
     void *dlogits;
     int64_t lddl;
+    float *low;          // what lse's rounding leaves, or null
 };
 
 // c[m][j] = sum over the contraction of a and b; see grouped_matmul.hip for
@@ -74,7 +75,7 @@ constexpr int kGradVecs = 1024;   // 16-byte vectors of a row that one workgroup
 int launch_norm_forward(const NormForward &a, void *stream);
 int launch_norm_backward(const NormBackward &a, void *stream);
 int launch_softmax_loss(const SoftmaxLoss &a, void *stream);            // loss and lse; dlogits unless null
-int launch_softmax_loss_backward(const SoftmaxLoss &a, void *stream);   // dlogits from lse
+int launch_softmax_loss_backward(const SoftmaxLoss &a, void *stream);   // dlogits from lse and low
 int launch_product_forward(const GroupedProduct &a, void *stream);
 int launch_product_rows_grad(const GroupedProduct &a, void *stream);
 int launch_product_weights_grad(const GroupedProduct &a, void *stream);

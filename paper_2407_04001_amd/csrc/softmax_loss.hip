@@ -2,7 +2,10 @@
 // (pase_operators.h).
 //
 // With m the row's maximum, lse = m + ln sum exp(l - m): no exponent is
-// positive, so nothing overflows.  A row that fits is held in one workgroup's
+// positive, so nothing overflows.  The loss is (m - l[target]) + ln sum and the
+// gradient's exponents are (l - m) - ln sum: lse itself, rounded to fp32, would put
+// half a unit of m's last place into each, more than a small loss where all logits
+// of a row are large.  A row that fits is held in one workgroup's
 // registers as it was read, so that the maximum, the sum and the gradient take
 // one pass over HBM; a longer one is read again, its maximum and sum formed
 // together on the first pass (a sum of terms exp(l - m) grows by the factor
@@ -23,45 +26,57 @@ __device__ __forceinline__ int64_t target_of(const SoftmaxLoss &a, int64_t row) 
                         : (int64_t) static_cast<const int32_t *>(a.targets)[row];
 }
 
-// The row's lse from its maximum and sum, and its loss.  sum is 0 exactly when
-// every class is masked (otherwise the maximum's own term is 1 or NaN).
-__device__ __forceinline__ float row_lse(float top, float sum) {
-    return sum == 0.0f ? -__builtin_inff() : top + logf(sum);
-}
+// A row's log-sum-exp as two numbers whose sum it is: its maximum and the log of its
+// sum, or lse and what the rounding of lse left.  Both -inf (or -inf and 0): every class is
+// masked, as the sum is 0 then alone (otherwise the maximum's own term is 1 or NaN).
+struct Lse {
+    float high, low;
+    __device__ __forceinline__ bool empty() const { return high + low == -__builtin_inff(); }
+};
 
 template <typename T>
-__device__ __forceinline__ float row_loss(const T *logits, int64_t classes, int64_t target, float lse) {
+__device__ __forceinline__ float row_loss(const T *logits, int64_t classes, int64_t target, Lse lse) {
     if (target < 0 || target >= classes) return __builtin_nanf("");
-    return lse == -__builtin_inff() ? __builtin_inff() : lse - (float)logits[target];
+    return lse.empty() ? __builtin_inff() : (lse.high - (float)logits[target]) + lse.low;
 }
 
-// Gradient of one vector: (exp(l - lse) - [target]) * scale, where scale is 0 for
-// a row with every class masked and NaN for a target out of range.
+// lse, its remainder where asked for (exact: high + low = lse + remainder), and the loss of a row.
 template <typename T>
-__device__ __forceinline__ void grad_pack(T *out, int64_t at, int64_t n, const Pack<T> &l, float lse, int64_t target,
-                                          float scale) {
+__device__ __forceinline__ void put_row(const SoftmaxLoss &a, int64_t row, const T *logits, int64_t target, Lse lse) {
+    const float sum = lse.high + lse.low, of_low = sum - lse.high;
+    a.lse[row] = sum;
+    if (a.low) a.low[row] = lse.empty() ? 0.0f : (lse.high - (sum - of_low)) + (lse.low - of_low);
+    a.loss[row] = row_loss(logits, a.classes, target, lse);
+}
+
+// What a row's gradient needs: (exp(l - lse) - [target]) * scale, where scale is 0 for
+// a row with every class masked and NaN for a target out of range.
+struct RowGrad {
+    Lse lse;
+    float scale;
+};
+
+__device__ __forceinline__ RowGrad row_grad(const SoftmaxLoss &a, int64_t row, int64_t target, Lse lse) {
+    const float g = a.dloss[row * a.dloss_stride];
+    const bool known = target >= 0 && target < a.classes, empty = lse.empty();
+    // every class masked: any finite lse makes exp(-inf - lse) = 0, and the scale takes the target's -1 away
+    return {{empty ? 0.0f : lse.high, empty ? 0.0f : lse.low}, !known ? __builtin_nanf("") : empty ? 0.0f : g};
+}
+
+template <typename T> __device__ __forceinline__ T grad_of(T logit, bool target, const RowGrad &g) {
+    const float p = __expf(((float)logit - g.lse.high) - g.lse.low);
+    return (T)((target ? p - 1.0f : p) * g.scale);
+}
+
+// Gradient of one vector.  KEEP: the target's own place keeps its logit.
+template <typename T, bool KEEP = false>
+__device__ __forceinline__ void grad_pack(T *out, int64_t at, int64_t n, const Pack<T> &l, int64_t target, const RowGrad &g) {
     if (n <= 0) return;
     Pack<T> o;
     const int64_t hit = target - at;
 #pragma unroll
-    for (int j = 0; j < kVec<T>; j++) {
-        float p = __expf((float)l.e[j] - lse);
-        if (j == hit) p -= 1.0f;
-        o.e[j] = (T)(p * scale);
-    }
+    for (int j = 0; j < kVec<T>; j++) o.e[j] = KEEP && j == hit ? l.e[j] : grad_of(l.e[j], j == hit, g);
     store_pack(out + at, n, o);
-}
-
-struct RowGrad {
-    float lse, scale;
-};
-
-__device__ __forceinline__ RowGrad row_grad(const SoftmaxLoss &a, int64_t row, int64_t target, float lse) {
-    const float g = a.dloss[row * a.dloss_stride];
-    if (target < 0 || target >= a.classes) return {lse, __builtin_nanf("")};
-    // every class masked: any finite lse makes exp(-inf - lse) = 0, and the scale takes the target's -1 away
-    if (lse == -__builtin_inff()) return {0.0f, 0.0f};
-    return {lse, g};
 }
 
 template <typename T> __device__ __forceinline__ void zero_row(T *out, int64_t classes, int threads) {
@@ -84,7 +99,10 @@ __global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
     T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
     const int64_t target = target_of(a, row);
     if (target == a.ignore) {
-        if (threadIdx.x == 0) a.loss[row] = 0, a.lse[row] = 0;
+        if (threadIdx.x == 0) {
+            a.loss[row] = 0, a.lse[row] = 0;
+            if (a.low) a.low[row] = 0;
+        }
         if (GRAD) zero_row(out, a.classes, THREADS);
         return;
     }
@@ -107,8 +125,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
 #pragma unroll
         for (int j = 0; j < V; j++) s[0] += __expf((float)l[i].e[j] - from);
     group_sum<WAVES>(s, lds + WAVES);
-    const float lse = row_lse(top, s[0]);
-    if (threadIdx.x == 0) a.loss[row] = row_loss(logits, a.classes, target, lse), a.lse[row] = lse;
+    const Lse lse = {top, logf(s[0])};
+    if (threadIdx.x == 0) put_row(a, row, logits, target, lse);
     if (GRAD) {
         // in place, the target's logit is read above before its own lane writes it
         __syncthreads();
@@ -116,7 +134,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int64_t at = (int64_t)(threadIdx.x + i * THREADS) * V;
-            grad_pack(out, at, a.classes - at, l[i], g.lse, target, g.scale);
+            grad_pack(out, at, a.classes - at, l[i], target, g);
         }
     }
 }
@@ -125,9 +143,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_loss_row(SoftmaxLoss a) {
 // one by one (that pass also writes; with 8 in flight 1280 x 65536 in fp32 took 210 us
 // against 161).  4096 x 131072 in bf16: loss 188 us (1.07 GB, 5.7 TB/s), loss and
 // gradient 501 us; 1 x 131072 loss 9 us.
+// Or, where workgroups that share the row make its gradient (SPLIT): leaves the maximum in
+// lse and the log of the sum in loss for them.
 constexpr int kAhead = 8;
 
-template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_long(SoftmaxLoss a) {
+template <typename T, bool GRAD, bool SPLIT = false> __global__ __launch_bounds__(1024) void k_loss_long(SoftmaxLoss a) {
     constexpr int V = kVec<T>, WAVES = 16, THREADS = 1024;
     __shared__ float lds[2 * WAVES];
     const int64_t row = blockIdx.x;
@@ -135,7 +155,10 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_
     T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
     const int64_t target = target_of(a, row);
     if (target == a.ignore) {
-        if (threadIdx.x == 0) a.loss[row] = 0, a.lse[row] = 0;
+        if (threadIdx.x == 0) {
+            a.loss[row] = 0, a.lse[row] = 0;
+            if (a.low) a.low[row] = 0;
+        }
         if (GRAD) zero_row(out, a.classes, THREADS);
         return;
     }
@@ -163,25 +186,35 @@ template <typename T, bool GRAD> __global__ __launch_bounds__(1024) void k_loss_
     const float all = group_max<WAVES>(top, lds);
     float s[1] = {top == -__builtin_inff() ? sum : sum * __expf(top - all)};
     group_sum<WAVES>(s, lds + WAVES);
-    const float lse = row_lse(all, s[0]);
-    if (threadIdx.x == 0) a.loss[row] = row_loss(logits, a.classes, target, lse), a.lse[row] = lse;
+    const Lse lse = {all, logf(s[0])};
+    if (threadIdx.x == 0) {
+        if (SPLIT)
+            a.lse[row] = lse.high, a.loss[row] = lse.low;
+        else
+            put_row(a, row, logits, target, lse);
+    }
     if (GRAD) {
         __syncthreads();
         const RowGrad g = row_grad(a, row, target, lse);
         for (int64_t at = first; at < a.classes; at += stride)
-            grad_pack(out, at, a.classes - at, load_pack(logits + at, a.classes - at, masked<T>()), g.lse, target, g.scale);
+            grad_pack(out, at, a.classes - at, load_pack(logits + at, a.classes - at, masked<T>()), target, g);
     }
 }
 
-// Gradient from the lse: 256 threads take 4 vectors each of one row.
-template <typename T> __global__ __launch_bounds__(256) void k_loss_grad(SoftmaxLoss a, int chunks) {
+// Gradient from the lse, from it and its remainder, or from what k_loss_long left of a row
+// (kSplit; the target's place keeps its logit for k_loss_ends): 256 threads take 4 vectors
+// each of one row.
+enum From { kLse, kParts, kSplit };
+
+template <typename T, From F> __global__ __launch_bounds__(256) void k_loss_grad(SoftmaxLoss a, int chunks) {
     constexpr int V = kVec<T>;
     const int64_t row = blockIdx.x / chunks, at0 = (int64_t)(blockIdx.x % chunks) * kGradVecs * V + threadIdx.x * V;
     const T *logits = static_cast<const T *>(a.logits) + row * a.ldl;
     T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
+    if (at0 >= a.classes) return;   // before the row's values are waited for: most waves, where rows are short
     const int64_t target = target_of(a, row);
     const bool ignored = target == a.ignore;
-    const RowGrad g = row_grad(a, row, target, a.lse[row]);
+    const RowGrad g = row_grad(a, row, target, {a.lse[row], F == kSplit ? a.loss[row] : F == kParts ? a.low[row] : 0.0f});
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const int64_t at = at0 + (int64_t)i * 256 * V, n = a.classes - at;
@@ -191,14 +224,27 @@ template <typename T> __global__ __launch_bounds__(256) void k_loss_grad(Softmax
             zero.v = 0;
             store_pack(out + at, n, zero);
         } else {
-            grad_pack(out, at, n, load_pack(logits + at, n, masked<T>()), g.lse, target, g.scale);
+            grad_pack<T, F == kSplit>(out, at, n, load_pack(logits + at, n, masked<T>()), target, g);
         }
     }
 }
 
-template <typename T> int grad_typed(const SoftmaxLoss &a, void *stream) {
+// The end of a gradient that workgroups shared: the rows' loss and lse, and the gradient
+// of their targets, whose logits the others could not read once it is written.
+template <typename T> __global__ __launch_bounds__(256) void k_loss_ends(SoftmaxLoss a) {
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row >= a.rows) return;
+    const int64_t target = target_of(a, row);
+    if (target == a.ignore) return;
+    T *out = static_cast<T *>(a.dlogits) + row * a.lddl;
+    const Lse lse = {a.lse[row], a.loss[row]};
+    put_row(a, row, out, target, lse);
+    if (target >= 0 && target < a.classes) out[target] = grad_of(out[target], true, row_grad(a, row, target, lse));
+}
+
+template <typename T, From F> int grad_from(const SoftmaxLoss &a, void *stream) {
     const int chunks = (int)((a.classes + kGradVecs * kVec<T> - 1) / (kGradVecs * kVec<T>));
-    return launch(k_loss_grad<T>, a.rows * chunks, 256, stream, a, chunks);
+    return launch(k_loss_grad<T, F>, a.rows * chunks, 256, stream, a, chunks);
 }
 
 template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *stream) {
@@ -206,11 +252,20 @@ template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *strea
     if (vecs <= 256) return launch(k_loss_row<T, 4, 1, GRAD>, a.rows, 64, stream, a);
     if (vecs <= 1024) return launch(k_loss_row<T, 4, 4, GRAD>, a.rows, 256, stream, a);
     if (vecs <= 4096) return launch(k_loss_row<T, 8, 8, GRAD>, a.rows, 512, stream, a);
-    if (!GRAD || a.rows >= 2 * kCus) return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
-    // fewer rows than fill the chip: the gradient from the lse, by workgroups that share rows
-    // (1 x 131072 in fp32: 28 us in one kernel, 13 in two)
-    if (const int e = launch(k_loss_long<T, false>, a.rows, 1024, stream, a)) return e;
-    return grad_typed<T>(a, stream);
+    if constexpr (GRAD) {
+        // fewer rows than fill the chip: the gradient by workgroups that share rows
+        // (1 x 131072 in fp32: 28 us in one kernel, 14 in three)
+        if (a.rows < 2 * kCus) {
+            if (const int e = launch(k_loss_long<T, false, true>, a.rows, 1024, stream, a)) return e;
+            if (const int e = grad_from<T, kSplit>(a, stream)) return e;
+            return launch(k_loss_ends<T>, (a.rows + 255) / 256, 256, stream, a);
+        }
+    }
+    return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
+}
+
+template <typename T> int grad_typed(const SoftmaxLoss &a, void *stream) {
+    return a.low ? grad_from<T, kParts>(a, stream) : grad_from<T, kLse>(a, stream);
 }
 
 template <typename T> int loss_typed(const SoftmaxLoss &a, void *stream) {

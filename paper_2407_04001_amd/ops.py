@@ -28,8 +28,8 @@ MAX_GROUPS = 65536
 
 EXPORTS = ["pase_operator_error", "pase_layer_norm_forward", "pase_layer_norm_workspace",
            "pase_layer_norm_backward", "pase_grouped_matmul_forward", "pase_grouped_matmul_workspace",
-           "pase_grouped_matmul_backward", "pase_softmax_loss_forward",
-           "pase_softmax_loss_grad", "pase_softmax_loss_backward"]
+           "pase_grouped_matmul_backward", "pase_softmax_loss_forward", "pase_softmax_loss_forward_parts",
+           "pase_softmax_loss_grad", "pase_softmax_loss_backward", "pase_softmax_loss_backward_parts"]
 
 _lib = None
 
@@ -49,8 +49,10 @@ def load():
         "pase_grouped_matmul_workspace": [I, I, U64, U32, U64, U64, P],
         "pase_grouped_matmul_backward": [I, I, U64, U32, U64, U64, P, U64, P, U64, P, P, I, P, U64, P, P, U64, P],
         "pase_softmax_loss_forward": [I, U64, U64, P, U64, P, I, I64, P, P, P],
+        "pase_softmax_loss_forward_parts": [I, U64, U64, P, U64, P, I, I64, P, P, P, P],
         "pase_softmax_loss_grad": [I, U64, U64, P, U64, P, I, I64, P, U64, P, P, P, U64, P],
         "pase_softmax_loss_backward": [I, U64, U64, P, U64, P, I, I64, P, P, U64, P, U64, P],
+        "pase_softmax_loss_backward_parts": [I, U64, U64, P, U64, P, I, I64, P, P, P, U64, P, U64, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -309,10 +311,17 @@ def _written(out):
 
 
 @_on_device(0)
-def softmax_loss_forward(logits, targets, ignore_index: int = -100):
+def softmax_loss_forward(logits, targets, ignore_index: int = -100, low: bool = False):
     """(loss, lse) per row of logits [rows, classes], float32.  targets: [rows],
-    int32 or int64; a row whose target is ignore_index has loss 0."""
+    int32 or int64; a row whose target is ignore_index has loss 0.  With `low` also
+    what the rounding of lse left of it, for a gradient without that rounding."""
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
+    if low:
+        loss, lse, rest = logits.new_empty((3, rows), dtype=torch.float32).unbind()
+        _check(load().pase_softmax_loss_forward_parts(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index,
+                                                      loss.data_ptr(), lse.data_ptr(), rest.data_ptr(),
+                                                      _raw_stream(logits.get_device())))
+        return loss, lse, rest
     loss, lse = logits.new_empty((2, rows), dtype=torch.float32).unbind()
     _check(load().pase_softmax_loss_forward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index,
                                             loss.data_ptr(), lse.data_ptr(), _raw_stream(logits.get_device())))
@@ -336,14 +345,21 @@ def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None
 
 
 @_on_device(1)
-def softmax_loss_backward(dloss, logits, targets, lse, ignore_index: int = -100, out=None):
-    """dlogits from the lse of `softmax_loss_forward`.  out may be logits."""
+def softmax_loss_backward(dloss, logits, targets, lse, ignore_index: int = -100, out=None, lse_low=None):
+    """dlogits from the lse of `softmax_loss_forward`, and what its rounding left where
+    given.  out may be logits."""
     d, ldl, rows, classes, t, t64 = _loss_args(logits, targets)
     g, step = _row_gradient(dloss, rows, logits)
     s = _vector("lse", lse, rows, torch.float32, logits)
     dlogits, lddl = _gradient_out(logits, out)
-    _check(load().pase_softmax_loss_backward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, s, g, step,
-                                             dlogits.data_ptr(), lddl, _raw_stream(logits.get_device())))
+    L, stream = load(), _raw_stream(logits.get_device())
+    if lse_low is None:
+        _check(L.pase_softmax_loss_backward(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, s, g, step,
+                                            dlogits.data_ptr(), lddl, stream))
+    else:
+        r = _vector("lse_low", lse_low, rows, torch.float32, logits)
+        _check(L.pase_softmax_loss_backward_parts(d, rows, classes, logits.data_ptr(), ldl, t, t64, ignore_index, s, r, g,
+                                                  step, dlogits.data_ptr(), lddl, stream))
     _written(out)
     return dlogits
 
@@ -407,18 +423,18 @@ def grouped_matmul(x, w, offsets):
 class _SoftmaxLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, ignore_index):
-        loss, lse = softmax_loss_forward(logits, targets, ignore_index)
-        ctx.save_for_backward(logits, targets, lse)
+        loss, lse, low = softmax_loss_forward(logits, targets, ignore_index, low=True)
+        ctx.save_for_backward(logits, targets, lse, low)
         ctx.ignore_index = ignore_index
         return loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dloss):
-        logits, targets, lse = ctx.saved_tensors
+        logits, targets, lse, low = ctx.saved_tensors
         if dloss.dim() == 1 and dloss.stride(0) not in (0, 1):
             dloss = dloss.contiguous()
-        return softmax_loss_backward(dloss, logits, targets, lse, ctx.ignore_index), None, None
+        return softmax_loss_backward(dloss, logits, targets, lse, ctx.ignore_index, lse_low=low), None, None
 
 
 def softmax_loss(logits, targets, ignore_index: int = -100):

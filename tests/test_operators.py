@@ -138,3 +138,17 @@ def test_argument_checks_under_sanitizers():
                         "no:cacheprovider", "--pase-lib", san], cwd=ROOT, env=env, capture_output=True, text=True,
                        timeout=600)
     assert r.returncode == 0 and " passed" in r.stdout, (r.stdout + r.stderr)[-4000:]
+
+
+LOSS_FP = {k: v for kv in LOSS_F.items() for k, v in ([("low", P), kv] if kv[0] == "stream" else [kv])}
+LOSS_BP = {k: v for kv in LOSS_B.items() for k, v in ([kv, ("low", P)] if kv[0] == "lse" else [kv])}
+
+
+@pytest.mark.parametrize("name,good,bad", [
+    ("pase_softmax_loss_forward_parts", LOSS_FP, [dict(low=None), dict(low=P + 2), dict(lse=None), dict(dtype=3), dict(classes=0), dict(ldl=7)]),
+    ("pase_softmax_loss_backward_parts", LOSS_BP, [dict(low=None), dict(low=P + 2), dict(lse=None), dict(dtype=3), dict(step=2), dict(lddl=7)])])
+def test_refusals_of_the_two_part_forms(lib, name, good, bad):
+    for change in bad:
+        assert getattr(lib, name)(*{**good, **change}.values()) == INVALID, change
+        assert lib.pase_operator_error()
+    assert getattr(lib, name)(*{k: None if v in (P, 2 * P) else v for k, v in {**good, "rows": 0}.items()}.values()) == OK

@@ -763,3 +763,84 @@ def test_norm_backward_where_mean_over_deviation_overflows(ops, width, dtype, pa
     close(dx, want, tol, "dx")
     assert not dgain.any()
     close(dbias, dy.double().sum(0), 11 * E * dy.double().abs().sum(0), "dbias")
+
+
+def loss_bounds(logits, targets, dloss):
+    """loss64's loss and gradient, with bounds that do not grow with an offset that all logits of a row share.
+
+    In fp32: x = l - max (off by e |x|); the sum of its exponentials (each off by 2 e (|x| + 4) of itself, and n e
+    in the summing); the log of that; then exp(x - log sum), whose exponent is off by e |x| and e of itself again."""
+    loss, _, d, _, _, _ = loss64(logits, targets, dloss)
+    l = logits.double()
+    x = l - l.max(1, keepdim=True).values
+    p, logsum = torch.softmax(l, 1), torch.logsumexp(x, 1)
+    far = -x.gather(1, targets[:, None])[:, 0]
+    sum_err = (p * (x.abs() + 4) * 2 * E).sum(1) + (l.shape[1] + 8) * E + 2 * E * logsum
+    loss_err = sum_err + 2 * E * (far + loss.abs())
+    rel = 4 * E * (x.abs() + logsum[:, None] + 2) + sum_err[:, None]
+    return loss, d, loss_err, p * rel * dloss.double().expand(len(l))[:, None].abs() + 4 * E * d.abs()
+
+
+@pytest.mark.parametrize("shift", [0.0, 1e3, -1e6])
+@pytest.mark.parametrize("rows,classes", [(9, 64), (9, 5000), (5, 40000), (600, 17000)])
+def test_softmax_loss_of_shifted_logits(ops, rows, classes, shift):
+    """An offset common to a row's logits changes neither its loss nor its gradient, also where the target is far
+    above the rest and both are small."""
+    g = gen(classes)
+    logits = rand(g, rows, classes, scale=3.0)
+    targets = torch.randint(0, classes, (rows,), generator=g, device="cuda")
+    sure = torch.arange(0, rows, 2, device="cuda")
+    logits[sure, targets[sure]] = logits[sure].max(1).values + 15
+    logits += shift
+    dloss = rand(g, rows)
+    loss, d, el, ed = loss_bounds(logits, targets, dloss)
+    close(ops.softmax_loss_forward(logits, targets)[0], loss, el, "loss")
+    got, _, grad = ops.softmax_loss_grad(logits, targets, dloss)
+    close(got, loss, el, "loss, with the gradient")
+    close(grad, d, ed, "dlogits")
+    over = logits.clone()
+    ops.softmax_loss_grad(over, targets, dloss, out=over)
+    assert torch.equal(over, grad)
+    leaf = logits.clone().requires_grad_()
+    ops.softmax_loss(leaf, targets).backward(dloss)
+    close(leaf.grad, d, ed, "dlogits, autograd")
+
+
+@pytest.mark.parametrize("classes", [600, 40000])
+@pytest.mark.parametrize("dtype", [BF, HF, SF])
+def test_lse_in_two_parts(ops, classes, dtype):
+    """lse is as without its second part; the two together are the log-sum-exp to more than fp32; rows that are masked,
+    ignored, out of range or NaN keep their rules in the gradient from both."""
+    g = gen(classes + 1)
+    logits, targets = rand(g, 9, classes, dtype=dtype, shift=500.0), torch.randint(0, classes, (9,), generator=g, device="cuda")
+    logits[1] = -INF                              # no class left
+    logits[2, classes // 2:] = -INF               # the target is masked
+    targets[2] = classes - 1
+    logits[3] = float("nan")                      # ignored
+    targets[3], targets[4] = -100, classes        # ignored, out of range
+    logits[5, 7] = float("nan")
+    logits[6] = -INF
+    logits[6, 3] = float("nan")                   # nothing but NaN and masked classes
+    dloss = rand(g, 9)
+    loss, lse, low = ops.softmax_loss_forward(logits, targets, low=True)
+    plain = ops.softmax_loss_forward(logits, targets)
+    assert torch.equal(loss.nan_to_num(1e9), plain[0].nan_to_num(1e9)) and torch.equal(lse.nan_to_num(1e9), plain[1].nan_to_num(1e9))
+    keep = [0, 2, 4, 7, 8]
+    x = logits.double()
+    x = x - x.max(1, keepdim=True).values
+    p = torch.softmax(x, 1).nan_to_num(0, 0, 0)
+    logsum = torch.logsumexp(x, 1)
+    err = (p * (x.abs().nan_to_num(0, 0, 0) + 4) * 2 * E).sum(1) + (classes + 8) * E + 2 * E * logsum
+    off = (lse.double() + low.double() - torch.logsumexp(logits.double(), 1)).abs()
+    assert (off[keep] <= err[keep]).all() and (low[keep].abs() <= E * lse[keep].abs() * 1.01).all()
+    assert lse[1] == -INF and low[1] == 0 and loss[1] == INF and lse[3] == 0 and low[3] == 0 and loss[3] == 0
+    one, _, d = ops.softmax_loss_grad(logits, targets, dloss)
+    both = ops.softmax_loss_backward(dloss, logits, targets, lse, lse_low=low)
+    assert torch.equal(one.nan_to_num(1e9), loss.nan_to_num(1e9))
+    for t in (d, both):
+        assert not t[1].any() and not t[3].any() and t[[4, 5, 6]].isnan().all() and torch.isfinite(t[[0, 2, 7, 8]]).all()
+        assert abs(t[2, classes - 1] + dloss[2]) <= U[dtype] * dloss[2].abs()
+    over = logits.clone()
+    assert torch.equal(ops.softmax_loss_backward(dloss, over, targets, lse, out=over, lse_low=low).nan_to_num(1e9), both.nan_to_num(1e9))
+    over = logits.clone()
+    assert torch.equal(ops.softmax_loss_grad(over, targets, dloss, out=over)[2].nan_to_num(1e9), d.nan_to_num(1e9))
