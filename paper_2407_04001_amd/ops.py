@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import inspect
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -75,13 +76,18 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _on_device(which):
-    """Runs an operator with the device of its argument number `which` as the
+def _on_device(name):
+    """Runs an operator with the device of its argument `name` as the
     current one; the operator enqueues on that device's current stream."""
     def wrap(fn):
+        which = list(inspect.signature(fn).parameters).index(name)
+
         @functools.wraps(fn)
         def run(*args, **kw):
-            index = args[which].get_device()
+            t = args[which] if len(args) > which else kw.get(name)
+            if t is None:
+                return fn(*args, **kw)   # says which argument is missing
+            index = t.get_device()
             if index < 0 or index == torch.cuda.current_device():   # a host tensor is refused by the checks
                 return fn(*args, **kw)
             with torch.cuda.device(index):
@@ -167,7 +173,7 @@ def _params(gain, bias, width, x):
     return g, _vector("bias", bias, width, gain.dtype, x) if bias is not None else None
 
 
-@_on_device(0)
+@_on_device("x")
 def layer_norm_forward(x, gain, bias=None, residual=None, eps: float = 1e-5):
     """(y, z, mean, rstd) of the rows of z = x + residual [rows, width]; without
     a residual z is x itself.  gain, bias: [width], in x's type or float32."""
@@ -188,7 +194,7 @@ def layer_norm_forward(x, gain, bias=None, residual=None, eps: float = 1e-5):
     return y, z, mean, rstd
 
 
-@_on_device(0)
+@_on_device("dy")
 def layer_norm_backward(dy, z, gain, mean, rstd, dz=None):
     """(dx, dgain, dbias): dx is the gradient of x and of the residual alike.
     dz: the gradient that reaches z other than through the norm."""
@@ -228,7 +234,7 @@ def _out_dtype(name, want, dtype):
     return want
 
 
-@_on_device(0)
+@_on_device("x")
 def grouped_matmul_forward(x, w, offsets, out_dtype=None):
     """y[t] = w[e] x[t] for the rows t of each group e, offsets[e] .. offsets[e + 1] - 1.
 
@@ -249,7 +255,7 @@ def grouped_matmul_forward(x, w, offsets, out_dtype=None):
     return y
 
 
-@_on_device(0)
+@_on_device("dy")
 def grouped_matmul_backward(dy, x, w, offsets, grad_dtype=None, need_dx: bool = True, need_dw: bool = True):
     """(dx, dw) of `grouped_matmul_forward`: dx in dy's type, dw [groups, n, k] in
     dy's type or float32 (grad_dtype).  One that is not needed is None."""
@@ -310,7 +316,7 @@ def _written(out):
         torch.autograd.graph.increment_version(out)
 
 
-@_on_device(0)
+@_on_device("logits")
 def softmax_loss_forward(logits, targets, ignore_index: int = -100, low: bool = False):
     """(loss, lse) per row of logits [rows, classes], float32.  targets: [rows],
     int32 or int64; a row whose target is ignore_index has loss 0.  With `low` also
@@ -328,7 +334,7 @@ def softmax_loss_forward(logits, targets, ignore_index: int = -100, low: bool = 
     return loss, lse
 
 
-@_on_device(0)
+@_on_device("logits")
 def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None):
     """(loss, lse, dlogits) in one pass over the logits, for a gradient of the
     rows' losses that is known beforehand (dloss: float32 [rows], or one value
@@ -344,7 +350,7 @@ def softmax_loss_grad(logits, targets, dloss, ignore_index: int = -100, out=None
     return loss, lse, dlogits
 
 
-@_on_device(1)
+@_on_device("logits")
 def softmax_loss_backward(dloss, logits, targets, lse, ignore_index: int = -100, out=None, lse_low=None):
     """dlogits from the lse of `softmax_loss_forward`, and what its rounding left where
     given.  out may be logits."""

@@ -152,3 +152,21 @@ def test_refusals_of_the_two_part_forms(lib, name, good, bad):
         assert getattr(lib, name)(*{**good, **change}.values()) == INVALID, change
         assert lib.pase_operator_error()
     assert getattr(lib, name)(*{k: None if v in (P, 2 * P) else v for k, v in {**good, "rows": 0}.items()}.values()) == OK
+
+
+def test_arguments_by_name_are_checked_alike():
+    """Every pass function takes its arguments by name; the host tensors here are refused, by name as in order."""
+    from paper_2407_04001_amd import PaseError, ops
+    x, t, v = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64), torch.zeros(4)
+    b, w, off = x.bfloat16(), torch.zeros(2, 8, 8, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    for call in (lambda: ops.layer_norm_forward(gain=v, x=x), lambda: ops.layer_norm_backward(dy=x, z=x, gain=v, mean=v, rstd=v),
+                 lambda: ops.grouped_matmul_forward(x=b, w=w, offsets=off),
+                 lambda: ops.grouped_matmul_backward(dy=b, x=b, w=w, offsets=off),
+                 lambda: ops.softmax_loss_forward(logits=x, targets=t), lambda: ops.softmax_loss_grad(logits=x, targets=t, dloss=v),
+                 lambda: ops.softmax_loss_backward(v, logits=x, targets=t, lse=v),
+                 lambda: ops.softmax_loss_backward(dloss=v, logits=x, targets=t, lse=v)):
+        with pytest.raises(PaseError) as e:
+            call()
+        assert e.value.status == INVALID
+    with pytest.raises(TypeError, match="missing 1 required positional argument: 'x'"):
+        ops.layer_norm_forward(gain=v)

@@ -844,3 +844,21 @@ def test_lse_in_two_parts(ops, classes, dtype):
     assert torch.equal(ops.softmax_loss_backward(dloss, over, targets, lse, out=over, lse_low=low).nan_to_num(1e9), both.nan_to_num(1e9))
     over = logits.clone()
     assert torch.equal(ops.softmax_loss_grad(over, targets, dloss, out=over)[2].nan_to_num(1e9), d.nan_to_num(1e9))
+
+
+def test_arguments_by_name(ops):
+    g = gen(33)
+    x, gain, w = rand(g, 5, 8, dtype=BF), rand(g, 8, dtype=BF), rand(g, 2, 6, 8, dtype=BF)
+    offsets, targets, dloss = ranges([2, 3]), torch.arange(5, device="cuda"), torch.ones((), device="cuda")
+    y, z, mean, rstd = ops.layer_norm_forward(x, gain)
+    dy = rand(g, 5, 6, dtype=BF)
+    loss, lse = ops.softmax_loss_forward(x, targets)
+    for a, b in (
+            (ops.layer_norm_forward(gain=gain, x=x)[0], y),
+            (ops.layer_norm_backward(dy=y, z=z, gain=gain, mean=mean, rstd=rstd)[0], ops.layer_norm_backward(y, z, gain, mean, rstd)[0]),
+            (ops.grouped_matmul_forward(x=x, w=w, offsets=offsets), ops.grouped_matmul_forward(x, w, offsets)),
+            (ops.grouped_matmul_backward(dy=dy, x=x, w=w, offsets=offsets)[1], ops.grouped_matmul_backward(dy, x, w, offsets)[1]),
+            (ops.softmax_loss_forward(logits=x, targets=targets)[0], loss),
+            (ops.softmax_loss_grad(targets=targets, logits=x, dloss=dloss)[2], ops.softmax_loss_grad(x, targets, dloss)[2]),
+            (ops.softmax_loss_backward(dloss=dloss, logits=x, targets=targets, lse=lse), ops.softmax_loss_backward(dloss, x, targets, lse))):
+        assert torch.equal(a, b)
