@@ -10,7 +10,8 @@
  *
  * Conventions:
  *  - Return value: PASE_OK or a pase_status of pase.h; pase_operator_error()
- *    then holds the reason.  On an error nothing has been enqueued.
+ *    then holds the reason.  On an error other than PASE_ERR_HIP nothing has been
+ *    enqueued.
  *  - Every array is device memory of the current device, owned by the caller;
  *    inputs are only read.  Work is enqueued on `stream` (a hipStream_t, NULL =
  *    the null stream) and the call returns without waiting for it.  Nothing is

@@ -203,9 +203,9 @@ template <typename T, typename O> struct Part {
     // run's sums are a matrix of their own).
     template <int BM, int BN> __device__ __forceinline__ void weights(const GroupedProduct &g) {
         const uint32_t nt = (g.n + BM - 1) / BM, kt = (g.k + BN - 1) / BN, tiles = nt * kt;
-        const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles);
+        const uint32_t block = g.first + blockIdx.x, item = __builtin_amdgcn_readfirstlane(block / tiles);
         // workgroups go round the XCDs: an XCD gets neighbouring tiles of a group
-        uint32_t t = blockIdx.x - item * tiles;
+        uint32_t t = block - item * tiles;
         if (tiles % kXcds == 0) t = t % kXcds * (tiles / kXcds) + t / kXcds;
         const int m0 = __builtin_amdgcn_readfirstlane(t / kt * BM), j0 = __builtin_amdgcn_readfirstlane(t % kt * BN);
         const int part = __builtin_amdgcn_readfirstlane(item / g.groups), e = longest(g, item - part * g.groups);
@@ -314,7 +314,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256,
     if (D == kWeights) {
         p.template weights<kTile, kTile>(a);
     } else {
-        const Tile t = Deal<kTile>(a, ((D == kForward ? a.n : a.k) + kTile - 1) / kTile).get(a, blockIdx.x / kXcds);
+        const Tile t = Deal<kTile>(a, ((D == kForward ? a.n : a.k) + kTile - 1) / kTile).get(a, a.first + blockIdx.x / kXcds);
         if (t.none) return;
         p.template rows<D, kTile, kTile>(a, t);
     }
@@ -682,7 +682,7 @@ template <typename T, typename O, int MT> __global__ __launch_bounds__(256) void
     };
     constexpr int JT = 2, BM = 16 * MT, BN = 16 * JT;
     __shared__ f32x4 join[3][MT * JT][64];
-    const Tile tile = Deal<BM>(a, (a.n + BN - 1) / BN).get(a, blockIdx.x / kXcds);
+    const Tile tile = Deal<BM>(a, (a.n + BN - 1) / BN).get(a, a.first + blockIdx.x / kXcds);
     if (tile.none) return;
     Part<T, O> p;
     p.template rows<kForward, BM, BN>(a, tile);
@@ -754,7 +754,7 @@ template <typename T, int MT> __global__ __launch_bounds__(256) void k_rows_grad
     };
     constexpr int JT = 4, BM = 16 * MT, BN = 16 * JT, kRow = BN * 2 + 16;   // LDS bytes of a row: 16 more, for the banks
     __shared__ __attribute__((aligned(16))) char lds[4 * 32 * kRow > 3 * MT * JT * 1024 ? 4 * 32 * kRow : 3 * MT * JT * 1024];
-    const Tile tile = Deal<BM>(a, (a.k + BN - 1) / BN).get(a, blockIdx.x / kXcds);
+    const Tile tile = Deal<BM>(a, (a.k + BN - 1) / BN).get(a, a.first + blockIdx.x / kXcds);
     if (tile.none) return;
     Part<T, T> p;
     p.template rows<kRowsGrad, BM, BN>(a, tile);
@@ -837,6 +837,18 @@ template <int BM, int BN, Direction D> int64_t blocks_for(const GroupedProduct &
     return (tiles + kXcds - 1) / kXcds * kXcds;
 }
 
+// Launches a kernel that takes one tile a workgroup, on as many of the `blocks` tiles at a
+// time as one launch holds.  a.first is where the launch begins: a tile of the weights'
+// gradient, or a tile of each XCD's run.
+template <Direction D, typename K> int launch_tiles(K *kernel, int64_t blocks, int threads, void *stream, GroupedProduct a) {
+    const int64_t most = most_blocks(threads) / kXcds * kXcds;
+    for (int64_t at = 0; at < blocks; at += most) {
+        a.first = (uint32_t)(D == kWeights ? at : at / kXcds);
+        if (const int e = launch(kernel, blocks - at < most ? blocks - at : most, threads, stream, a)) return e;
+    }
+    return 0;
+}
+
 // The sum of a.splits matrices of `count` elements, in order.
 template <typename O> __global__ __launch_bounds__(256) void k_join(GroupedProduct a, int64_t count) {
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -881,20 +893,20 @@ template <typename T, typename O, Direction D> int go(const GroupedProduct &a, v
         if (few_rows<D>(a, big)) {
             const int64_t some = a.rows / a.groups;
             if constexpr (D == kForward) {
-                if (some < 8) return launch(k_product_thin<T, O, 1>, blocks_for<16, 32, D>(a), 256, stream, a);
-                if (some < 16) return launch(k_product_thin<T, O, 2>, blocks_for<32, 32, D>(a), 256, stream, a);
-                return launch(k_product_thin<T, O, 4>, blocks_for<64, 32, D>(a), 256, stream, a);
+                if (some < 8) return launch_tiles<D>(k_product_thin<T, O, 1>, blocks_for<16, 32, D>(a), 256, stream, a);
+                if (some < 16) return launch_tiles<D>(k_product_thin<T, O, 2>, blocks_for<32, 32, D>(a), 256, stream, a);
+                return launch_tiles<D>(k_product_thin<T, O, 4>, blocks_for<64, 32, D>(a), 256, stream, a);
             } else {
-                if (some < 8) return launch(k_rows_grad_thin<T, 1>, blocks_for<16, 64, D>(a), 256, stream, a);
-                if (some < 16) return launch(k_rows_grad_thin<T, 2>, blocks_for<32, 64, D>(a), 256, stream, a);
-                return launch(k_rows_grad_thin<T, 4>, blocks_for<64, 64, D>(a), 256, stream, a);
+                if (some < 8) return launch_tiles<D>(k_rows_grad_thin<T, 1>, blocks_for<16, 64, D>(a), 256, stream, a);
+                if (some < 16) return launch_tiles<D>(k_rows_grad_thin<T, 2>, blocks_for<32, 64, D>(a), 256, stream, a);
+                return launch_tiles<D>(k_rows_grad_thin<T, 4>, blocks_for<64, 64, D>(a), 256, stream, a);
             }
         }
     }
-    if (!big) return launch(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
+    if (!big) return launch_tiles<D>(k_product<T, O, D>, blocks_for<kTile, kTile, D>(a), 256, stream, a);
     int64_t blocks = blocks_for<kBig, kBig, D>(a);
     if (D != kWeights && blocks > kCus) blocks = kCus;   // one a CU: LDS holds no second
-    return launch(k_product_big<T, O, D>, blocks, 512, stream, a);
+    return launch_tiles<D>(k_product_big<T, O, D>, blocks, 512, stream, a);
 }
 
 template <typename T> int weights(const GroupedProduct &a, void *stream) {

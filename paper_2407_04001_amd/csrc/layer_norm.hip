@@ -280,7 +280,19 @@ struct Forward {
     const NormForward &a;
     void *stream;
     template <typename T, typename P, int NV, int LANES> int operator()() {
-        return launch(k_norm_forward<T, P, NV, LANES>, (a.rows + kTeams<LANES> - 1) / kTeams<LANES>, kBlock<LANES>, stream, a);
+        constexpr int TEAMS = kTeams<LANES>, THREADS = kBlock<LANES>;
+        const int64_t most = most_blocks(THREADS) * TEAMS;
+        for (int64_t row = 0; row < a.rows; row += most) {
+            NormForward part = a;
+            part.rows = a.rows - row < most ? a.rows - row : most;
+            part.x = static_cast<const T *>(a.x) + row * a.ldx;
+            if (a.residual) part.residual = static_cast<const T *>(a.residual) + row * a.ldr;
+            part.y = static_cast<T *>(a.y) + row * a.ldy;
+            if (a.z) part.z = static_cast<T *>(a.z) + row * a.ldz;
+            part.mean = a.mean + row, part.rstd = a.rstd + row;
+            if (const int e = launch(k_norm_forward<T, P, NV, LANES>, (part.rows + TEAMS - 1) / TEAMS, THREADS, stream, part)) return e;
+        }
+        return 0;
     }
 };
 

@@ -55,6 +55,7 @@ struct GroupedProduct {
     int64_t ldx, lddy, ldo;
     float *partial;      // weights gradient: [splits][groups][n][k] when splits > 1
     int splits;
+    uint32_t first;      // of this launch, where several share the tiles: see launch_tiles()
 };
 
 // 16-byte vectors of a layer norm's row, and the lanes of the team that holds it

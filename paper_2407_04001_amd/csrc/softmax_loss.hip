@@ -242,16 +242,35 @@ template <typename T> __global__ __launch_bounds__(256) void k_loss_ends(Softmax
     if (target >= 0 && target < a.classes) out[target] = grad_of(out[target], true, row_grad(a, row, target, lse));
 }
 
+// Launches a kernel of `blocks` workgroups a row, on as many rows at a time as one launch holds.
+template <typename T, typename K, typename... Args>
+int on_rows(K *kernel, int64_t blocks, int threads, void *stream, const SoftmaxLoss &a, Args... args) {
+    const int64_t most = most_blocks(threads) / blocks;
+    for (int64_t row = 0; row < a.rows; row += most) {
+        SoftmaxLoss part = a;
+        part.rows = a.rows - row < most ? a.rows - row : most;
+        part.logits = static_cast<const T *>(a.logits) + row * a.ldl;
+        part.targets = static_cast<const char *>(a.targets) + row * (a.targets_64 ? 8 : 4);
+        if (a.dloss) part.dloss = a.dloss + row * a.dloss_stride;
+        if (a.loss) part.loss = a.loss + row;
+        part.lse = a.lse + row;
+        if (a.low) part.low = a.low + row;
+        if (a.dlogits) part.dlogits = static_cast<T *>(a.dlogits) + row * a.lddl;
+        if (const int e = launch(kernel, part.rows * blocks, threads, stream, part, args...)) return e;
+    }
+    return 0;
+}
+
 template <typename T, From F> int grad_from(const SoftmaxLoss &a, void *stream) {
     const int chunks = (int)((a.classes + kGradVecs * kVec<T> - 1) / (kGradVecs * kVec<T>));
-    return launch(k_loss_grad<T, F>, a.rows * chunks, 256, stream, a, chunks);
+    return on_rows<T>(k_loss_grad<T, F>, chunks, 256, stream, a, chunks);
 }
 
 template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *stream) {
     const int64_t vecs = (a.classes + kVec<T> - 1) / kVec<T>;
-    if (vecs <= 256) return launch(k_loss_row<T, 4, 1, GRAD>, a.rows, 64, stream, a);
-    if (vecs <= 1024) return launch(k_loss_row<T, 4, 4, GRAD>, a.rows, 256, stream, a);
-    if (vecs <= 4096) return launch(k_loss_row<T, 8, 8, GRAD>, a.rows, 512, stream, a);
+    if (vecs <= 256) return on_rows<T>(k_loss_row<T, 4, 1, GRAD>, 1, 64, stream, a);
+    if (vecs <= 1024) return on_rows<T>(k_loss_row<T, 4, 4, GRAD>, 1, 256, stream, a);
+    if (vecs <= 4096) return on_rows<T>(k_loss_row<T, 8, 8, GRAD>, 1, 512, stream, a);
     if constexpr (GRAD) {
         // fewer rows than fill the chip: the gradient by workgroups that share rows
         // (1 x 131072 in fp32: 28 us in one kernel, 14 in three)
@@ -261,7 +280,7 @@ template <typename T, bool GRAD> int loss_rows(const SoftmaxLoss &a, void *strea
             return launch(k_loss_ends<T>, (a.rows + 255) / 256, 256, stream, a);
         }
     }
-    return launch(k_loss_long<T, GRAD>, a.rows, 1024, stream, a);
+    return on_rows<T>(k_loss_long<T, GRAD>, 1, 1024, stream, a);
 }
 
 template <typename T> int grad_typed(const SoftmaxLoss &a, void *stream) {

@@ -90,9 +90,13 @@ template <int WAVES> __device__ __forceinline__ float group_max(float v, float *
     return v;
 }
 
+// A launch holds fewer than 2^32 threads; operators with more cut their rows or tiles into several.
+inline int64_t most_blocks(int threads) { return ((1ll << 32) - 1) / threads; }
+
 template <typename F, typename... Args>
 inline int launch(F *kernel, int64_t blocks, int threads, void *stream, Args... args) {
     void *ptrs[] = {(void *)&args...};
+    if (blocks > most_blocks(threads)) return (int)hipErrorInvalidConfiguration;
     return (int)hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)blocks), dim3(threads), ptrs, 0,
                                 static_cast<hipStream_t>(stream));
 }

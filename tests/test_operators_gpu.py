@@ -862,3 +862,54 @@ def test_arguments_by_name(ops):
             (ops.softmax_loss_grad(targets=targets, logits=x, dloss=dloss)[2], ops.softmax_loss_grad(x, targets, dloss)[2]),
             (ops.softmax_loss_backward(dloss=dloss, logits=x, targets=targets, lse=lse), ops.softmax_loss_backward(dloss, x, targets, lse))):
         assert torch.equal(a, b)
+
+
+def periodic(t, rows):
+    """t's rows over and over, `rows` of them (a multiple of its own)."""
+    return t.unsqueeze(0).expand(rows // len(t), *t.shape).reshape(rows, *t.shape[1:])
+
+
+def repeats(big, small):
+    """Whether big is small over and over."""
+    return all(bool((part.view(-1, *small.shape) == small).all()) for part in big.split(len(small) << 12))
+
+
+def test_norm_of_more_rows_than_one_launch_holds(ops):
+    """2^29 rows of 8: 32 rows a workgroup of 256 are more than 2^32 - 1 threads."""
+    g = gen(35)
+    x, res, gain = rand(g, 4096, 8, dtype=BF), rand(g, 4096, 8, dtype=BF), rand(g, 8, dtype=BF, shift=1.0)
+    few = ops.layer_norm_forward(x, gain, residual=res)
+    rows = (1 << 29) + 4096
+    many = ops.layer_norm_forward(periodic(x, rows), gain, residual=periodic(res, rows))
+    for a, b in zip(many, few):
+        assert a.shape[0] == rows and repeats(a, b)
+
+
+@pytest.mark.parametrize("each", [True, False])
+def test_softmax_loss_of_more_rows_than_one_launch_holds(ops, each):
+    """2^26 rows of a wave each, and their gradients by workgroups of 256."""
+    g = gen(36)
+    logits, targets = rand(g, 4096, 24, dtype=BF, scale=2.0), torch.randint(0, 24, (4096,), generator=g, device="cuda").int()
+    targets[5] = -100
+    dloss = rand(g, 4096) if each else torch.full((), 0.5, device="cuda")
+    loss, lse, low = ops.softmax_loss_forward(logits, targets, low=True)
+    d, both = ops.softmax_loss_grad(logits, targets, dloss)[2], ops.softmax_loss_backward(dloss, logits, targets, lse, lse_low=low)
+    rows = (1 << 26) + 4096
+    logits, targets = periodic(logits, rows), periodic(targets, rows)
+    dloss = periodic(dloss, rows) if each else dloss
+    for a, b in zip(ops.softmax_loss_forward(logits, targets, low=True), (loss, lse, low)):
+        assert repeats(a, b)
+    assert repeats(ops.softmax_loss_backward(dloss, logits, targets, periodic(lse, rows), lse_low=periodic(low, rows)), both)
+    assert all(repeats(a, b) for a, b in zip(ops.softmax_loss_grad(logits, targets, dloss, out=logits), (loss, lse, d)))
+
+
+def test_product_of_more_tiles_than_one_launch_holds(ops):
+    """512 groups of one row each and 2^20 columns: 17.9 million workgroups of 256."""
+    g = gen(37)
+    groups, n, k = 512, 1 << 20, 8
+    x, w = whole(g, groups, k, dtype=BF), whole(g, 8, n, k, dtype=BF)
+    offsets = torch.arange(groups + 1, dtype=torch.int32, device="cuda")
+    y = ops.grouped_matmul_forward(x, periodic(w, groups), offsets)
+    for t in range(groups):
+        want = (w[t % 8].float() * x[t].float()).sum(1)      # whole numbers below 2^24: exact
+        assert torch.equal(y[t], want.to(BF)), t
