@@ -129,7 +129,11 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_norm_backward(NormBackward a)
 #pragma unroll
         for (int j = 0; j < V; j++) dg[i][j] = db[i][j] = 0;
 
-    // the next row is on its way while this one is reduced
+    // The next row is on its way while this one is reduced.  Teams of 1024 lanes have 128
+    // registers a lane, too few for two rows (57 to 109 of them spilled): 4096 x 8200 in bf16 217 us with the
+    // next row against 101 without, 4096 x 16384 in fp32 405 against 250; rows of fp32 to 8192, where nothing
+    // spills either way, 4096 x 8192 112 us with and without.
+    constexpr bool AHEAD = LANES < 1024;
     Pack<T> ny[NV], nz[NV];
     float next_mean = 0, next_rstd = 0;
     const auto fetch = [&](int64_t row) {
@@ -143,14 +147,15 @@ __global__ __launch_bounds__(kBlock<LANES>) void k_norm_backward(NormBackward a)
         }
     };
     const int64_t first = (int64_t)blockIdx.x * TEAMS + team, stride = (int64_t)gridDim.x * TEAMS;
-    if (first < a.rows) fetch(first);
+    if (AHEAD && first < a.rows) fetch(first);
     int odd = 0;
     for (int64_t row = first; row < a.rows; row += stride, odd ^= 1) {
+        if (!AHEAD) fetch(row);
         const float mean = next_mean, rstd = next_rstd;
         Pack<T> py[NV], pz[NV];
 #pragma unroll
         for (int i = 0; i < NV; i++) py[i] = ny[i], pz[i] = nz[i];
-        if (row + stride < a.rows) fetch(row + stride);
+        if (AHEAD && row + stride < a.rows) fetch(row + stride);
         float g[NV][V];
         float s[2] = {0, 0};
 #pragma unroll

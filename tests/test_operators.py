@@ -170,3 +170,20 @@ def test_arguments_by_name_are_checked_alike():
         assert e.value.status == INVALID
     with pytest.raises(TypeError, match="missing 1 required positional argument: 'x'"):
         ops.layer_norm_forward(gain=v)
+
+
+def test_norm_kernels_keep_their_rows_in_registers(tmp_path):
+    """What the compiler says of the layer norm kernels: at most a few registers of the widest rows are spilled (a
+    second row held by a team of 1024 lanes spills 56 and more, which doubled the time)."""
+    import subprocess
+    from paper_2407_04001_amd import build
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not os.path.exists(hipcc) or "libasan" in os.environ.get("LD_PRELOAD", ""):
+        pytest.skip("no hipcc, or the sanitizers' run")
+    r = subprocess.run([hipcc, *build.HIP_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", build.CSRC, "-c", "--offload-device-only",
+                        "-Rpass-analysis=kernel-resource-usage", os.path.join(build.CSRC, "layer_norm.hip"), "-o",
+                        str(tmp_path / "o")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    kernels = re.findall(r"Function Name: (\S+).*?VGPRs Spill: (\d+)", r.stderr, flags=re.S)
+    assert sum("k_norm_backward" in name for name, _ in kernels) >= 40
+    assert not [k for k in kernels if int(k[1]) > 16]
