@@ -442,7 +442,7 @@ template <typename T, bool ACROSS, bool J> struct Feed {
     }
 };
 
-// All but the last N loads (and stores) of this wave have ended, and its LDS reads.
+// All but the last N loads and stores of this wave have ended, and its LDS reads.
 template <int N> __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
@@ -505,7 +505,6 @@ template <typename F> __device__ __forceinline__ void mask_frag(F &f, int left) 
 
 template <typename T, typename O, Direction D> __global__ __launch_bounds__(512) void k_product_big(GroupedProduct a) {
     constexpr bool A_ACROSS = D == kWeights, B_ACROSS = D != kForward;
-    constexpr int kStores = 8 * 16 / kVec<O>;   // of a wave that stores a whole tile
     // A lane's 16 bytes of c are one fragment's 4 columns in fp32 and two fragments' 8
     // in 16 bits: the j side's rows are in order in the first case, paired in the second.
     constexpr bool PAIRED = sizeof(O) == 2;
@@ -557,7 +556,6 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         }
     };
     feed();
-    bool stored = false;   // kStores stores of the tile before are in flight behind this tile's first loads
     for (;;) {
         Tile after;
         after.none = true;
@@ -568,10 +566,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
             for (int j = 0; j < 4; j++) acc[m][j] = 0.0f;
         if (p.depth > 0) {
             const int steps = (p.depth + 63) >> 6;
-            if (stored)
-                wait_loads<8 + kStores>();
-            else
-                wait_loads<8>();
+            wait_loads<8>();   // this tile's second step may be on its way
             barrier();
             // this step's and the next step's places, each operand's; the compiler would
             // keep every fragment's address of both in registers, more than there are
@@ -602,11 +597,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
                 }
                 fa.next(cur);
                 fb.next(cur + kStage / 2);
-                // all loads are the next step's; in a tile's first step the stores follow them
-                if (t == 0 && stored)
-                    wait_loads<kStores>();
-                else
-                    wait_loads<0>();
+                wait_loads<0>();   // all are the next step's
                 barrier();
 #pragma unroll
                 for (int m = 0; m < 4; m++) {
@@ -649,14 +640,13 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(512)
         barrier();
         O *c = p.c;
         const int m_rows = p.m_rows, j_rows = p.j_rows;
-        if (!after.none) {   // the next tile's loads go before this one's stores
+        if (!after.none) {   // the next tile's loads go before this one's stores; finding the tile after it waits for both
             p.template rows<D, kBig, kBig>(a, after);
             feed();
         }
-        stored = m_rows >= kBig && j_rows >= kBig;
         const int row = wm + (lane & 15), col = wj + (lane >> 4) * kVec<O>;
         c += row * a.ldo + col;
-        if (stored) {
+        if (m_rows >= kBig && j_rows >= kBig) {
 #pragma unroll
             for (int m = 0; m < 8; m++) store_row<PAIRED>(c + m * 16 * a.ldo, 64, acc[m]);
         } else {
