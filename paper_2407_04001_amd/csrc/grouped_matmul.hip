@@ -909,16 +909,18 @@ template <typename T> int weights(const GroupedProduct &a, void *stream) {
     return narrow ? launch(k_join<T>, blocks, 256, stream, a, count) : launch(k_join<float>, blocks, 256, stream, a, count);
 }
 
-template <Direction D> int by_type(const GroupedProduct &a, void *stream) {
-    if (a.dtype == PASE_BF16)
-        return a.out_dtype == PASE_FP32 ? go<__bf16, float, D>(a, stream) : go<__bf16, __bf16, D>(a, stream);
-    return a.out_dtype == PASE_FP32 ? go<_Float16, float, D>(a, stream) : go<_Float16, _Float16, D>(a, stream);
+template <typename T> int forward(const GroupedProduct &a, void *stream) {
+    return a.out_dtype == PASE_FP32 ? go<T, float, kForward>(a, stream) : go<T, T, kForward>(a, stream);
 }
 
 }  // namespace
 
-int launch_product_forward(const GroupedProduct &a, void *stream) { return by_type<kForward>(a, stream); }
-int launch_product_rows_grad(const GroupedProduct &a, void *stream) { return by_type<kRowsGrad>(a, stream); }
+int launch_product_forward(const GroupedProduct &a, void *stream) {
+    return a.dtype == PASE_BF16 ? forward<__bf16>(a, stream) : forward<_Float16>(a, stream);
+}
+int launch_product_rows_grad(const GroupedProduct &a, void *stream) {   // always in the operands' type
+    return a.dtype == PASE_BF16 ? go<__bf16, __bf16, kRowsGrad>(a, stream) : go<_Float16, _Float16, kRowsGrad>(a, stream);
+}
 int launch_product_weights_grad(const GroupedProduct &a, void *stream) {
     return a.dtype == PASE_BF16 ? weights<__bf16>(a, stream) : weights<_Float16>(a, stream);
 }
