@@ -913,3 +913,32 @@ def test_product_of_more_tiles_than_one_launch_holds(ops):
     for t in range(groups):
         want = (w[t % 8].float() * x[t].float()).sum(1)      # whole numbers below 2^24: exact
         assert torch.equal(y[t], want.to(BF)), t
+
+
+@pytest.mark.parametrize("pad", [0, 8, 3])
+@pytest.mark.parametrize("rows,n,k", [(50, 24, 40), (3000, 520, 264), (3000, 1024, 1030)])
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_product_clamped_offsets(ops, rows, n, k, pad, dtype):
+    """Offsets that leave 0 .. rows or fall below an earlier one are those of the nearest that keep the rule."""
+    g = gen(rows + n)
+    x, dy = wide(whole(g, rows, k, dtype=BF), pad), wide(whole(g, rows, n, dtype=BF), pad)
+    w = whole(g, 4, n, k, dtype=BF)
+    a, b = rows // 5, rows // 2
+    for given, taken in (([-5, a, rows + 40, 7, b], [0, a, rows, rows, rows]), ([a, b, a - 3, b + 9, -1], [a, b, b, b + 9, b + 9]),
+                         ([rows + 1, 0, 0, 0, 0], [rows] * 5), ([-9] * 5, [0] * 5), ([7, -2 ** 31, 2 ** 31 - 1, 0, 3], [7, 7, rows, rows, rows])):
+        offsets, as_if = (torch.tensor(o, dtype=dtype, device="cuda") for o in (given, taken))
+        y, _ = product64(x, w, as_if)
+        assert torch.equal(ops.grouped_matmul_forward(x, w, offsets, out_dtype=SF), y.float())
+        dx, dw, _, _ = product_grad64(dy, x, w, as_if)
+        gx, gw = ops.grouped_matmul_backward(dy, x, w, offsets, grad_dtype=SF)
+        assert torch.equal(gx, dx.to(BF)) and torch.equal(gw, dw.float())
+
+
+def test_norm_constant_row_whose_squares_overflow(ops):
+    """y of a constant row is the bias, whatever fp32 makes of the square of its mean's rounding."""
+    x = torch.full((2, 300), 1e30, device="cuda")
+    gain, bias = torch.rand(300, device="cuda") + 0.5, torch.randn(300, device="cuda")
+    y, _, mean, rstd = ops.layer_norm_forward(x, gain, bias, eps=1e-5)
+    tol = 308 * E * 1e30
+    close(mean, x[:, 0].double(), tol, "mean")
+    assert torch.equal(y, bias.expand(2, 300))
