@@ -110,10 +110,10 @@ def _matrix(name, t, like=None, rows=None, cols=None):
     ld, step = t.stride()
     if step != 1 and have_cols > 1:
         _refuse(f"the elements of a row of {name} are {step} apart, not adjacent")
+    if have_rows < 2:
+        return have_cols   # whatever the distance to a next row is, also beyond the operators' limit
     if ld < have_cols:
-        if have_rows > 1:
-            _refuse(f"the rows of {name} overlap")
-        return have_cols
+        _refuse(f"the rows of {name} overlap")
     return ld
 
 

@@ -942,3 +942,16 @@ def test_norm_constant_row_whose_squares_overflow(ops):
     tol = 308 * E * 1e30
     close(mean, x[:, 0].double(), tol, "mean")
     assert torch.equal(y, bias.expand(2, 300))
+
+
+def test_one_row_of_a_wide_buffer(ops):
+    """The distance between rows does not matter where there is one."""
+    g = gen(34)
+    buffer = torch.zeros(2, 5_000_000, dtype=BF, device="cuda")
+    x = buffer[1:, :64]
+    x.copy_(rand(g, 1, 64))
+    w, offsets = rand(g, 1, 16, 64, dtype=BF), ranges([1])
+    dy = rand(g, 1, 16, dtype=BF)
+    assert torch.equal(ops.grouped_matmul_forward(x, w, offsets), ops.grouped_matmul_forward(x.clone(), w, offsets))
+    for a, b in zip(ops.grouped_matmul_backward(dy, x, w, offsets), ops.grouped_matmul_backward(dy, x.clone(), w, offsets)):
+        assert torch.equal(a, b)
