@@ -376,7 +376,7 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256,
 // without both 303: it is bound by neither alone.  Tried and slower: 128 x 256 tiles,
 // two workgroups a CU (522); stages of 32 i, four deep (455-482); two groups of waves
 // a barrier apart, one reading while the other multiplies (446).
-// 16384 x 1024 -> 4096 in 8 even groups 122 us (1.12 PFLOP/s), in ragged ones 142-163:
+// 16384 x 1024 -> 4096 in 8 even groups 123 us (1.12 PFLOP/s), in ragged ones 142-163:
 // the last round of tiles is then nearly empty, and bound by latency (halving its
 // tiles changed nothing).
 constexpr int kStage = 2 * kBig * 8 * 16;   // bytes of one step's two operands in LDS
@@ -866,7 +866,9 @@ template <typename O> __global__ __launch_bounds__(256) void k_join(GroupedProdu
 // forward 24, 26 and 31 (128 tiles of 16 steps), gradient 73, 74 and 78 (32 tiles of 64
 // steps).  Where rows are not 4-byte aligned a tile takes 2.2 times as long (16384 x
 // 1023 -> 4095 in 8 groups 317 us), and these kernels read at 1.0 and 2.7 TB/s (176 rows
-// a group of 32 x 1023 x 1365: 325 and 122 us).
+// a group of 32 x 1023 x 1365: 325 and 122 us).  Left out: the bytes of big tiles (1024
+// groups of 256 x 64 -> 256 take 87 us, of which this counts 15) and uneven groups, whose
+// average stands for all.
 template <Direction D> bool few_rows(const GroupedProduct &a, bool big) {
     const double some = (double)a.rows / a.groups, live = a.groups * (1 - __builtin_exp(-some));
     const double reads = 2.0 * live * a.n * a.k * (some < 16 ? 1 : 0.75 + some / 64);

@@ -87,7 +87,7 @@ template <typename T> __device__ __forceinline__ void zero_row(T *out, int64_t c
 }
 
 // One row a workgroup of WAVES waves, NV vectors a lane.  Bound by HBM: 16384 x 32768 in
-// bf16, loss and gradient, 380 us for 2.15 GB (5.7 TB/s).  Sixteen waves with sixteen
+// bf16, loss and gradient, 380-400 us for 2.15 GB (5.4-5.7 TB/s).  Sixteen waves with sixteen
 // vectors a lane (rows of 131072 in bf16) would leave one workgroup on a CU, which loads,
 // sums and stores by turns: 1608 us against 501 for k_loss_long.
 template <typename T, int NV, int WAVES, bool GRAD>
