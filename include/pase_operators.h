@@ -1,8 +1,9 @@
 /*
  * pase_operators.h - the layers of the computation graphs as operators on one
  * MI355X (gfx950): residual add + layer norm, matrix products grouped by
- * ragged row ranges (one range: a plain product), and the softmax loss over a
- * vocabulary, each with its backward pass.
+ * ragged row ranges (one range: a plain product), attention over ragged
+ * sequences, rotary positions, dropout with the residual's addition, and the
+ * softmax loss over a vocabulary, each with its backward pass.
  *
  * They run a vertex of a graph, or the shard of it that a configuration gives
  * one device, whatever sizes the split leaves; layer costs can be measured with
@@ -40,7 +41,8 @@ extern "C" {
 typedef enum { PASE_BF16 = 0, PASE_FP16 = 1, PASE_FP32 = 2 } pase_dtype;
 
 #define PASE_NORM_MAX_WIDTH 16384   /* columns of a layer norm */
-#define PASE_MAX_GROUPS 65536       /* groups of a grouped product */
+#define PASE_MAX_GROUPS 65536       /* groups of a grouped product, sequences of attention */
+#define PASE_ATTENTION_MAX_DIM 128  /* elements of a head of attention */
 
 /* Reason of this thread's last failed operator call ("" if none yet). */
 const char *pase_operator_error(void);
@@ -139,6 +141,79 @@ pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t 
                                              uint64_t ldl, const void *targets, int targets_64, int64_t ignore_index,
                                              const float *lse, const float *lse_low, const float *dloss,
                                              uint64_t dloss_stride, void *dlogits, uint64_t lddl, void *stream);
+
+/* Attention of ragged sequences: sequence b has the query rows q_offsets[b] ..
+ * q_offsets[b + 1] - 1 of q and, of the key rows k_offsets[b] .. k_offsets[b + 1] - 1, the
+ * first k_lengths[b] (k_lengths NULL: all).  With the scores s_ij = scale q_i . k_j of
+ * the keys j that query i sees (all of its sequence, or, causal, those up to i + keys -
+ * queries: the last query sees every key),
+ *     lse_i = log sum_j exp(s_ij),   out_i = sum_j exp(s_ij - lse_i) v_j
+ * for each head; heads is a multiple of kv_heads, and head h reads the keys and values
+ * of head h / (heads / kv_heads).  A query that sees no key, and a row of no sequence, has
+ * out 0 and lse -inf.
+ * dtype: PASE_BF16 or PASE_FP16, of all matrices.  q, out: [rows, heads, dim], k, v: [key_rows,
+ * kv_heads, dim], dim up to PASE_ATTENTION_MAX_DIM; ld* is the distance between
+ * rows, hs* between heads (16-byte aligned rows and heads, and a dim that is a multiple of 8, are
+ * faster).  lse: fp32 [heads, rows].  Offsets and lengths: device arrays of one type,
+ * int32 (offsets_64 = 0) or int64 (1), offsets not decreasing and within 0..rows, 0..key_rows, lengths
+ * within their ranges.  They are read on the device only and taken as the nearest
+ * that stay within; where offsets decrease, results are undefined.
+ * Keys and values past a sequence's length are not read.  Within it a value that is not
+ * finite may reach every query of its sequence, also past the causal limit.
+ * scale: positive.  Weights exp(s_ij - lse_i) are rounded to dtype before they
+ * multiply the values.  workspace: pase_attention_workspace() bytes, 16-byte
+ * aligned. */
+pase_status pase_attention_forward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                                   uint32_t kv_heads, uint32_t dim, const void *q, uint64_t ldq, uint64_t hsq,
+                                   const void *k, uint64_t ldk, uint64_t hsk, const void *v, uint64_t ldv, uint64_t hsv,
+                                   const void *q_offsets, const void *k_offsets, const void *k_lengths,
+                                   int offsets_64, int causal, float scale, void *out, uint64_t ldo, uint64_t hso,
+                                   float *lse, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace pase_attention_forward (backward = 0; 0 is possible) or
+ * pase_attention_backward (1) needs. */
+pase_status pase_attention_workspace(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                                     uint32_t kv_heads, uint32_t dim, int backward, uint64_t *bytes);
+
+/* Backward pass, from the out and lse of the forward pass: with p_ij = exp(s_ij - lse_i)
+ * and ds_ij = p_ij (dout_i . v_j - dout_i . out_i),
+ *     dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
+ * dk and dv summed over the heads that share them.  p and ds are recomputed, and
+ * rounded to dtype before the second products.  Rows of no sequence and keys past a length get 0.
+ * No output may be an input. */
+pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                                    uint32_t kv_heads, uint32_t dim, const void *dout, uint64_t lddo, uint64_t hsdo,
+                                    const void *q, uint64_t ldq, uint64_t hsq, const void *k, uint64_t ldk, uint64_t hsk,
+                                    const void *v, uint64_t ldv, uint64_t hsv, const void *out, uint64_t ldo,
+                                    uint64_t hso, const float *lse, const void *q_offsets, const void *k_offsets,
+                                    const void *k_lengths, int offsets_64, int causal, float scale, void *dq,
+                                    uint64_t lddq, uint64_t hsdq, void *dk, uint64_t lddk, uint64_t hsdk, void *dv,
+                                    uint64_t lddv, uint64_t hsdv, void *workspace, uint64_t workspace_bytes,
+                                    void *stream);
+
+/* Rotary positions: of each head of row t, pair i turns by the angle t_i =
+ * positions[t] * frequencies[i], times magnitude:
+ *     (a, b) -> magnitude (a cos t_i - b sin t_i, a sin t_i + b cos t_i).
+ * Pair i < turned / 2 is elements i and i + turned / 2, or (interleaved) 2 i and 2 i + 1; the
+ * elements from `turned` on (even, at most dim) are copied.  inverse = 1 turns the other way: the
+ * gradient of x from that of y.  x, y: [rows, heads, dim]; y may be x (same
+ * strides).  positions: device array [rows], int32 (positions_64 = 0) or int64 (1).
+ * frequencies: fp64 device array [turned / 2]; angles are formed in fp64. */
+pase_status pase_rotary(int dtype, uint64_t rows, uint32_t heads, uint32_t dim, uint32_t turned, int interleaved,
+                        int inverse, const void *x, uint64_t ldx, uint64_t hsx, const void *positions, int positions_64,
+                        const double *frequencies, float magnitude, void *y, uint64_t ldy, uint64_t hsy, void *stream);
+
+/* Dropout with the residual's addition: y = residual + keep * x / (1 - p'), where p' is p
+ * to the nearest multiple of 2^-16 and keep = 1 with probability 1 - p'.  Without a
+ * residual (NULL) it is also the backward pass: dx from dy, with the same p and seed.
+ * Element (row, column) is kept if its 16-bit number is at least 2^16 p': number column %
+ * 8 (low halves first) of the four words that Philox 4x32-10 gives for the counter (row
+ * * ceil(width / 8) + column / 8, seed[1]) and the key seed[0], low words first.  seed: two
+ * int64 in device memory, so that a captured call takes new numbers when they are
+ * changed.  No mask is stored.  A dropped element of x has no influence, whatever it
+ * is.  y may be x or residual (same ld). */
+pase_status pase_dropout(int dtype, uint64_t rows, uint64_t width, const void *x, uint64_t ldx, const void *residual,
+                         uint64_t ldr, double p, const int64_t *seed, void *y, uint64_t ldy, void *stream);
 
 #ifdef __cplusplus
 }

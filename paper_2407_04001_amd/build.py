@@ -20,7 +20,8 @@ HIP_FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC",
 # The search's keys are never NaN; the layer operators pass NaN on.
 SEARCH_FLAGS = ["-fno-honor-nans"]
 SEARCH = ("host.cpp", "launch_plan.cpp", "assign.cpp", "device.hip")
-OPERATORS = ("operators.cpp", "layer_norm.hip", "softmax_loss.hip", "grouped_matmul.hip")
+OPERATORS = ("operators.cpp", "layer_norm.hip", "softmax_loss.hip", "grouped_matmul.hip",
+             "attention.hip", "rotary.hip", "dropout.hip")
 
 
 def sources():

@@ -1,0 +1,724 @@
+// Attention over ragged sequences and its gradients (pase_operators.h).
+//
+// Scores stand in the matrix instruction's result with the query (forward, dq) or the
+// key (dk, dv) along the lanes: s^T = k q^T gives a lane one query and 16 of 32 keys, so
+// maxima and sums over keys stay in a lane but for one exchange with lane ^ 32, a
+// rescaling of the output is one factor a lane, and the weights are, rounded, the next
+// product's operand as they stand: o^T += v^T p^T contracts over keys, in the order that
+// the result registers hold them (keys 4 h + {0..3, 8..11} of 16 in half h of the wave),
+// which the transposing LDS reads of v follow.  p never leaves the registers.
+//
+// Exponents are powers of two, p = 2^(c s - c m) with c = scale log2 e, one fused
+// multiply-add each.
+#include <cfloat>
+
+#include "lds.h"
+#include "operators.h"
+#include "vectors.h"
+
+namespace pase {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+template <typename T> struct Mfma;
+template <> struct Mfma<__bf16> {
+    typedef __bf16 Frag __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x16 go(Frag a, Frag b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<_Float16> {
+    typedef _Float16 Frag __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x16 go(Frag a, Frag b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The lane's partner with the same query (or key): the other half of the wave.
+__device__ __forceinline__ float other_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float other_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// ---------------------------------------------------------------- which rows a workgroup has
+__device__ __forceinline__ int clamped(const void *p, int wide, int i, int lo, int hi) {
+    const int64_t o = wide ? static_cast<const int64_t *>(p)[i] : (int64_t) static_cast<const int32_t *>(p)[i];
+    return o < lo ? lo : o > hi ? hi : (int)o;
+}
+
+// Range v of sequences + 2: the rows before offsets[0], each sequence's, those from
+// offsets[sequences] on.
+struct Range {
+    int lo, hi;
+    __device__ __forceinline__ Range(const void *offsets, int wide, int sequences, int rows, int v) {
+        lo = v == 0 ? 0 : clamped(offsets, wide, v - 1, 0, rows);
+        hi = v > sequences ? rows : clamped(offsets, wide, v, lo, rows);
+    }
+};
+
+// Tiles of `size` of a range's rows x group: range v owns those from start(v) * group /
+// size + v up to its successor's, as many as it needs or one more.  Which range a tile
+// is of follows by a search with 64 probes a step, without a pass over all offsets.
+// Offsets that break their rule give some range: whatever it is, rows stay within it.
+struct Owner {
+    int v, first;   // the range, and its first tile
+
+    __device__ __forceinline__ Owner(const void *offsets, int wide, int sequences, int rows, int group, int size, int tile) {
+        const int lane = threadIdx.x & 63;
+        int lo = 0, n = sequences + 2;
+        while (n > 1) {
+            const int step = (n + 63) >> 6, at = lane * step, mine = lo + at;
+            const bool before = at < n && begin(offsets, wide, rows, group, size, mine) <= tile;
+            const int found = __builtin_popcountll(__ballot(before));
+            const int skip = (found > 1 ? found - 1 : 0) * step;
+            lo += skip;
+            n = n - skip < step ? n - skip : step;
+        }
+        v = uniform(lo);
+        first = uniform(begin(offsets, wide, rows, group, size, lo));
+    }
+    static __device__ __forceinline__ int begin(const void *offsets, int wide, int rows, int group, int size, int v) {
+        return (v == 0 ? 0 : clamped(offsets, wide, v - 1, 0, rows)) * group / size + v;
+    }
+};
+
+// What a tile of the queries sees, or a tile of the keys is seen by.
+struct Sequence {
+    int q_lo, q_rows, k_lo, k_rows, keys;   // keys: the first of k_rows that count
+    __device__ __forceinline__ Sequence(const Attention &a, int v) {
+        const Range q(a.q_offsets, a.offsets_64, a.sequences, a.rows, v), k(a.k_offsets, a.offsets_64, a.sequences, a.key_rows, v);
+        q_lo = uniform(q.lo), q_rows = uniform(q.hi - q.lo), k_lo = uniform(k.lo), k_rows = uniform(k.hi - k.lo);
+        keys = v < 1 || v > a.sequences ? 0 : k_rows;
+        if (a.k_lengths && keys) keys = uniform(clamped(a.k_lengths, a.offsets_64, v - 1, 0, k_rows));
+    }
+    // How many of the keys query i sees.
+    __device__ __forceinline__ int seen(const Attention &a, int i) const {
+        if (!a.causal) return keys;
+        const int n = i + keys - q_rows + 1;
+        return n < 0 ? 0 : n > keys ? keys : n;
+    }
+};
+
+// ---------------------------------------------------------------- tiles in LDS
+// A row of D elements is D / 8 chunks of 16 bytes; chunk c of row r stands at place
+// c ^ fold(r) of its row.  Sixteen rows' reads of one chunk, and the four rows x four
+// chunks of a transposing read, then reach different banks.
+template <int D> __device__ __forceinline__ int fold(int r) {
+    if (D == 128) return (r & 3) << 2 | (r >> 2 & 3);
+    if (D == 64) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+    return r >> 2 & 3;
+}
+
+// Loads ROWS rows of a head, D elements of each (0 past `dim` and past the rows that
+// exist), by WAVES waves: from HBM to LDS without registers where rows are 4-byte aligned
+// and dim a multiple of 8 (DIRECT; the buffer's range ends with the last row), else
+// through them.
+template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
+    static constexpr int kChunks = D / 8, N = ROWS * kChunks / (64 * WAVES);
+    static_assert(N >= 1 && ROWS * kChunks == N * 64 * WAVES, "whole loads");
+    int at[DIRECT ? N : 1];
+    Pack<T> r[DIRECT ? 1 : N];
+    int64_t ld;
+    int dim, wave;
+
+    __device__ __forceinline__ Feed(int64_t ld_, int dim_) : ld(ld_), dim(dim_) {
+        wave = uniform(threadIdx.x >> 6);
+        if (DIRECT)
+#pragma unroll
+            for (int n = 0; n < N; n++) {
+                const int q = chunk(n), row = q / kChunks, c = q % kChunks ^ fold<D>(row);
+                at[n] = c * 8 < dim ? row * (int)ld * 2 + c * 16 : 0x7fffff00;   // past every range
+            }
+    }
+    __device__ __forceinline__ int chunk(int n) const { return (n * WAVES + wave) * 64 + (threadIdx.x & 63); }
+
+    __device__ __forceinline__ void load(const T *p, int rows, const char *lds) {
+        if (DIRECT) {
+            rows = rows > ROWS ? ROWS : rows;
+            const u32x4 range = buffer_of(p, rows > 0 ? ((rows - 1) * (int)ld + dim) * 2 : 0);
+            const uint32_t dst = lds_address(lds) + wave * 1024;
+#pragma unroll
+            for (int n = 0; n < N; n++) load_to_lds(range, at[n], dst + n * WAVES * 1024);
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; n++) {
+                const int q = chunk(n), row = q / kChunks, c = q % kChunks ^ fold<D>(row);
+                r[n] = load_pack(p + row * ld + c * 8, row < rows ? dim - c * 8 : 0, (T)0.0f);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char *lds) {
+        if (!DIRECT)
+#pragma unroll
+            for (int n = 0; n < N; n++) reinterpret_cast<Pack<T> *>(lds)[chunk(n)] = r[n];
+    }
+};
+
+// The loads of a tile have arrived, and every wave is past its reads of the one before.
+template <bool DIRECT> __device__ __forceinline__ void arrive() {
+    if (DIRECT) {
+        wait_loads<0>();
+        barrier();
+    } else {
+        __syncthreads();
+    }
+}
+
+// Operand reads of a tile.  Along: row r0 + lane % 32, elements 16 s + 8 h of it.
+// Across: column 32 d + lane % 32, rows 16 g + 4 h + {0..3, 8..11} of the 16.
+template <typename T, int D> struct Reader {
+    typedef typename Mfma<T>::Frag Frag;
+    uint32_t along, across;   // byte places within a tile
+
+    __device__ __forceinline__ Reader() {
+        const int lane = threadIdx.x & 63, h = lane >> 5, l = lane & 15;
+        along = ((lane & 31) * (D / 8) + (h ^ fold<D>(lane & 31))) * 16;
+        const int row = 4 * h + (l >> 2), c = (lane >> 4 & 1) * 2 + (l >> 1 & 1);
+        across = (row * (D / 8) + (c ^ fold<D>(row))) * 16 + (l & 1) * 8;
+    }
+    __device__ __forceinline__ Frag row(uint32_t tile, int r0, int s) const {
+        return *(__attribute__((address_space(3))) const Frag *)(uintptr_t)(tile + r0 * D * 2 + (along ^ s * 32));
+    }
+    __device__ __forceinline__ Frag column(uint32_t tile, int g, int d) const {
+        union {
+            Frag f;
+            s16x4 half[2];
+        } u;
+        const uint32_t at = across ^ d * 64;
+        u.half[0] = read_across(tile + g * 16 * D * 2 + at);
+        u.half[1] = read_across(tile + (g * 16 + 8) * D * 2 + (at ^ 32));
+        return u.f;
+    }
+};
+
+// Operand registers of the lane's own row: 16 s + 8 h on, for the D / 16 s; 0 past `n`.
+template <typename T, int D>
+__device__ __forceinline__ void load_row(typename Mfma<T>::Frag (&f)[D / 16], const T *p, int n) {
+    const int h = threadIdx.x >> 5 & 1;
+#pragma unroll
+    for (int s = 0; s < D / 16; s++) {
+        const Pack<T> r = load_pack(p + 16 * s + 8 * h, n - 16 * s - 8 * h, (T)0.0f);
+        f[s] = __builtin_bit_cast(typename Mfma<T>::Frag, r.v);
+    }
+}
+
+// Eight consecutive registers of a result as an operand.
+template <typename T> __device__ __forceinline__ typename Mfma<T>::Frag narrow(const f32x16 &v, int from) {
+    typename Mfma<T>::Frag f;
+#pragma unroll
+    for (int j = 0; j < 8; j++) f[j] = (T)v[from + j];
+    return f;
+}
+
+// Stores a wave's 32 rows (lane % 32 its row, element 32 d + 8 i + 4 h + j in register 4 i + j
+// of v[d]), times `factor`, or 0 where it has `none`, rounded once.  They pass LDS (32 D elements of the wave's own),
+// so that whole rows are written 16 bytes a lane.  at(row): where a row goes, or null.
+template <typename T, int D, typename F>
+__device__ __forceinline__ void store_rows(char *lds, const f32x16 (&v)[D / 32], bool none, float factor, int dim, F at) {
+    constexpr int kChunks = D / 8;
+    const int lane = threadIdx.x & 63, h = lane >> 5, row = lane & 31;
+#pragma unroll
+    for (int d = 0; d < D / 32; d++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            union {
+                T e[4];
+                uint64_t u;
+            } o;
+#pragma unroll
+            for (int j = 0; j < 4; j++) o.e[j] = none ? (T)0.0f : (T)(v[d][4 * i + j] * factor);
+            *reinterpret_cast<uint64_t *>(lds + (row * kChunks + ((d * 4 + i) ^ fold<D>(row))) * 16 + h * 8) = o.u;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int n = 0; n < 32 * kChunks / 64; n++) {
+        const int q = n * 64 + lane, r = q / kChunks, c = q % kChunks;
+        const Pack<T> o = reinterpret_cast<const Pack<T> *>(lds)[r * kChunks + (c ^ fold<D>(r))];
+        T *p = at(r);
+        if (p && c * 8 < dim) store_pack(p + c * 8, dim - c * 8, o);
+    }
+}
+
+template <typename T> __device__ __forceinline__ const T *head_of(const HeadRows &x, int64_t row, int64_t head) {
+    return static_cast<const T *>(x.p) + row * x.ld + head * x.head_ld;
+}
+template <typename T> __device__ __forceinline__ T *out_of(const HeadRows &x, int64_t row, int64_t head) {
+    return static_cast<T *>(x.p) + row * x.ld + head * x.head_ld;
+}
+
+// The queries of a tile: a range's rows x the heads that share one of keys and values,
+// the heads of a row next to each other, so that these heads share the keys' tiles and
+// single tokens fill more of a tile.
+struct Queries {
+    int group, head0, rows, first;   // rows x group there are; the tile's first
+
+    __device__ __forceinline__ bool has(int p) const { return first + p < rows; }
+    __device__ __forceinline__ int index(int p) const { return (first + p) / group; }
+    __device__ __forceinline__ int head(int p) const { return head0 + (first + p) % group; }
+};
+
+// Rows and heads of one share's log-sum-exps in a.partial, which its outputs follow.
+__device__ __forceinline__ int64_t part_rows(const Attention &a) { return ((int64_t)a.rows * a.heads + 3) & ~3ll; }
+
+// ---------------------------------------------------------------- forward
+// WAVES x 32 queries a workgroup, KT keys a step, keys and values two steps deep in LDS.
+// SPLIT: the tile's keys are dealt to a.splits workgroups, each of which leaves its share's
+// output and log-sum-exp for k_join.
+template <typename T, int D, int WAVES, int KT, bool DIRECT, bool SPLIT>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void k_forward(Attention a) {
+    typedef typename Mfma<T>::Frag Frag;
+    constexpr int BM = WAVES * 32, kTile = KT * D * 2;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
+    static_assert(2 * 2 * kTile >= BM * D * 2, "the output passes the same LDS");
+    const uint32_t block = a.first + blockIdx.x, item = SPLIT ? block / a.splits : block;
+    const int part = SPLIT ? (int)(block - item * a.splits) : 0;
+    // heads next to each other, so that an XCD's workgroups share as few as may be; late tiles,
+    // which see the most keys, first
+    const int kv_head = (int)(item % a.kv_heads), tile = a.tiles - 1 - (int)(item / a.kv_heads);
+    const int group = a.heads / a.kv_heads;
+    const Owner own(a.q_offsets, a.offsets_64, a.sequences, a.rows, group, BM, tile);
+    const Sequence sq(a, own.v);
+    const Queries qs{group, kv_head * group, sq.q_rows * group, (tile - own.first) * BM};
+    if (tile < own.first || !qs.has(0)) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = wave * 32 + (lane & 31);
+    const bool there = qs.has(mine);
+    const int i = qs.index(mine), head = qs.head(mine);
+    Frag q[D / 16];
+    load_row<T, D>(q, head_of<T>(a.q, there ? sq.q_lo + i : 0, head), there ? a.dim : 0);
+
+    // keys that the wave's first and last query, and the tile's last, see
+    const int last = qs.rows - 1 - qs.first < BM - 1 ? qs.rows - 1 - qs.first : BM - 1;
+    const int w_last = wave * 32 + 31 < last ? wave * 32 + 31 : last;
+    const bool busy = wave * 32 <= last;
+    const int seen = sq.seen(a, i);
+    const int all_see = busy ? uniform(sq.seen(a, qs.index(wave * 32))) : 0;
+    const int any_sees = busy ? uniform(sq.seen(a, qs.index(w_last))) : 0;
+    const int end = uniform(sq.seen(a, qs.index(last)));
+    int t0 = 0, t1 = (end + KT - 1) / KT;
+    if (SPLIT) {
+        const int64_t n = t1;
+        t0 = (int)(n * part / a.splits), t1 = (int)(n * (part + 1) / a.splits);
+    }
+
+    const float c = a.scale * kLog2e;
+    f32x16 o[D / 32] = {};
+    float m = -__builtin_inff(), sum = 0;   // sum: of this lane's keys
+    Feed<T, D, KT, WAVES, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
+    const Reader<T, D> read;
+    const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
+    const auto load = [&](int t, char *to) {
+        fk.load(k + (int64_t)t * KT * a.k.ld, sq.keys - t * KT, to);
+        fv.load(v + (int64_t)t * KT * a.v.ld, sq.keys - t * KT, to + kTile);
+    };
+    const auto store = [&](char *to) { fk.store(to), fv.store(to + kTile); };
+    if (t0 < t1) load(t0, lds[0]), store(lds[0]);
+    for (int t = t0; t < t1; t++) {
+        const int at = (t - t0) & 1;
+        arrive<DIRECT>();
+        if (t + 1 < t1) load(t + 1, lds[at ^ 1]);
+        if (t * KT < any_sees) {
+            const uint32_t kt = lds_address(lds[at]), vt = kt + kTile;
+            f32x16 s[KT / 32];
+#pragma unroll
+            for (int b = 0; b < KT / 32; b++) {
+                s[b] = 0.0f;
+#pragma unroll
+                for (int d = 0; d < D / 16; d++) s[b] = Mfma<T>::go(read.row(kt, b * 32, d), q[d], s[b]);
+            }
+            if ((t + 1) * KT > all_see) {
+#pragma unroll
+                for (int b = 0; b < KT / 32; b++)
+#pragma unroll
+                    for (int j = 0; j < 16; j++)
+                        if (t * KT + b * 32 + 8 * (j / 4) + 4 * h + j % 4 >= seen) s[b][j] = -__builtin_inff();
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int b = 0; b < KT / 32; b++)
+#pragma unroll
+                for (int j = 0; j < 16; j++) top = fmaxf(top, s[b][j]);
+            top = other_max(top);
+            // The exponents' reference moves only when it is over 8 too low: weights stay below 2^8,
+            // exact in either type's range, and the outputs are seldom rescaled.
+            if (__any((top - m) * c > 8)) {
+                const float now = fmaxf(m, top), f = now == m ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
+                m = now;
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < D / 32; d++) o[d] *= f;
+            }
+            const float from = m == -__builtin_inff() ? 0.0f : m * c;
+#pragma unroll
+            for (int b = 0; b < KT / 32; b++)
+#pragma unroll
+                for (int j = 0; j < 16; j++) {
+                    s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], c, -from));
+                    sum += s[b][j];
+                }
+            // weights are rounded to the values' type: 2^-9 (bf16) of each, unbiased
+#pragma unroll
+            for (int g = 0; g < KT / 16; g++) {
+                const Frag p = narrow<T>(s[g / 2], g % 2 * 8);
+#pragma unroll
+                for (int d = 0; d < D / 32; d++) o[d] = Mfma<T>::go(read.column(vt, g, d), p, o[d]);
+            }
+        }
+        if (t + 1 < t1) store(lds[at ^ 1]);
+    }
+    sum = other_sum(sum);
+    const float lse = sum == 0 ? -__builtin_inff() : (m * c + __builtin_amdgcn_logf(sum)) * kLn2;   // sum >= 1 or nothing was seen
+    const float inverse = sum == 0 ? 0.0f : 1.0f / sum;
+    if (SPLIT) {
+        if (!there) return;
+        const int64_t at = (int64_t)(sq.q_lo + i) * a.heads + head, all = part_rows(a);
+        if (h == 0) a.partial[part * all + at] = lse;
+        if (sum == 0) return;   // not read
+        const int width = (a.dim + 3) & ~3;
+        float *out = a.partial + a.splits * all + (part * all + at) * width + 4 * h;
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                Pack<float> r;
+#pragma unroll
+                for (int j = 0; j < 4; j++) r.e[j] = o[d][4 * e + j] * inverse;
+                if (32 * d + 8 * e + 4 * h < width) *reinterpret_cast<u32x4 *>(out + 32 * d + 8 * e) = r.v;
+            }
+        return;
+    }
+    if (there && h == 0) a.lse[(int64_t)head * a.rows + sq.q_lo + i] = lse;
+    __syncthreads();
+    store_rows<T, D>(lds[0] + wave * 32 * D * 2, o, sum == 0, inverse, a.dim, [&](int r) -> T * {
+        const int p = wave * 32 + r;
+        return qs.has(p) ? out_of<T>(a.out, sq.q_lo + qs.index(p), qs.head(p)) : nullptr;
+    });
+}
+
+// Joins the shares of one row and head: weights exp(lse_p - lse).  A wave's half takes
+// every eighth share, its 32 lanes four elements each.
+template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a) {
+    __shared__ float lds[2][256];
+    __shared__ Pack<float> sums[8][32];
+    const int64_t at = (int64_t)a.first + blockIdx.x, all = part_rows(a);
+    const int lane = threadIdx.x & 31, part0 = threadIdx.x >> 5, width = (a.dim + 3) & ~3;
+    float m = -__builtin_inff(), total[1] = {0};
+    for (int p = threadIdx.x; p < a.splits; p += 256) m = fmaxf(m, a.partial[p * all + at]);
+    m = group_max<4>(m, lds[0]);
+    const float from = m == -__builtin_inff() ? 0.0f : m;
+    for (int p = threadIdx.x; p < a.splits; p += 256) total[0] += __expf(a.partial[p * all + at] - from);
+    group_sum<4>(total, lds[1]);
+    Pack<float> sum;
+    sum.v = 0;
+    if (lane * 4 < width)
+        for (int p = part0; p < a.splits; p += 8) {
+            const float lse = a.partial[p * all + at];
+            if (lse == -__builtin_inff()) continue;   // nothing was seen there, or written
+            const float w = __expf(lse - from);
+            const Pack<float> o = load_pack(a.partial + a.splits * all + (p * all + at) * width + lane * 4, 4, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 4; j++) sum.e[j] += w * o.e[j];
+        }
+    sums[part0][lane] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    for (int p = 1; p < 8; p++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum.e[j] += sums[p][lane].e[j];
+    const int64_t row = at / a.heads, head = at % a.heads;
+    const float inverse = total[0] == 0 ? 0.0f : 1.0f / total[0];
+    T *out = out_of<T>(a.out, row, head) + lane * 4;
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+        if (lane * 4 + j < a.dim) out[j] = (T)(sum.e[j] * inverse);
+    if (lane == 0) a.lse[head * a.rows + row] = total[0] == 0 ? -__builtin_inff() : m + logf(total[0]);
+}
+
+// ---------------------------------------------------------------- backward
+// p = exp(s - lse), ds = p (dp - delta) with dp = v . dout and delta = out . dout.  Two
+// kernels, each with its own outputs in registers: dq over the keys, which also leaves
+// delta, and dk and dv over the queries.  Scores and dp are formed in both (seven
+// products where one kernel with atomics would take five): sums have a fixed order.
+// p and ds are rounded to the operands' type before their second products.
+
+__device__ __forceinline__ float exponent_of(float lse) {   // rows without keys: p = 0
+    return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+}
+
+// Queries along the lanes, as in the forward pass.
+template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(256, 1) void k_queries_grad(Attention a) {
+    typedef typename Mfma<T>::Frag Frag;
+    constexpr int WAVES = 4, BM = 128, kTile = KT * D * 2;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
+    static_assert(2 * 2 * kTile >= BM * D * 2, "the gradient passes the same LDS");
+    const uint32_t item = a.first + blockIdx.x;
+    const int kv_head = (int)(item % a.kv_heads), tile = a.tiles - 1 - (int)(item / a.kv_heads);
+    const int group = a.heads / a.kv_heads;
+    const Owner own(a.q_offsets, a.offsets_64, a.sequences, a.rows, group, BM, tile);
+    const Sequence sq(a, own.v);
+    const Queries qs{group, kv_head * group, sq.q_rows * group, (tile - own.first) * BM};
+    if (tile < own.first || !qs.has(0)) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = wave * 32 + (lane & 31);
+    const bool there = qs.has(mine);
+    const int i = qs.index(mine), head = qs.head(mine), row = there ? sq.q_lo + i : 0, width = there ? a.dim : 0;
+    Frag q[D / 16], g[D / 16];
+    load_row<T, D>(q, head_of<T>(a.q, row, head), width);
+    load_row<T, D>(g, head_of<T>(a.dout, row, head), width);
+    float delta = 0, lse2 = __builtin_inff();
+    {
+        Frag out[D / 16];
+        load_row<T, D>(out, head_of<T>(a.out, row, head), width);
+#pragma unroll
+        for (int d = 0; d < D / 16; d++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) delta += (float)g[d][j] * (float)out[d][j];
+        delta = other_sum(delta);
+        if (there) {
+            const int64_t at = (int64_t)head * a.rows + row;
+            lse2 = exponent_of(a.lse[at]);
+            if (h == 0) a.delta[at] = delta;
+        }
+    }
+    const int last = qs.rows - 1 - qs.first < BM - 1 ? qs.rows - 1 - qs.first : BM - 1;
+    const int w_last = wave * 32 + 31 < last ? wave * 32 + 31 : last;
+    const bool busy = wave * 32 <= last;
+    const int seen = sq.seen(a, i);
+    const int all_see = busy ? uniform(sq.seen(a, qs.index(wave * 32))) : 0;
+    const int any_sees = busy ? uniform(sq.seen(a, qs.index(w_last))) : 0;
+    const int tiles = (uniform(sq.seen(a, qs.index(last))) + KT - 1) / KT;
+
+    const float c = a.scale * kLog2e;
+    f32x16 dq[D / 32] = {};
+    Feed<T, D, KT, WAVES, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
+    const Reader<T, D> read;
+    const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
+    const auto load = [&](int t, char *to) {
+        fk.load(k + (int64_t)t * KT * a.k.ld, sq.keys - t * KT, to);
+        fv.load(v + (int64_t)t * KT * a.v.ld, sq.keys - t * KT, to + kTile);
+    };
+    const auto store = [&](char *to) { fk.store(to), fv.store(to + kTile); };
+    if (tiles) load(0, lds[0]), store(lds[0]);
+    for (int t = 0; t < tiles; t++) {
+        const int at = t & 1;
+        arrive<DIRECT>();
+        if (t + 1 < tiles) load(t + 1, lds[at ^ 1]);
+        if (t * KT < any_sees) {
+            const uint32_t kt = lds_address(lds[at]), vt = kt + kTile;
+            const bool whole = (t + 1) * KT <= all_see;
+#pragma unroll
+            for (int b = 0; b < KT / 32; b++) {
+                f32x16 s = 0.0f, dp = 0.0f;
+#pragma unroll
+                for (int d = 0; d < D / 16; d++) {
+                    s = Mfma<T>::go(read.row(kt, b * 32, d), q[d], s);
+                    dp = Mfma<T>::go(read.row(vt, b * 32, d), g[d], dp);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; j++) s[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], c, -lse2)) * (dp[j] - delta);
+                if (!whole) {
+#pragma unroll
+                    for (int j = 0; j < 16; j++)
+                        if (t * KT + b * 32 + 8 * (j / 4) + 4 * h + j % 4 >= seen) s[j] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const Frag ds = narrow<T>(s, e * 8);
+#pragma unroll
+                    for (int d = 0; d < D / 32; d++) dq[d] = Mfma<T>::go(read.column(kt, b * 2 + e, d), ds, dq[d]);
+                }
+            }
+        }
+        if (t + 1 < tiles) store(lds[at ^ 1]);
+    }
+    __syncthreads();
+    store_rows<T, D>(lds[0] + wave * 32 * D * 2, dq, lse2 == __builtin_inff(), a.scale, a.dim, [&](int r) -> T * {
+        const int p = wave * 32 + r;
+        return qs.has(p) ? out_of<T>(a.dq, sq.q_lo + qs.index(p), qs.head(p)) : nullptr;
+    });
+}
+
+// Keys along the lanes: s = q k^T and dp = dout v^T give a lane one key and 16 of 32
+// queries; dv^T += dout^T p and dk^T += q^T ds.  The heads that share the keys come one
+// after the other.
+template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(256, 1) void k_keys_grad(Attention a) {
+    typedef typename Mfma<T>::Frag Frag;
+    constexpr int WAVES = 4, BM = 128, kTile = QT * D * 2;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
+    __shared__ __attribute__((aligned(16))) float stats[2][2][QT];
+    static_assert(2 * 2 * kTile >= BM * D * 2, "the gradients pass the same LDS");
+    const uint32_t item = a.first + blockIdx.x;
+    // early tiles, which the most queries see, first
+    const int kv_head = (int)(item % a.kv_heads), tile = (int)(item / a.kv_heads);
+    const int group = a.heads / a.kv_heads;
+    const Owner own(a.k_offsets, a.offsets_64, a.sequences, a.key_rows, 1, BM, tile);
+    const Sequence sq(a, own.v);
+    const int first = (tile - own.first) * BM;
+    if (first < 0 || first >= sq.k_rows) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
+    const int key = first + wave * 32 + (lane & 31);
+    const bool there = key < sq.keys;
+    const int64_t row = sq.k_lo + (there ? key : 0);
+    Frag k[D / 16], v[D / 16];
+    load_row<T, D>(k, head_of<T>(a.k, row, kv_head), there ? a.dim : 0);
+    load_row<T, D>(v, head_of<T>(a.v, row, kv_head), there ? a.dim : 0);
+    f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+
+    const float c = a.scale * kLog2e;
+    const int shift = a.causal ? sq.keys - sq.q_rows : 1 << 30;   // query i sees keys up to i + shift
+    const int from = first - shift < 0 ? 0 : first - shift;
+    const int t0 = from / QT, per = first < sq.keys && from < sq.q_rows ? (sq.q_rows + QT - 1) / QT - t0 : 0;
+    const int steps = per * group;
+    Feed<T, D, QT, WAVES, DIRECT> fq(a.q.ld, a.dim), fg(a.dout.ld, a.dim);
+    const Reader<T, D> read;
+    float stat = 0;
+    int next_head = kv_head * group, next = t0;   // what is loaded next
+    const auto load = [&](char *to) {
+        const int r0 = next * QT, left = sq.q_rows - r0;
+        if (threadIdx.x < 2 * QT) {
+            const int r = threadIdx.x % QT;
+            const float *of = threadIdx.x < QT ? a.lse : a.delta;
+            stat = r < left ? of[(int64_t)next_head * a.rows + sq.q_lo + r0 + r] : threadIdx.x < QT ? -__builtin_inff() : 0.0f;
+        }
+        fq.load(head_of<T>(a.q, sq.q_lo + r0, next_head), left, to);
+        fg.load(head_of<T>(a.dout, sq.q_lo + r0, next_head), left, to + kTile);
+        if (++next == t0 + per) next = t0, next_head++;
+    };
+    const auto store = [&](char *to, float *st) {
+        if (threadIdx.x < 2 * QT) st[threadIdx.x] = threadIdx.x < QT ? exponent_of(stat) : stat;
+        fq.store(to), fg.store(to + kTile);
+    };
+    if (steps) load(lds[0]), store(lds[0], stats[0][0]);
+    int t = t0;
+    for (int n = 0; n < steps; n++) {
+        const int at = n & 1;
+        arrive<DIRECT>();
+        if (n + 1 < steps) load(lds[at ^ 1]);
+        const int limit = key - shift - t * QT;   // the tile's queries below it do not see the key
+        if (t * QT + QT - 1 + shift >= first + wave * 32) {
+            const uint32_t qt = lds_address(lds[at]), gt = qt + kTile;
+            const bool whole = t * QT + shift >= first + wave * 32 + 31;
+#pragma unroll
+            for (int b = 0; b < QT / 32; b++) {
+                f32x16 s = 0.0f, dp = 0.0f;
+#pragma unroll
+                for (int d = 0; d < D / 16; d++) {
+                    s = Mfma<T>::go(read.row(qt, b * 32, d), k[d], s);
+                    dp = Mfma<T>::go(read.row(gt, b * 32, d), v[d], dp);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const Pack<float> lse2 = *reinterpret_cast<const Pack<float> *>(&stats[at][0][b * 32 + 8 * e + 4 * h]);
+                    const Pack<float> delta = *reinterpret_cast<const Pack<float> *>(&stats[at][1][b * 32 + 8 * e + 4 * h]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        s[4 * e + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * e + j], c, -lse2.e[j]));
+                        dp[4 * e + j] = s[4 * e + j] * (dp[4 * e + j] - delta.e[j]);
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int j = 0; j < 16; j++)
+                        if (b * 32 + 8 * (j / 4) + 4 * h + j % 4 < limit) s[j] = dp[j] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const Frag p = narrow<T>(s, e * 8), ds = narrow<T>(dp, e * 8);
+#pragma unroll
+                    for (int d = 0; d < D / 32; d++) {
+                        dv[d] = Mfma<T>::go(read.column(gt, b * 2 + e, d), p, dv[d]);
+                        dk[d] = Mfma<T>::go(read.column(qt, b * 2 + e, d), ds, dk[d]);
+                    }
+                }
+            }
+        }
+        if (n + 1 < steps) store(lds[at ^ 1], stats[at ^ 1][0]);
+        if (++t == t0 + per) t = t0;
+    }
+    // keys of the range that do not count get 0 (their lanes hold what a key of zeros would)
+    const int left = sq.k_rows - first - wave * 32;
+    char *mine = lds[0] + wave * 32 * D * 2;
+    __syncthreads();
+    store_rows<T, D>(mine, dv, !there, 1.0f, a.dim, [&](int r) -> T * {
+        return r < left ? out_of<T>(a.dv, sq.k_lo + first + wave * 32 + r, kv_head) : nullptr;
+    });
+    __builtin_amdgcn_wave_barrier();
+    store_rows<T, D>(mine, dk, !there, a.scale, a.dim, [&](int r) -> T * {
+        return r < left ? out_of<T>(a.dk, sq.k_lo + first + wave * 32 + r, kv_head) : nullptr;
+    });
+}
+
+// ---------------------------------------------------------------- launches
+// Tiles of `size` rows that the ranges of `rows` rows can need together.
+int64_t tiles_of(int64_t rows, int64_t size, int sequences) { return rows / size + sequences + 2; }
+
+// Launches a kernel that takes one item a workgroup, on as many items at a time as one launch holds.
+template <typename K> int launch_items(K *kernel, int64_t items, int threads, void *stream, Attention a) {
+    const int64_t most = most_blocks(threads);
+    for (int64_t at = 0; at < items; at += most) {
+        a.first = (uint32_t)at;
+        if (const int e = launch(kernel, items - at < most ? items - at : most, threads, stream, a)) return e;
+    }
+    return 0;
+}
+
+template <typename T> bool direct(const Attention &a, const HeadRows &x) {
+    return a.dim % 8 == 0 && reinterpret_cast<uintptr_t>(x.p) % 4 == 0 && x.ld % 2 == 0 && x.head_ld % 2 == 0;
+}
+
+template <typename T, int D, bool DIRECT> int forward(Attention a, void *stream) {
+    const int64_t packed = (int64_t)a.rows * (a.heads / a.kv_heads);
+    if (a.splits > 1) {
+        a.tiles = (int)tiles_of(packed, 32, a.sequences);
+        const int64_t items = (int64_t)a.tiles * a.kv_heads * a.splits;
+        if (const int e = launch_items(k_forward<T, D, 1, 32, DIRECT, true>, items, 64, stream, a)) return e;
+        return launch_items(k_join<T>, (int64_t)a.rows * a.heads, 256, stream, a);
+    }
+    a.tiles = (int)tiles_of(packed, 128, a.sequences);
+    return launch_items(k_forward<T, D, 4, 64, DIRECT, false>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
+}
+
+template <typename T, int D> int forward(const Attention &a, void *stream) {
+    return direct<T>(a, a.k) && direct<T>(a, a.v) ? forward<T, D, true>(a, stream) : forward<T, D, false>(a, stream);
+}
+
+template <typename T> int forward(const Attention &a, void *stream) {
+    if (a.dim <= 32) return forward<T, 32>(a, stream);
+    return a.dim <= 64 ? forward<T, 64>(a, stream) : forward<T, 128>(a, stream);
+}
+
+template <typename T, int D> int backward(Attention a, void *stream) {
+    const int64_t packed = (int64_t)a.rows * (a.heads / a.kv_heads);
+    a.tiles = (int)tiles_of(packed, 128, a.sequences);
+    const int64_t items = a.rows ? (int64_t)a.tiles * a.kv_heads : 0;
+    if (const int e = direct<T>(a, a.k) && direct<T>(a, a.v) ? launch_items(k_queries_grad<T, D, 64, true>, items, 256, stream, a)
+                                                             : launch_items(k_queries_grad<T, D, 64, false>, items, 256, stream, a))
+        return e;
+    a.tiles = (int)tiles_of(a.key_rows, 128, a.sequences);
+    const int64_t keys = a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0;
+    return direct<T>(a, a.q) && direct<T>(a, a.dout) ? launch_items(k_keys_grad<T, D, 64, true>, keys, 256, stream, a)
+                                                     : launch_items(k_keys_grad<T, D, 64, false>, keys, 256, stream, a);
+}
+
+template <typename T> int backward(const Attention &a, void *stream) {
+    if (a.dim <= 32) return backward<T, 32>(a, stream);
+    return a.dim <= 64 ? backward<T, 64>(a, stream) : backward<T, 128>(a, stream);
+}
+
+}  // namespace
+
+int launch_attention_forward(const Attention &a, void *stream) {
+    return a.dtype == PASE_BF16 ? forward<__bf16>(a, stream) : forward<_Float16>(a, stream);
+}
+int launch_attention_backward(const Attention &a, void *stream) {
+    return a.dtype == PASE_BF16 ? backward<__bf16>(a, stream) : backward<_Float16>(a, stream);
+}
+
+}  // namespace pase

@@ -26,6 +26,10 @@ int launch_softmax_loss_backward(const SoftmaxLoss &, void *) { return -1; }
 int launch_product_forward(const GroupedProduct &, void *) { return -1; }
 int launch_product_rows_grad(const GroupedProduct &, void *) { return -1; }
 int launch_product_weights_grad(const GroupedProduct &, void *) { return -1; }
+int launch_attention_forward(const Attention &, void *) { return -1; }
+int launch_attention_backward(const Attention &, void *) { return -1; }
+int launch_rotary(const Rotary &, void *) { return -1; }
+int launch_dropout(const Dropout &, void *) { return -1; }
 const char *launch_error(int) { return "host-only build: no device runtime"; }
 
 }  // namespace pase

@@ -12,6 +12,7 @@
 // rows of 64 i, one whose rows run along m or j ("across") as 64 rows of i; the
 // matrix instruction wants eight consecutive i a lane, which is a 16-byte LDS
 // read of the first and two transposing reads of the second.
+#include "lds.h"
 #include "operators.h"
 #include "vectors.h"
 
@@ -21,7 +22,6 @@ namespace {
 enum Direction { kForward, kRowsGrad, kWeights };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
@@ -381,19 +381,6 @@ template <typename T, typename O, Direction D> __global__ __launch_bounds__(256,
 // tiles changed nothing).
 constexpr int kStage = 2 * kBig * 8 * 16;   // bytes of one step's two operands in LDS
 
-__device__ __forceinline__ uint32_t lds_address(const void *p) {
-    return (uint32_t) reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)p);
-}
-
-// 16 bytes a lane from buffer r, byte offset `at`, to LDS byte dst + 16 * lane (dst
-// the same for the wave, through M0, which nothing else here uses).  The load has no register result; whoever reads the
-// LDS bytes waits for it by wait_loads().  The builtin of the same instruction
-// makes the compiler wait for every such load before each transposing LDS read,
-// a step too early: 16384 x 4096 x 4096 rows gradient 510 us with it, 436 without.
-__device__ __forceinline__ void load_to_lds(u32x4 r, int at, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(r) : "memory");
-}
-
 // One operand's loads: 4 of 16 bytes a lane and step, each 64 rows (along) or 16 i
 // (across) on from the one before.
 template <typename T, bool ACROSS, bool J> struct Feed {
@@ -441,20 +428,6 @@ template <typename T, bool ACROSS, bool J> struct Feed {
         for (int s = 0; s < 4; s++) issue(s);
     }
 };
-
-// All but the last N loads and stores of this wave have ended, and its LDS reads.
-template <int N> __device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
-}
-
-// A barrier alone: what it orders is waited for where it is needed.
-__device__ __forceinline__ void barrier() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 
 // The same fragments as frag(), by byte address: `at` is `base` plus the address
 // of the operand's stage.  One address register an operand, from which each

@@ -2,6 +2,8 @@
 // Nothing here touches the device; the launches are in the .hip files.
 #include "operators.h"
 
+#include <cfloat>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 
@@ -26,6 +28,8 @@ pase_status launched(int e) {
 constexpr uint64_t kMaxRows = 1ull << 40, kMaxLd = 1ull << 32;
 constexpr uint64_t kMaxProductDim = 1u << 20;     // n and k of a grouped product
 constexpr uint64_t kMaxProductLd = 1u << 22;      // 256 rows of a tile stay within 2^31 bytes
+constexpr uint64_t kMaxHeadStride = 1ull << 40;
+constexpr int kMaxShares = 256;                   // of a tile's keys
 constexpr uint64_t kMaxClasses = (1ull << 31) - 1024;
 
 int element_bytes(int dtype) { return dtype == PASE_FP32 ? 4 : 2; }
@@ -37,6 +41,12 @@ bool aligned(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) 
 #define REQUIRE(cond, ...) \
     do { \
         if (!(cond)) return refuse(PASE_ERR_INVALID_ARGUMENT, __VA_ARGS__); \
+    } while (0)
+
+#define CHECK(call) \
+    do { \
+        const pase_status st_ = (call); \
+        if (st_ != PASE_OK) return st_; \
     } while (0)
 
 // One matrix argument: there, aligned to its element, with rows that do not overlap.
@@ -115,12 +125,6 @@ uint64_t product_bytes(uint64_t rows, uint32_t groups, uint64_t n, uint64_t k) {
     return splits > 1 ? (uint64_t)splits * groups * n * k * sizeof(float) : 0;
 }
 
-#define CHECK(call) \
-    do { \
-        const pase_status st_ = (call); \
-        if (st_ != PASE_OK) return st_; \
-    } while (0)
-
 pase_status softmax_loss(int dtype, uint64_t rows, uint64_t classes, const void *logits, uint64_t ldl,
                          const void *targets, int targets_64, int64_t ignore_index, const float *dloss,
                          uint64_t dloss_stride, float *loss, float *lse, float *low, void *dlogits, uint64_t lddl,
@@ -175,6 +179,65 @@ pase_status softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, co
     return launched(launch_softmax_loss_backward(a, stream));
 }
 
+constexpr uint64_t kMaxAttentionRows = 1ull << 30;   // rows x the heads that share keys and values
+
+pase_status check_attention(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                            uint32_t kv_heads, uint32_t dim) {
+    REQUIRE(dtype == PASE_BF16 || dtype == PASE_FP16, "attention takes bf16 or fp16, not dtype %d", dtype);
+    REQUIRE(sequences >= 1, "no sequences");
+    REQUIRE(heads >= 1 && kv_heads >= 1, "no heads");
+    REQUIRE(heads % kv_heads == 0, "%u heads are no multiple of %u", heads, kv_heads);
+    REQUIRE(dim >= 1, "dim 0");
+    if (dim > PASE_ATTENTION_MAX_DIM) return refuse(PASE_ERR_TOO_LARGE, "dim %u above %d", dim, PASE_ATTENTION_MAX_DIM);
+    if (sequences > PASE_MAX_GROUPS)
+        return refuse(PASE_ERR_TOO_LARGE, "%u sequences, above %d", sequences, PASE_MAX_GROUPS);
+    if (heads > 65536) return refuse(PASE_ERR_TOO_LARGE, "%u heads, above 65536", heads);
+    if (rows > kMaxAttentionRows / heads || key_rows > kMaxAttentionRows / kv_heads)
+        return refuse(PASE_ERR_TOO_LARGE, "2^30 rows x heads or more");
+    // workgroups are counted in 32 bits
+    const uint64_t most = (rows > key_rows ? rows : key_rows) * (heads / kv_heads) / 32 + sequences + 2;
+    if (most * kv_heads > ((1ull << 31) - 1) / kMaxShares) return refuse(PASE_ERR_TOO_LARGE, "too many sequences x heads");
+    return PASE_OK;
+}
+
+pase_status check_sequences(const void *q_offsets, const void *k_offsets, const void *k_lengths, int offsets_64,
+                            int causal, float scale) {
+    CHECK(check_offsets(q_offsets, offsets_64));
+    CHECK(check_offsets(k_offsets, offsets_64));
+    REQUIRE(!k_lengths || aligned(k_lengths, offsets_64 ? 8 : 4), "k_lengths is not aligned to its element");
+    REQUIRE(causal == 0 || causal == 1, "causal is neither 0 nor 1");
+    REQUIRE(scale >= FLT_MIN && scale <= FLT_MAX, "scale is not a positive normal number");
+    return PASE_OK;
+}
+
+// One [rows, heads, dim] argument: there, aligned to its element, with rows and heads that do not overlap.
+#define REQUIRE_HEADS(p, ld, hs, rows, heads, dim, dtype) \
+    do { \
+        REQUIRE((p) != nullptr, #p " is null"); \
+        REQUIRE(aligned(p, element_bytes(dtype)), #p " is not aligned to its element"); \
+        CHECK(check_heads(#p, ld, hs, rows, heads, dim)); \
+    } while (0)
+
+pase_status check_heads(const char *name, uint64_t ld, uint64_t hs, uint64_t rows, uint64_t heads, uint64_t dim) {
+    REQUIRE(ld <= kMaxProductLd, "row stride of %s above 2^22", name);
+    REQUIRE(hs <= kMaxHeadStride, "head stride of %s too large", name);
+    // one of the two is the inner one: it holds dim, the other all of it
+    const bool rows_outside = heads == 1 || (hs >= dim && ld >= (heads - 1) * hs + dim);
+    const bool heads_outside = rows <= 1 || (ld >= dim && hs >= (rows - 1) * ld + dim);
+    REQUIRE((rows <= 1 || ld >= dim) && (heads == 1 || hs >= dim) && (rows <= 1 || heads == 1 || rows_outside || heads_outside),
+            "rows or heads of %s overlap", name);
+    return PASE_OK;
+}
+
+HeadRows head_rows(const void *p, uint64_t ld, uint64_t hs) { return {const_cast<void *>(p), (int64_t)ld, (int64_t)hs}; }
+
+uint64_t attention_bytes(uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads,
+                         uint32_t dim) {
+    const uint64_t splits = (uint64_t)attention_splits((int64_t)rows, (int64_t)key_rows, (int)sequences, (int)heads, (int)kv_heads);
+    const uint64_t all = (rows * heads + 3) & ~3ull;
+    return splits > 1 ? splits * all * (1 + ((dim + 3) & ~3u)) * sizeof(float) : 0;
+}
+
 }  // namespace
 
 int norm_backward_blocks(int dtype, int64_t rows, int width) {
@@ -189,6 +252,17 @@ int grouped_matmul_splits(int64_t rows, int groups, int n, int k) {
     const int64_t tiles = (int64_t)groups * ((n + kBig - 1) / kBig) * ((k + kBig - 1) / kBig);
     const int64_t idle = kCus / tiles, deep = rows / groups / 512, most = idle < deep ? idle : deep;
     return (int)(most < 1 ? 1 : most > 32 ? 32 : most);
+}
+
+// Shares of at least 128 keys, until four workgroups a CU have one, where the queries alone
+// make fewer.
+int attention_splits(int64_t rows, int64_t key_rows, int sequences, int heads, int kv_heads) {
+    const int64_t packed = rows * (heads / kv_heads), some = rows < sequences ? rows : sequences;
+    const int64_t large = (packed + 127) / 128, tiles = (large > some ? large : some) * kv_heads;
+    if (tiles <= 0 || tiles >= kCus) return 1;
+    const int64_t small = (packed + 31) / 32, items = (small > some ? small : some) * kv_heads;
+    const int64_t want = 4 * kCus / items, deep = key_rows / sequences / 128, most = want < deep ? want : deep;
+    return (int)(most < 1 ? 1 : most > kMaxShares ? kMaxShares : most);
 }
 
 }  // namespace pase
@@ -377,6 +451,135 @@ pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t 
     if (rows) REQUIRE(lse_low, "lse_low is null");
     return softmax_loss_backward(dtype, rows, classes, logits, ldl, targets, targets_64, ignore_index, lse, lse_low,
                                  dloss, dloss_stride, dlogits, lddl, stream);
+}
+
+pase_status pase_attention_forward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                                   uint32_t kv_heads, uint32_t dim, const void *q, uint64_t ldq, uint64_t hsq,
+                                   const void *k, uint64_t ldk, uint64_t hsk, const void *v, uint64_t ldv, uint64_t hsv,
+                                   const void *q_offsets, const void *k_offsets, const void *k_lengths,
+                                   int offsets_64, int causal, float scale, void *out, uint64_t ldo, uint64_t hso,
+                                   float *lse, void *workspace, uint64_t workspace_bytes, void *stream) {
+    CHECK(check_attention(dtype, rows, key_rows, sequences, heads, kv_heads, dim));
+    if (!rows) return PASE_OK;
+    REQUIRE_HEADS(q, ldq, hsq, rows, heads, dim, dtype);
+    if (key_rows) {
+        REQUIRE_HEADS(k, ldk, hsk, key_rows, kv_heads, dim, dtype);
+        REQUIRE_HEADS(v, ldv, hsv, key_rows, kv_heads, dim, dtype);
+    }
+    CHECK(check_sequences(q_offsets, k_offsets, k_lengths, offsets_64, causal, scale));
+    REQUIRE_HEADS(out, ldo, hso, rows, heads, dim, dtype);
+    REQUIRE(lse && aligned(lse, 4), "lse is null or not aligned to its element");
+    CHECK(check_workspace(workspace, workspace_bytes, attention_bytes(rows, key_rows, sequences, heads, kv_heads, dim)));
+    Attention a{};
+    a.dtype = dtype, a.offsets_64 = offsets_64, a.causal = causal;
+    a.rows = (int)rows, a.key_rows = (int)key_rows, a.sequences = (int)sequences;
+    a.heads = (int)heads, a.kv_heads = (int)kv_heads, a.dim = (int)dim, a.scale = scale;
+    a.q_offsets = q_offsets, a.k_offsets = k_offsets, a.k_lengths = k_lengths;
+    a.q = head_rows(q, ldq, hsq), a.k = head_rows(k, ldk, hsk), a.v = head_rows(v, ldv, hsv);
+    a.out = head_rows(out, ldo, hso), a.lse = lse;
+    a.splits = attention_splits(a.rows, a.key_rows, a.sequences, a.heads, a.kv_heads);
+    a.partial = a.splits > 1 ? static_cast<float *>(workspace) : nullptr;
+    return launched(launch_attention_forward(a, stream));
+}
+
+pase_status pase_attention_workspace(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                                     uint32_t kv_heads, uint32_t dim, int backward, uint64_t *bytes) {
+    REQUIRE(bytes, "bytes is null");
+    REQUIRE(backward == 0 || backward == 1, "backward is neither 0 nor 1");
+    CHECK(check_attention(dtype, rows, key_rows, sequences, heads, kv_heads, dim));
+    *bytes = backward ? rows * heads * sizeof(float) : attention_bytes(rows, key_rows, sequences, heads, kv_heads, dim);
+    return PASE_OK;
+}
+
+pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
+                                    uint32_t kv_heads, uint32_t dim, const void *dout, uint64_t lddo, uint64_t hsdo,
+                                    const void *q, uint64_t ldq, uint64_t hsq, const void *k, uint64_t ldk, uint64_t hsk,
+                                    const void *v, uint64_t ldv, uint64_t hsv, const void *out, uint64_t ldo,
+                                    uint64_t hso, const float *lse, const void *q_offsets, const void *k_offsets,
+                                    const void *k_lengths, int offsets_64, int causal, float scale, void *dq,
+                                    uint64_t lddq, uint64_t hsdq, void *dk, uint64_t lddk, uint64_t hsdk, void *dv,
+                                    uint64_t lddv, uint64_t hsdv, void *workspace, uint64_t workspace_bytes,
+                                    void *stream) {
+    CHECK(check_attention(dtype, rows, key_rows, sequences, heads, kv_heads, dim));
+    if (!rows && !key_rows) return PASE_OK;
+    CHECK(check_sequences(q_offsets, k_offsets, k_lengths, offsets_64, causal, scale));
+    if (rows) {
+        REQUIRE_HEADS(dout, lddo, hsdo, rows, heads, dim, dtype);
+        REQUIRE_HEADS(q, ldq, hsq, rows, heads, dim, dtype);
+        REQUIRE_HEADS(out, ldo, hso, rows, heads, dim, dtype);
+        REQUIRE(lse && aligned(lse, 4), "lse is null or not aligned to its element");
+        REQUIRE_HEADS(dq, lddq, hsdq, rows, heads, dim, dtype);
+        CHECK(check_workspace(workspace, workspace_bytes, rows * heads * sizeof(float)));
+    }
+    if (key_rows) {
+        REQUIRE_HEADS(k, ldk, hsk, key_rows, kv_heads, dim, dtype);
+        REQUIRE_HEADS(v, ldv, hsv, key_rows, kv_heads, dim, dtype);
+        REQUIRE_HEADS(dk, lddk, hsdk, key_rows, kv_heads, dim, dtype);
+        REQUIRE_HEADS(dv, lddv, hsdv, key_rows, kv_heads, dim, dtype);
+    }
+    Attention a{};
+    a.dtype = dtype, a.offsets_64 = offsets_64, a.causal = causal;
+    a.rows = (int)rows, a.key_rows = (int)key_rows, a.sequences = (int)sequences;
+    a.heads = (int)heads, a.kv_heads = (int)kv_heads, a.dim = (int)dim, a.scale = scale;
+    a.q_offsets = q_offsets, a.k_offsets = k_offsets, a.k_lengths = k_lengths;
+    a.q = head_rows(q, ldq, hsq), a.k = head_rows(k, ldk, hsk), a.v = head_rows(v, ldv, hsv);
+    a.out = head_rows(out, ldo, hso), a.dout = head_rows(dout, lddo, hsdo), a.lse = const_cast<float *>(lse);
+    a.dq = head_rows(dq, lddq, hsdq), a.dk = head_rows(dk, lddk, hsdk), a.dv = head_rows(dv, lddv, hsdv);
+    a.delta = static_cast<float *>(workspace);
+    return launched(launch_attention_backward(a, stream));
+}
+
+pase_status pase_rotary(int dtype, uint64_t rows, uint32_t heads, uint32_t dim, uint32_t turned, int interleaved,
+                        int inverse, const void *x, uint64_t ldx, uint64_t hsx, const void *positions, int positions_64,
+                        const double *frequencies, float magnitude, void *y, uint64_t ldy, uint64_t hsy, void *stream) {
+    REQUIRE(known(dtype), "unknown dtype %d", dtype);
+    REQUIRE(heads >= 1 && dim >= 1, "no heads or dim 0");
+    REQUIRE(turned >= 2 && turned % 2 == 0 && turned <= dim, "%u elements of %u cannot be turned in pairs", turned, dim);
+    REQUIRE(interleaved == 0 || interleaved == 1, "interleaved is neither 0 nor 1");
+    REQUIRE(inverse == 0 || inverse == 1, "inverse is neither 0 nor 1");
+    if (turned > 1024) return refuse(PASE_ERR_TOO_LARGE, "%u elements of a head turned, above 1024", turned);
+    if ((uint64_t)heads * dim > 1u << 22) return refuse(PASE_ERR_TOO_LARGE, "heads x dim above 2^22");
+    if (rows > kMaxRows) return refuse(PASE_ERR_TOO_LARGE, "too many rows");
+    if (!rows) return PASE_OK;
+    REQUIRE_HEADS(x, ldx, hsx, rows, heads, dim, dtype);
+    REQUIRE_HEADS(y, ldy, hsy, rows, heads, dim, dtype);
+    REQUIRE(x != y || (ldx == ldy && hsx == hsy), "y is x with other strides");
+    REQUIRE(positions, "positions is null");
+    REQUIRE(positions_64 == 0 || positions_64 == 1, "positions_64 is neither 0 nor 1");
+    REQUIRE(aligned(positions, positions_64 ? 8 : 4), "positions is not aligned to its element");
+    REQUIRE(frequencies && aligned(frequencies, 8), "frequencies is null or not aligned to its element");
+    Rotary a{};
+    a.dtype = dtype, a.positions_64 = positions_64, a.interleaved = interleaved;
+    a.rows = (int64_t)rows, a.heads = (int)heads, a.dim = (int)dim, a.half = (int)turned / 2;
+    a.x = head_rows(x, ldx, hsx), a.y = head_rows(y, ldy, hsy);
+    a.positions = positions, a.frequencies = frequencies;
+    a.magnitude = magnitude, a.sine = inverse ? -magnitude : magnitude;
+    return launched(launch_rotary(a, stream));
+}
+
+pase_status pase_dropout(int dtype, uint64_t rows, uint64_t width, const void *x, uint64_t ldx, const void *residual,
+                         uint64_t ldr, double p, const int64_t *seed, void *y, uint64_t ldy, void *stream) {
+    REQUIRE(known(dtype), "unknown dtype %d", dtype);
+    REQUIRE(width >= 1, "width 0");
+    REQUIRE(p >= 0 && p <= 1, "p is not within 0 and 1");
+    if (width > kMaxLd) return refuse(PASE_ERR_TOO_LARGE, "width above 2^32");
+    const uint64_t calls = (width + 7) / 8;
+    if (rows > kMaxRows / calls) return refuse(PASE_ERR_TOO_LARGE, "2^43 elements or more");
+    if (!rows) return PASE_OK;
+    REQUIRE_MATRIX(x, ldx, width, dtype);
+    if (residual) REQUIRE_MATRIX(residual, ldr, width, dtype);
+    REQUIRE_MATRIX(y, ldy, width, dtype);
+    REQUIRE(x != y || ldx == ldy, "y is x with another row stride");
+    REQUIRE(residual != y || ldr == ldy, "y is the residual with another row stride");
+    REQUIRE(seed && aligned(seed, 8), "seed is null or not aligned to its element");
+    Dropout a{};
+    a.dtype = dtype, a.rows = (int64_t)rows, a.width = (int64_t)width, a.calls = (int64_t)calls;
+    a.x = x, a.ldx = (int64_t)ldx, a.residual = residual, a.ldr = (int64_t)ldr;
+    a.y = y, a.ldy = (int64_t)ldy;
+    a.seed = reinterpret_cast<const uint32_t *>(seed);
+    a.drop = (uint32_t)std::lrint(p * 65536);
+    a.scale = a.drop < 65536 ? (float)(65536.0 / (65536 - a.drop)) : 0.0f;
+    return launched(launch_dropout(a, stream));
 }
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 // Arguments of the layer operators, between the checks of operators.cpp (host)
-// and the launches in layer_norm.hip, softmax_loss.hip and grouped_matmul.hip.
+// and the launches in the .hip file of each.
 #pragma once
 
 #include <cstdint>
@@ -58,6 +58,48 @@ struct GroupedProduct {
     uint32_t first;      // of this launch, where several share the tiles: see launch_tiles()
 };
 
+// An argument [rows, heads, dim]: distances in elements.
+struct HeadRows {
+    void *p;
+    int64_t ld, head_ld;
+};
+
+struct Attention {
+    int dtype, offsets_64, causal;
+    int rows, key_rows, sequences, heads, kv_heads, dim;
+    float scale;
+    const void *q_offsets, *k_offsets, *k_lengths;
+    HeadRows q, k, v, out, dout, dq, dk, dv;
+    float *lse, *delta;  // [heads][rows]
+    float *partial;      // forward with splits > 1: [splits][rows x heads, up to a multiple of 4], then as many rows of dim, up to a multiple of 4
+    int splits, tiles;   // tiles: of the queries' (keys') rows, see tiles_of()
+    uint32_t first;
+};
+
+struct Rotary {
+    int dtype, positions_64, interleaved;
+    int64_t rows;
+    int heads, dim, half;
+    HeadRows x, y;
+    const void *positions;
+    const double *frequencies;
+    float magnitude, sine;   // sine: magnitude, or its negative for the gradient
+    int each;                // rows of a workgroup
+    int64_t first;
+};
+
+struct Dropout {
+    int dtype;
+    int64_t rows, width, calls;      // calls: of the generator for a row
+    const void *x, *residual;
+    void *y;
+    int64_t ldx, ldr, ldy;
+    const uint32_t *seed;
+    uint32_t drop;                   // of 2^16
+    float scale;
+    int64_t first;
+};
+
 // 16-byte vectors of a layer norm's row, and the lanes of the team that holds it
 inline int norm_vectors(int width, int element) { return (int)(((int64_t)width * element + 15) / 16); }
 inline int norm_lanes(int vecs) {
@@ -67,6 +109,9 @@ inline int norm_lanes(int vecs) {
 int norm_backward_blocks(int dtype, int64_t rows, int width);
 // parts each group's rows are cut into by the weights' gradient
 int grouped_matmul_splits(int64_t rows, int groups, int n, int k);
+
+// shares each tile's keys are cut into by the forward pass
+int attention_splits(int64_t rows, int64_t key_rows, int sequences, int heads, int kv_heads);
 
 constexpr int kCus = 256;          // compute units of an MI355X
 constexpr int kBig = 256;          // rows and columns of a tile of the grouped products
@@ -80,6 +125,10 @@ int launch_softmax_loss_backward(const SoftmaxLoss &a, void *stream);   // dlogi
 int launch_product_forward(const GroupedProduct &a, void *stream);
 int launch_product_rows_grad(const GroupedProduct &a, void *stream);
 int launch_product_weights_grad(const GroupedProduct &a, void *stream);
+int launch_attention_forward(const Attention &a, void *stream);
+int launch_attention_backward(const Attention &a, void *stream);
+int launch_rotary(const Rotary &a, void *stream);
+int launch_dropout(const Dropout &a, void *stream);
 const char *launch_error(int e);
 
 }  // namespace pase

@@ -1,13 +1,14 @@
 """The layers of the computation graphs as operators on device tensors.
 
-Residual add + layer norm, matrix products grouped by ragged row ranges, and
-the softmax loss, each with its backward pass: hand-written gfx950 kernels in
+Residual add + layer norm, matrix products grouped by ragged row ranges,
+attention over ragged sequences, rotary positions, dropout with the residual's
+addition, and the softmax loss, each with its backward pass: hand-written gfx950 kernels in
 ``libpase.so`` behind the C ABI of ``include/pase_operators.h``, which says
 what each computes.  The functions here check their arguments, allocate the
 outputs and enqueue the work on the current stream of the tensors' device;
 nothing waits for it.  A refused argument raises `PaseError`.
 
-``layer_norm``, ``grouped_matmul`` and ``softmax_loss`` are differentiable, once
+``layer_norm``, ``grouped_matmul``, ``attention``, ``rotary``, ``dropout`` and ``softmax_loss`` are differentiable, once
 (`torch.autograd`; a second derivative raises); the others are the passes they are made of.
 """
 from __future__ import annotations
@@ -26,11 +27,13 @@ BF16, FP16, FP32 = range(3)
 _DTYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
 NORM_MAX_WIDTH = 16384
 MAX_GROUPS = 65536
+ATTENTION_MAX_DIM = 128
 
 EXPORTS = ["pase_operator_error", "pase_layer_norm_forward", "pase_layer_norm_workspace",
            "pase_layer_norm_backward", "pase_grouped_matmul_forward", "pase_grouped_matmul_workspace",
            "pase_grouped_matmul_backward", "pase_softmax_loss_forward", "pase_softmax_loss_forward_parts",
-           "pase_softmax_loss_grad", "pase_softmax_loss_backward", "pase_softmax_loss_backward_parts"]
+           "pase_softmax_loss_grad", "pase_softmax_loss_backward", "pase_softmax_loss_backward_parts",
+           "pase_attention_forward", "pase_attention_workspace", "pase_attention_backward", "pase_rotary", "pase_dropout"]
 
 _lib = None
 
@@ -42,6 +45,7 @@ def load():
         return _lib
     L = pase.load()
     P, I, U32, U64, I64, F = C.c_void_p, C.c_int, C.c_uint32, C.c_uint64, C.c_int64, C.c_float
+    heads = [P, U64, U64]   # an argument [rows, heads, dim]
     sig = {
         "pase_layer_norm_forward": [I, I, U64, U64, P, U64, P, U64, P, P, F, P, U64, P, U64, P, P, P],
         "pase_layer_norm_workspace": [I, U64, U64, P],
@@ -54,6 +58,11 @@ def load():
         "pase_softmax_loss_grad": [I, U64, U64, P, U64, P, I, I64, P, U64, P, P, P, U64, P],
         "pase_softmax_loss_backward": [I, U64, U64, P, U64, P, I, I64, P, P, U64, P, U64, P],
         "pase_softmax_loss_backward_parts": [I, U64, U64, P, U64, P, I, I64, P, P, P, U64, P, U64, P],
+        "pase_attention_forward": [I, U64, U64, U32, U32, U32, U32, *heads * 3, P, P, P, I, I, F, *heads, P, P, U64, P],
+        "pase_attention_workspace": [I, U64, U64, U32, U32, U32, U32, I, P],
+        "pase_attention_backward": [I, U64, U64, U32, U32, U32, U32, *heads * 5, P, P, P, P, I, I, F, *heads * 3, P, U64, P],
+        "pase_rotary": [I, U64, U32, U32, U32, I, I, *heads, P, I, P, F, *heads, P],
+        "pase_dropout": [I, U64, U64, P, U64, P, U64, C.c_double, P, P, U64, P],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -281,6 +290,178 @@ def grouped_matmul_backward(dy, x, w, offsets, grad_dtype=None, need_dx: bool = 
     return dx, dw
 
 
+# ------------------------------------------------------------------ attention
+def _heads(name, t, like=None, rows=None, heads=None, dim=None):
+    """Checks a [rows, heads, dim] argument and gives its pointer, row stride and head stride."""
+    if t.dim() != 3:
+        _refuse(f"{name} has {t.dim()} dimensions, (rows, heads, dim) is wanted")
+    have_rows, have_heads, have_dim = t.shape
+    if like is not None:
+        if have_dim != dim or (rows is not None and have_rows != rows) or (heads is not None and have_heads != heads):
+            _refuse(f"{name} is {tuple(t.shape)}, ({'...' if rows is None else rows}, {'...' if heads is None else heads}, {dim}) is wanted")
+        _same(name, t, like.dtype, like)
+    elif t.get_device() < 0:
+        _refuse(f"{name} is not on a GPU")
+    ld, hs, step = t.stride()
+    if step != 1 and have_dim > 1:
+        _refuse(f"the elements of a head of {name} are {step} apart, not adjacent")
+    # the distance to a next row or head that is not there does not matter
+    if have_heads < 2:
+        hs = have_dim
+    if have_rows < 2:
+        ld = have_dim
+    if ld < 0 or hs < 0:
+        _refuse(f"{name} has negative strides")
+    return t.data_ptr(), ld, hs
+
+
+def _sequences(q_offsets, k_offsets, k_lengths, like):
+    if q_offsets.dim() != 1 or q_offsets.shape[0] < 2:
+        _refuse(f"q_offsets is {tuple(q_offsets.shape)}, (sequences + 1,) is wanted")
+    n = q_offsets.shape[0] - 1
+    qo, wide = _index("q_offsets", q_offsets, n + 1, like)
+    ko, wide_k = _index("k_offsets", k_offsets, n + 1, like)
+    kl, wide_l = _index("k_lengths", k_lengths, n, like) if k_lengths is not None else (None, wide)
+    if wide != wide_k or wide != wide_l:
+        _refuse("q_offsets, k_offsets and k_lengths are of different types")
+    return n, qo, ko, kl, wide
+
+
+def _attention_args(q, k, v, scale):
+    """(dtype, rows, key rows, heads, kv heads, dim, scale) and the three arguments' pointers and strides."""
+    d = _dtype("q", q.dtype)
+    hq = _heads("q", q)
+    rows, heads, dim = q.shape
+    hk = _heads("k", k, q, dim=dim)
+    key_rows, kv_heads, _ = k.shape
+    hv = _heads("v", v, q, key_rows, kv_heads, dim)
+    return (d, rows, key_rows), (heads, kv_heads, dim), max(dim, 1) ** -0.5 if scale is None else scale, (*hq, *hk, *hv)
+
+
+@_on_device("q")
+def attention_forward(q, k, v, q_offsets, k_offsets, k_lengths=None, causal: bool = False, scale=None):
+    """(out, lse) of attention over ragged sequences: sequence b has the queries
+    q_offsets[b] .. q_offsets[b + 1] - 1 and the keys from k_offsets[b] on, up to k_offsets[b + 1] - 1 or
+    k_lengths[b] of them.  Causal: query i of n sees the keys up to i + (keys - n), so
+    that the last one sees all, as where new tokens follow kept ones.
+
+    q: [rows, heads, dim]; k, v: [key rows, kv heads, dim], each read by heads / kv heads heads next to each
+    other; any distances between rows and heads.  Offsets and lengths: int32 or int64,
+    alike, on the device.  scale: dim ** -0.5 unless given.  out: [rows, heads, dim];
+    lse: float32 [heads, rows].  Queries that see no key, and rows of no sequence, have out 0
+    and lse -inf."""
+    (d, rows, key_rows), (heads, kv_heads, dim), scale, args = _attention_args(q, k, v, scale)
+    n, qo, ko, kl, wide = _sequences(q_offsets, k_offsets, k_lengths, q)
+    L = load()
+    ws, wp, have = _workspace(q, "pase_attention_workspace", d, rows, key_rows, n, heads, kv_heads, dim, 0)
+    out = q.new_empty((rows, heads, dim))
+    lse = q.new_empty((heads, rows), dtype=torch.float32)
+    _check(L.pase_attention_forward(d, rows, key_rows, n, heads, kv_heads, dim, *args, qo, ko, kl, wide, bool(causal), scale,
+                                    out.data_ptr(), heads * dim, dim, lse.data_ptr(), wp, have, _raw_stream(q.get_device())))
+    return out, lse
+
+
+@_on_device("dout")
+def attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, k_lengths=None, causal: bool = False, scale=None):
+    """(dq, dk, dv) from the out and lse of `attention_forward`: dk and dv summed over
+    the heads that share them, 0 for keys that no sequence has."""
+    (d, rows, key_rows), (heads, kv_heads, dim), scale, args = _attention_args(q, k, v, scale)
+    hdo = _heads("dout", dout, q, rows, heads, dim)
+    ho = _heads("out", out, q, rows, heads, dim)
+    if lse.shape != (heads, rows) or not lse.is_contiguous():
+        _refuse(f"lse is {tuple(lse.shape)}, contiguous ({heads}, {rows}) is wanted")
+    _same("lse", lse, torch.float32, q)
+    n, qo, ko, kl, wide = _sequences(q_offsets, k_offsets, k_lengths, q)
+    L = load()
+    ws, wp, have = _workspace(q, "pase_attention_workspace", d, rows, key_rows, n, heads, kv_heads, dim, 1)
+    dq = q.new_empty((rows, heads, dim))
+    dk, dv = q.new_empty((key_rows, kv_heads, dim)), q.new_empty((key_rows, kv_heads, dim))
+    _check(L.pase_attention_backward(d, rows, key_rows, n, heads, kv_heads, dim, *hdo, *args, *ho, lse.data_ptr(), qo, ko, kl,
+                                     wide, bool(causal), scale, dq.data_ptr(), heads * dim, dim, dk.data_ptr(),
+                                     kv_heads * dim, dim, dv.data_ptr(), kv_heads * dim, dim, wp, have,
+                                     _raw_stream(q.get_device())))
+    return dq, dk, dv
+
+
+# ------------------------------------------------------------------ rotary positions
+def rotary_frequencies(turned: int, base: float = 10000.0, factor: float = 1.0, trained=None, slow: float = 1.0,
+                       fast: float = 32.0, device="cuda"):
+    """Frequencies of the turned / 2 pairs for `rotary`, float64: base ** (-2 i / turned), divided by
+    `factor` for sequences that many times as long.  With `trained`, the length trained on, by
+    parts: pairs that turn more than `fast` times over that length keep their
+    frequency, those below `slow` turns are divided, those between are mixed in proportion to their turns."""
+    if turned < 2 or turned % 2:
+        _refuse(f"{turned} elements cannot be turned in pairs")
+    if not factor > 0 or not base > 0 or (trained is not None and not 0 < slow < fast):
+        _refuse("base and factor are positive, and slow is below fast")
+    f = base ** (-torch.arange(0, turned, 2, dtype=torch.float64, device=device) / turned)
+    if trained is None:
+        return f / factor
+    kept = ((trained * f / 6.283185307179586 - slow) / (fast - slow)).clamp(0, 1)
+    return f * kept + f / factor * (1 - kept)
+
+
+def _rotary(x, positions, frequencies, interleaved, magnitude, out, inverse):
+    d = _dtype("x", x.dtype)
+    hx = _heads("x", x)
+    rows, heads, dim = x.shape
+    p, wide = _index("positions", positions, rows, x)
+    if frequencies.dim() != 1:
+        _refuse(f"frequencies is {tuple(frequencies.shape)}, (turned / 2,) is wanted")
+    f = _vector("frequencies", frequencies, frequencies.shape[0], torch.float64, x)
+    y = x.new_empty((rows, heads, dim)) if out is None else out
+    hy = _heads("out", y, x, rows, heads, dim)
+    _check(load().pase_rotary(d, rows, heads, dim, 2 * frequencies.shape[0], bool(interleaved), inverse, *hx, p, wide, f,
+                              magnitude, *hy, _raw_stream(x.get_device())))
+    _written(out)
+    return y
+
+
+@_on_device("x")
+def rotary_forward(x, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0, out=None):
+    """Turns pair i of every head of row t by the angle positions[t] * frequencies[i], times magnitude.
+
+    x: [rows, heads, dim], any distances between rows and heads; positions: [rows], int32 or
+    int64; frequencies: float64 [turned / 2] (`rotary_frequencies`).  Pairs are elements i and i + turned / 2,
+    or (interleaved) 2 i and 2 i + 1; the elements from `turned` on stay.  out may be x."""
+    return _rotary(x, positions, frequencies, interleaved, magnitude, out, 0)
+
+
+@_on_device("dy")
+def rotary_backward(dy, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0, out=None):
+    """dx of `rotary_forward`: the same turned the other way.  out may be dy."""
+    return _rotary(dy, positions, frequencies, interleaved, magnitude, out, 1)
+
+
+# ------------------------------------------------------------------ dropout
+def _dropout(x, p, seed, residual):
+    d = _dtype("x", x.dtype)
+    ldx = _matrix("x", x)
+    rows, width = x.shape
+    r, ldr = None, 0
+    if residual is not None:
+        ldr, r = _matrix("residual", residual, x, rows, width), residual.data_ptr()
+    s = _vector("seed", seed, 2, torch.int64, x)
+    y = x.new_empty((rows, width))
+    _check(load().pase_dropout(d, rows, width, x.data_ptr(), ldx, r, ldr, p, s, y.data_ptr(), width, _raw_stream(x.get_device())))
+    return y
+
+
+@_on_device("x")
+def dropout_forward(x, p: float, seed, residual=None):
+    """residual + keep * x / (1 - p) for x [rows, width], where every element is kept with
+    probability 1 - p (p to the nearest multiple of 2 ** -16).  Which are kept follows from seed, two int64 on the device, and the
+    element's row and column alone: no mask is stored.  Calls whose masks are to be
+    independent need different seeds; a captured call reads its seed when it is replayed."""
+    return _dropout(x, p, seed, residual)
+
+
+@_on_device("dy")
+def dropout_backward(dy, p: float, seed):
+    """dx of `dropout_forward` with the same p and seed; the residual's gradient is dy."""
+    return _dropout(dy, p, seed, None)
+
+
 # ------------------------------------------------------------------ softmax loss
 def _loss_args(logits, targets):
     d = _dtype("logits", logits.dtype)
@@ -377,6 +558,11 @@ def _rows_adjacent(t):
     return t if t.stride(-1) == 1 and (t.shape[0] < 2 or t.stride(0) >= t.shape[1]) else t.contiguous()
 
 
+def _heads_adjacent(t):
+    """The same for [rows, heads, dim]."""
+    return t if t.stride(-1) == 1 and all(s >= t.shape[2] for s, n in zip(t.stride()[:2], t.shape) if n > 1) else t.contiguous()
+
+
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gain, bias, residual, eps):
@@ -424,6 +610,66 @@ class _GroupedMatmul(torch.autograd.Function):
 def grouped_matmul(x, w, offsets):
     """`grouped_matmul_forward`, differentiable in x and w."""
     return _GroupedMatmul.apply(x, w, offsets)
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, q_offsets, k_offsets, k_lengths, causal, scale):
+        out, lse = attention_forward(q, k, v, q_offsets, k_offsets, k_lengths, causal, scale)
+        ctx.save_for_backward(q, k, v, out, lse, q_offsets, k_offsets, k_lengths)
+        ctx.rest = causal, scale
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, q_offsets, k_offsets, k_lengths = ctx.saved_tensors
+        grads = attention_backward(_heads_adjacent(dout), q, k, v, out, lse, q_offsets, k_offsets, k_lengths, *ctx.rest)
+        return *grads, None, None, None, None, None
+
+
+def attention(q, k, v, q_offsets, k_offsets, k_lengths=None, causal: bool = False, scale=None):
+    """The out of `attention_forward`, differentiable in q, k and v."""
+    return _Attention.apply(q, k, v, q_offsets, k_offsets, k_lengths, causal, scale)
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, positions, frequencies, interleaved, magnitude):
+        ctx.save_for_backward(positions, frequencies)
+        ctx.rest = interleaved, magnitude
+        return rotary_forward(x, positions, frequencies, interleaved, magnitude)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return rotary_backward(_heads_adjacent(dy), *ctx.saved_tensors, *ctx.rest), None, None, None, None
+
+
+def rotary(x, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0):
+    """`rotary_forward`, differentiable in x."""
+    return _Rotary.apply(x, positions, frequencies, interleaved, magnitude)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, residual):
+        # the seed as it is now: a caller may advance it in place before the backward pass
+        ctx.save_for_backward(seed.clone())
+        ctx.p = p
+        return dropout_forward(x, p, seed, residual)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        seed, = ctx.saved_tensors
+        dx = dropout_backward(_rows_adjacent(dy), ctx.p, seed) if ctx.needs_input_grad[0] else None
+        return dx, None, None, dy if ctx.needs_input_grad[3] else None
+
+
+def dropout(x, p: float, seed, residual=None):
+    """`dropout_forward`, differentiable in x and residual."""
+    return _Dropout.apply(x, p, seed, residual)
 
 
 class _SoftmaxLoss(torch.autograd.Function):
