@@ -38,6 +38,9 @@ template <> struct Mfma<_Float16> {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// Keeps a uniform branch a branch, where the compiler would make it selects on every path.
+__device__ __forceinline__ void stay_apart() { asm volatile(""); }
+
 // The lane's partner with the same query (or key): the other half of the wave.
 __device__ __forceinline__ float other_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -124,7 +127,9 @@ template <int D> __device__ __forceinline__ int fold(int r) {
 template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
     static constexpr int kChunks = D / 8, N = ROWS * kChunks / (64 * WAVES);
     static_assert(N >= 1 && ROWS * kChunks == N * 64 * WAVES, "whole loads");
-    int at[DIRECT ? N : 1];
+    // A load of all waves takes kStep rows: where that keeps the fold, one place stands for all.
+    static constexpr int kStep = 64 * WAVES / kChunks, kPlaces = !DIRECT || kStep % 16 == 0 ? 1 : N;
+    int at[kPlaces];
     Pack<T> r[DIRECT ? 1 : N];
     int64_t ld;
     int dim, wave;
@@ -133,7 +138,7 @@ template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
         wave = uniform(threadIdx.x >> 6);
         if (DIRECT)
 #pragma unroll
-            for (int n = 0; n < N; n++) {
+            for (int n = 0; n < kPlaces; n++) {
                 const int q = chunk(n), row = q / kChunks, c = q % kChunks ^ fold<D>(row);
                 at[n] = c * 8 < dim ? row * (int)ld * 2 + c * 16 : 0x7fffff00;   // past every range
             }
@@ -146,7 +151,9 @@ template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
             const u32x4 range = buffer_of(p, rows > 0 ? ((rows - 1) * (int)ld + dim) * 2 : 0);
             const uint32_t dst = lds_address(lds) + wave * 1024;
 #pragma unroll
-            for (int n = 0; n < N; n++) load_to_lds(range, at[n], dst + n * WAVES * 1024);
+            for (int n = 0; n < N; n++)
+                load_to_lds(range, kPlaces > 1 ? at[n] : (int)((uint32_t)at[0] + (uint32_t)(n * kStep * 2) * (uint32_t)ld),
+                            dst + n * WAVES * 1024);
         } else {
 #pragma unroll
             for (int n = 0; n < N; n++) {
@@ -184,6 +191,8 @@ template <typename T, int D> struct Reader {
         const int row = 4 * h + (l >> 2), c = (lane >> 4 & 1) * 2 + (l >> 1 & 1);
         across = (row * (D / 8) + (c ^ fold<D>(row))) * 16 + (l & 1) * 8;
     }
+    // The places are formed from these two where they are used: all of them would take 16 registers.
+    __device__ __forceinline__ void again() { asm volatile("" : "+v"(along), "+v"(across)); }
     __device__ __forceinline__ Frag row(uint32_t tile, int r0, int s) const {
         return *(__attribute__((address_space(3))) const Frag *)(uintptr_t)(tile + r0 * D * 2 + (along ^ s * 32));
     }
@@ -335,11 +344,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void k_forward(Atte
                 for (int d = 0; d < D / 16; d++) s[b] = Mfma<T>::go(read.row(kt, b * 32, d), q[d], s[b]);
             }
             if ((t + 1) * KT > all_see) {
+                stay_apart();
 #pragma unroll
                 for (int b = 0; b < KT / 32; b++)
 #pragma unroll
                     for (int j = 0; j < 16; j++)
-                        if (t * KT + b * 32 + 8 * (j / 4) + 4 * h + j % 4 >= seen) s[b][j] = -__builtin_inff();
+                        if (8 * (j / 4) + j % 4 >= seen - t * KT - b * 32 - 4 * h) s[b][j] = -__builtin_inff();
             }
             float top = s[0][0];
 #pragma unroll
@@ -454,7 +464,7 @@ __device__ __forceinline__ float exponent_of(float lse) {   // rows without keys
 }
 
 // Queries along the lanes, as in the forward pass.
-template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(256, 1) void k_queries_grad(Attention a) {
+template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(256, 2) void k_queries_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
     constexpr int WAVES = 4, BM = 128, kTile = KT * D * 2;
     __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
@@ -524,9 +534,10 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
 #pragma unroll
                 for (int j = 0; j < 16; j++) s[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], c, -lse2)) * (dp[j] - delta);
                 if (!whole) {
+                    stay_apart();
 #pragma unroll
                     for (int j = 0; j < 16; j++)
-                        if (t * KT + b * 32 + 8 * (j / 4) + 4 * h + j % 4 >= seen) s[j] = 0.0f;
+                        if (8 * (j / 4) + j % 4 >= seen - t * KT - b * 32 - 4 * h) s[j] = 0.0f;
                 }
 #pragma unroll
                 for (int e = 0; e < 2; e++) {
@@ -548,10 +559,14 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
 // Keys along the lanes: s = q k^T and dp = dout v^T give a lane one key and 16 of 32
 // queries; dv^T += dout^T p and dk^T += q^T ds.  The heads that share the keys come one
 // after the other.
-template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(256, 1) void k_keys_grad(Attention a) {
+template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(256, 2) void k_keys_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
     constexpr int WAVES = 4, BM = 128, kTile = QT * D * 2;
+    // The accumulators of 128 columns leave no registers for both operands of a wave's keys at two waves
+    // a SIMD: the values stay in LDS.
+    constexpr bool kValuesInLds = D == 128;
     __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
+    __shared__ __attribute__((aligned(1024))) char values[kValuesInLds ? BM * D * 2 : 1024];
     __shared__ __attribute__((aligned(16))) float stats[2][2][QT];
     static_assert(2 * 2 * kTile >= BM * D * 2, "the gradients pass the same LDS");
     const uint32_t item = a.first + blockIdx.x;
@@ -566,9 +581,9 @@ template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(2
     const int key = first + wave * 32 + (lane & 31);
     const bool there = key < sq.keys;
     const int64_t row = sq.k_lo + (there ? key : 0);
-    Frag k[D / 16], v[D / 16];
+    Frag k[D / 16], v[kValuesInLds ? 1 : D / 16];
     load_row<T, D>(k, head_of<T>(a.k, row, kv_head), there ? a.dim : 0);
-    load_row<T, D>(v, head_of<T>(a.v, row, kv_head), there ? a.dim : 0);
+    const uint32_t vt = lds_address(values);
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
 
     const float c = a.scale * kLog2e;
@@ -576,8 +591,17 @@ template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(2
     const int from = first - shift < 0 ? 0 : first - shift;
     const int t0 = from / QT, per = first < sq.keys && from < sq.q_rows ? (sq.q_rows + QT - 1) / QT - t0 : 0;
     const int steps = per * group;
+    if constexpr (kValuesInLds) {
+        if (steps) {
+            Feed<T, D, BM, WAVES, DIRECT> fv(a.v.ld, a.dim);
+            fv.load(head_of<T>(a.v, sq.k_lo + first, kv_head), sq.keys - first, values);
+            fv.store(values);
+        }
+    } else {
+        load_row<T, D>(v, head_of<T>(a.v, row, kv_head), there ? a.dim : 0);
+    }
     Feed<T, D, QT, WAVES, DIRECT> fq(a.q.ld, a.dim), fg(a.dout.ld, a.dim);
-    const Reader<T, D> read;
+    Reader<T, D> read;
     float stat = 0;
     int next_head = kv_head * group, next = t0;   // what is loaded next
     const auto load = [&](char *to) {
@@ -601,42 +625,54 @@ template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(2
         const int at = n & 1;
         arrive<DIRECT>();
         if (n + 1 < steps) load(lds[at ^ 1]);
-        const int limit = key - shift - t * QT;   // the tile's queries below it do not see the key
+        const int limit = key - shift - t * QT - 4 * h;   // the lane's queries below it, in the order of its registers, do not see the key
         if (t * QT + QT - 1 + shift >= first + wave * 32) {
             const uint32_t qt = lds_address(lds[at]), gt = qt + kTile;
             const bool whole = t * QT + shift >= first + wave * 32 + 31;
-#pragma unroll
+#pragma unroll 1
             for (int b = 0; b < QT / 32; b++) {
+                read.again();
                 f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
-                for (int d = 0; d < D / 16; d++) {
-                    s = Mfma<T>::go(read.row(qt, b * 32, d), k[d], s);
-                    dp = Mfma<T>::go(read.row(gt, b * 32, d), v[d], dp);
-                }
+                for (int d = 0; d < D / 16; d++) s = Mfma<T>::go(read.row(qt, b * 32, d), k[d], s);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     const Pack<float> lse2 = *reinterpret_cast<const Pack<float> *>(&stats[at][0][b * 32 + 8 * e + 4 * h]);
-                    const Pack<float> delta = *reinterpret_cast<const Pack<float> *>(&stats[at][1][b * 32 + 8 * e + 4 * h]);
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
+                    for (int j = 0; j < 4; j++)
                         s[4 * e + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * e + j], c, -lse2.e[j]));
-                        dp[4 * e + j] = s[4 * e + j] * (dp[4 * e + j] - delta.e[j]);
-                    }
                 }
                 if (!whole) {
+                    stay_apart();
 #pragma unroll
                     for (int j = 0; j < 16; j++)
-                        if (b * 32 + 8 * (j / 4) + 4 * h + j % 4 < limit) s[j] = dp[j] = 0.0f;
+                        if (8 * (j / 4) + j % 4 < limit - b * 32) s[j] = 0.0f;
                 }
+                const Frag p[2] = {narrow<T>(s, 0), narrow<T>(s, 8)};
+                #pragma unroll
+                for (int e = 0; e < 2; e++)
 #pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    const Frag p = narrow<T>(s, e * 8), ds = narrow<T>(dp, e * 8);
+                    for (int d = 0; d < D / 32; d++) dv[d] = Mfma<T>::go(read.column(gt, b * 2 + e, d), p[e], dv[d]);
 #pragma unroll
-                    for (int d = 0; d < D / 32; d++) {
-                        dv[d] = Mfma<T>::go(read.column(gt, b * 2 + e, d), p, dv[d]);
-                        dk[d] = Mfma<T>::go(read.column(qt, b * 2 + e, d), ds, dk[d]);
-                    }
+                for (int d = 0; d < D / 16; d++)
+                    dp = Mfma<T>::go(read.row(gt, b * 32, d), kValuesInLds ? read.row(vt, wave * 32, d) : v[kValuesInLds ? 0 : d], dp);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const Pack<float> delta = *reinterpret_cast<const Pack<float> *>(&stats[at][1][b * 32 + 8 * e + 4 * h]);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) dp[4 * e + j] = s[4 * e + j] * (dp[4 * e + j] - delta.e[j]);
                 }
+                if (!whole) {
+                    stay_apart();
+#pragma unroll
+                    for (int j = 0; j < 16; j++)
+                        if (8 * (j / 4) + j % 4 < limit - b * 32) dp[j] = 0.0f;
+                }
+                const Frag ds[2] = {narrow<T>(dp, 0), narrow<T>(dp, 8)};
+                #pragma unroll
+                for (int e = 0; e < 2; e++)
+#pragma unroll
+                    for (int d = 0; d < D / 32; d++) dk[d] = Mfma<T>::go(read.column(qt, b * 2 + e, d), ds[e], dk[d]);
             }
         }
         if (n + 1 < steps) store(lds[at ^ 1], stats[at ^ 1][0]);
@@ -699,12 +735,12 @@ template <typename T, int D> int backward(Attention a, void *stream) {
     a.tiles = (int)tiles_of(packed, 128, a.sequences);
     const int64_t items = a.rows ? (int64_t)a.tiles * a.kv_heads : 0;
     if (const int e = direct<T>(a, a.k) && direct<T>(a, a.v) ? launch_items(k_queries_grad<T, D, 64, true>, items, 256, stream, a)
-                                                             : launch_items(k_queries_grad<T, D, 64, false>, items, 256, stream, a))
+                                                             : launch_items(k_queries_grad<T, D, D == 128 ? 32 : 64, false>, items, 256, stream, a))
         return e;
     a.tiles = (int)tiles_of(a.key_rows, 128, a.sequences);
     const int64_t keys = a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0;
-    return direct<T>(a, a.q) && direct<T>(a, a.dout) ? launch_items(k_keys_grad<T, D, 64, true>, keys, 256, stream, a)
-                                                     : launch_items(k_keys_grad<T, D, 64, false>, keys, 256, stream, a);
+    return direct<T>(a, a.q) && direct<T>(a, a.dout) ? launch_items(k_keys_grad<T, D, D == 128 ? 32 : 64, true>, keys, 256, stream, a)
+                                                     : launch_items(k_keys_grad<T, D, D == 128 ? 32 : 64, false>, keys, 256, stream, a);
 }
 
 template <typename T> int backward(const Attention &a, void *stream) {
