@@ -19,6 +19,7 @@
 namespace pase {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -135,7 +136,7 @@ template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
     int dim, wave;
 
     __device__ __forceinline__ Feed(int64_t ld_, int dim_) : ld(ld_), dim(dim_) {
-        wave = uniform(threadIdx.x >> 6);
+        wave = uniform(threadIdx.x >> 6) % WAVES;
         if (DIRECT)
 #pragma unroll
             for (int n = 0; n < kPlaces; n++) {
@@ -179,8 +180,10 @@ template <bool DIRECT> __device__ __forceinline__ void arrive() {
     }
 }
 
-// Operand reads of a tile.  Along: row r0 + lane % 32, elements 16 s + 8 h of it.
-// Across: column 32 d + lane % 32, rows 16 g + 4 h + {0..3, 8..11} of the 16.
+// Operand reads of a tile (at a multiple of 256 bytes).  Along: row r0 + lane % 32, elements
+// 16 s + 8 h of it.  Across: column 32 d + lane % 32, rows 16 g + 4 h + {0..3, 8..11} of the 16.
+// A fragment's place follows from the tile's by an exclusive or and a constant; begun anew for
+// each tile, so that not all places of all tiles are kept in registers.
 template <typename T, int D> struct Reader {
     typedef typename Mfma<T>::Frag Frag;
     uint32_t along, across;   // byte places within a tile
@@ -191,19 +194,23 @@ template <typename T, int D> struct Reader {
         const int row = 4 * h + (l >> 2), c = (lane >> 4 & 1) * 2 + (l >> 1 & 1);
         across = (row * (D / 8) + (c ^ fold<D>(row))) * 16 + (l & 1) * 8;
     }
-    // The places are formed from these two where they are used: all of them would take 16 registers.
-    __device__ __forceinline__ void again() { asm volatile("" : "+v"(along), "+v"(across)); }
-    __device__ __forceinline__ Frag row(uint32_t tile, int r0, int s) const {
-        return *(__attribute__((address_space(3))) const Frag *)(uintptr_t)(tile + r0 * D * 2 + (along ^ s * 32));
+    static __device__ __forceinline__ uint32_t begin(uint32_t tile, uint32_t place) {
+        uint32_t at = tile + place;
+        asm volatile("" : "+v"(at));
+        return at;
     }
-    __device__ __forceinline__ Frag column(uint32_t tile, int g, int d) const {
+    __device__ __forceinline__ uint32_t rows_of(uint32_t tile) const { return begin(tile, along); }
+    __device__ __forceinline__ uint32_t columns_of(uint32_t tile) const { return begin(tile, across); }
+    static __device__ __forceinline__ Frag row(uint32_t at, int r0, int s) {
+        return *(__attribute__((address_space(3))) const Frag *)(uintptr_t)((at ^ s * 32) + r0 * D * 2);
+    }
+    static __device__ __forceinline__ Frag column(uint32_t at, int g, int d) {
         union {
             Frag f;
             s16x4 half[2];
         } u;
-        const uint32_t at = across ^ d * 64;
-        u.half[0] = read_across(tile + g * 16 * D * 2 + at);
-        u.half[1] = read_across(tile + (g * 16 + 8) * D * 2 + (at ^ 32));
+        u.half[0] = read_across((at ^ d * 64) + g * 16 * D * 2);
+        u.half[1] = read_across((at ^ (d * 64 + 32)) + (g * 16 + 8) * D * 2);
         return u.f;
     }
 };
@@ -335,7 +342,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void k_forward(Atte
         arrive<DIRECT>();
         if (t + 1 < t1) load(t + 1, lds[at ^ 1]);
         if (t * KT < any_sees) {
-            const uint32_t kt = lds_address(lds[at]), vt = kt + kTile;
+            const uint32_t tile = lds_address(lds[at]), kt = read.rows_of(tile), vt = read.columns_of(tile + kTile);
             f32x16 s[KT / 32];
 #pragma unroll
             for (int b = 0; b < KT / 32; b++) {
@@ -455,7 +462,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a)
 // ---------------------------------------------------------------- backward
 // p = exp(s - lse), ds = p (dp - delta) with dp = v . dout and delta = out . dout.  Two
 // kernels, each with its own outputs in registers: dq over the keys, which also leaves
-// delta, and dk and dv over the queries.  Scores and dp are formed in both (seven
+// the rows' exponents and deltas, and dk and dv over the queries.  Scores and dp are formed in both (seven
 // products where one kernel with atomics would take five): sums have a fixed order.
 // p and ds are rounded to the operands' type before their second products.
 
@@ -494,7 +501,7 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
         if (there) {
             const int64_t at = (int64_t)head * a.rows + row;
             lse2 = exponent_of(a.lse[at]);
-            if (h == 0) a.delta[at] = delta;
+            if (h == 0) a.stats[at] = {lse2, delta};
         }
     }
     const int last = qs.rows - 1 - qs.first < BM - 1 ? qs.rows - 1 - qs.first : BM - 1;
@@ -521,7 +528,7 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
         arrive<DIRECT>();
         if (t + 1 < tiles) load(t + 1, lds[at ^ 1]);
         if (t * KT < any_sees) {
-            const uint32_t kt = lds_address(lds[at]), vt = kt + kTile;
+            const uint32_t tile = lds_address(lds[at]), kt = read.rows_of(tile), vt = read.rows_of(tile + kTile), kc = read.columns_of(tile);
             const bool whole = (t + 1) * KT <= all_see;
 #pragma unroll
             for (int b = 0; b < KT / 32; b++) {
@@ -543,7 +550,7 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
                 for (int e = 0; e < 2; e++) {
                     const Frag ds = narrow<T>(s, e * 8);
 #pragma unroll
-                    for (int d = 0; d < D / 32; d++) dq[d] = Mfma<T>::go(read.column(kt, b * 2 + e, d), ds, dq[d]);
+                    for (int d = 0; d < D / 32; d++) dq[d] = Mfma<T>::go(read.column(kc, b * 2 + e, d), ds, dq[d]);
                 }
             }
         }
@@ -557,18 +564,22 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
 }
 
 // Keys along the lanes: s = q k^T and dp = dout v^T give a lane one key and 16 of 32
-// queries; dv^T += dout^T p and dk^T += q^T ds.  The heads that share the keys come one
-// after the other.
-template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(256, 2) void k_keys_grad(Attention a) {
+// queries; dv^T += dout^T p and dk^T += q^T ds.  One or two teams of four waves have the
+// same 128 keys: of the steps through the queries of all heads that share them, QT at a
+// time, two teams take every other one each, and their sums are added at the end.
+// DIRECT: three steps in LDS, two on their way (two and one where LDS would hold no second
+// workgroup); else one, loaded where it is needed.
+template <typename T, int D, int QT, int TEAMS, bool DIRECT>
+__global__ __launch_bounds__(TEAMS * 256, TEAMS == 2 ? 1 : D == 128 ? 2 : 3) void k_keys_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
-    constexpr int WAVES = 4, BM = 128, kTile = QT * D * 2;
-    // The accumulators of 128 columns leave no registers for both operands of a wave's keys at two waves
-    // a SIMD: the values stay in LDS.
+    constexpr int WAVES = 4, BM = 128, kTile = QT * D * 2, kStats = QT * 8, kStep = 2 * kTile + kStats;
+    constexpr int kSteps = !DIRECT ? 1 : TEAMS == 1 && D == 128 ? 2 : 3, kJoin = BM * D * 4;   // (both gradients pass as many bytes on their way out)
+    // The accumulators of 128 columns leave no registers for both operands of a wave's keys:
+    // the values stay in LDS.
     constexpr bool kValuesInLds = D == 128;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
-    __shared__ __attribute__((aligned(1024))) char values[kValuesInLds ? BM * D * 2 : 1024];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][QT];
-    static_assert(2 * 2 * kTile >= BM * D * 2, "the gradients pass the same LDS");
+    constexpr int kValues = kValuesInLds ? BM * D * 2 : 0;
+    constexpr int kLds = kValues + TEAMS * kSteps * kStep > kJoin ? kValues + TEAMS * kSteps * kStep : kJoin;
+    __shared__ __attribute__((aligned(1024))) char lds[kLds];
     const uint32_t item = a.first + blockIdx.x;
     // early tiles, which the most queries see, first
     const int kv_head = (int)(item % a.kv_heads), tile = (int)(item / a.kv_heads);
@@ -577,70 +588,96 @@ template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(2
     const Sequence sq(a, own.v);
     const int first = (tile - own.first) * BM;
     if (first < 0 || first >= sq.k_rows) return;
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5;
-    const int key = first + wave * 32 + (lane & 31);
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int team = TEAMS == 1 ? 0 : uniform(threadIdx.x >> 8), wave = uniform(threadIdx.x >> 6) & 3;
+    const int key0 = first + wave * 32, key = key0 + (lane & 31);
     const bool there = key < sq.keys;
     const int64_t row = sq.k_lo + (there ? key : 0);
     Frag k[D / 16], v[kValuesInLds ? 1 : D / 16];
     load_row<T, D>(k, head_of<T>(a.k, row, kv_head), there ? a.dim : 0);
-    const uint32_t vt = lds_address(values);
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
 
     const float c = a.scale * kLog2e;
     const int shift = a.causal ? sq.keys - sq.q_rows : 1 << 30;   // query i sees keys up to i + shift
     const int from = first - shift < 0 ? 0 : first - shift;
     const int t0 = from / QT, per = first < sq.keys && from < sq.q_rows ? (sq.q_rows + QT - 1) / QT - t0 : 0;
-    const int steps = per * group;
+    const int steps = (per * group + TEAMS - 1) / TEAMS;   // of either team; the second's last one may be empty
     if constexpr (kValuesInLds) {
         if (steps) {
-            Feed<T, D, BM, WAVES, DIRECT> fv(a.v.ld, a.dim);
-            fv.load(head_of<T>(a.v, sq.k_lo + first, kv_head), sq.keys - first, values);
-            fv.store(values);
+            Feed<T, D, BM, TEAMS * WAVES, DIRECT> fv(a.v.ld, a.dim);
+            fv.load(head_of<T>(a.v, sq.k_lo + first, kv_head), sq.keys - first, lds);
+            fv.store(lds);
         }
     } else {
         load_row<T, D>(v, head_of<T>(a.v, row, kv_head), there ? a.dim : 0);
     }
     Feed<T, D, QT, WAVES, DIRECT> fq(a.q.ld, a.dim), fg(a.dout.ld, a.dim);
-    Reader<T, D> read;
-    float stat = 0;
-    int next_head = kv_head * group, next = t0;   // what is loaded next
-    const auto load = [&](char *to) {
-        const int r0 = next * QT, left = sq.q_rows - r0;
-        if (threadIdx.x < 2 * QT) {
-            const int r = threadIdx.x % QT;
-            const float *of = threadIdx.x < QT ? a.lse : a.delta;
-            stat = r < left ? of[(int64_t)next_head * a.rows + sq.q_lo + r0 + r] : threadIdx.x < QT ? -__builtin_inff() : 0.0f;
+    const Reader<T, D> read;
+    char *const mine = lds + kValues + team * kSteps * kStep;
+    const auto step_at = [&](int n) { return mine + (kSteps > 1 ? n % kSteps : 0) * kStep; };
+    // the tile and the head of the team's n-th step; past the last, no rows
+    const auto load = [&](int n) {
+        const int s = TEAMS * n + team, down = s / per, r0 = (t0 + s - down * per) * QT, head = kv_head * group + down;
+        const int left = down < group ? sq.q_rows - r0 : 0;
+        char *to = step_at(n);
+        const int64_t at = left > 0 ? (int64_t)head * a.rows + sq.q_lo + r0 : 0;
+        if (DIRECT) {
+            const int64_t row = left > 0 ? sq.q_lo + r0 : 0, of = left > 0 ? head : 0;
+            fq.load(head_of<T>(a.q, row, of), left, to);
+            fg.load(head_of<T>(a.dout, row, of), left, to + kTile);
+            // each wave the same: one count of loads for all
+            load_words_to_lds(buffer_of(a.stats + at, left > 0 ? (left < QT ? left : QT) * 8 : 0), lane * 4, lds_address(to + 2 * kTile));
+            if (QT == 64)
+                load_words_to_lds(buffer_of(a.stats + at, left > 0 ? (left < QT ? left : QT) * 8 : 0), lane * 4 + 256, lds_address(to + 2 * kTile + 256));
+        } else {
+            const int r = threadIdx.x & 255;
+            if (r < QT) reinterpret_cast<RowStats *>(to + 2 * kTile)[r] = r < left ? a.stats[at + r] : RowStats{0, 0};
+            const int64_t row = left > 0 ? sq.q_lo + r0 : 0, of = left > 0 ? head : 0;
+            fq.load(head_of<T>(a.q, row, of), left, to);
+            fq.store(to);
+            fg.load(head_of<T>(a.dout, row, of), left, to + kTile);
+            fg.store(to + kTile);
         }
-        fq.load(head_of<T>(a.q, sq.q_lo + r0, next_head), left, to);
-        fg.load(head_of<T>(a.dout, sq.q_lo + r0, next_head), left, to + kTile);
-        if (++next == t0 + per) next = t0, next_head++;
     };
-    const auto store = [&](char *to, float *st) {
-        if (threadIdx.x < 2 * QT) st[threadIdx.x] = threadIdx.x < QT ? exponent_of(stat) : stat;
-        fq.store(to), fg.store(to + kTile);
-    };
-    if (steps) load(lds[0]), store(lds[0], stats[0][0]);
-    int t = t0;
+    if (DIRECT) {
+        for (int n = 0; n < kSteps - 1; n++)
+            if (n < steps) load(n);
+    }
     for (int n = 0; n < steps; n++) {
-        const int at = n & 1;
-        arrive<DIRECT>();
-        if (n + 1 < steps) load(lds[at ^ 1]);
-        const int limit = key - shift - t * QT - 4 * h;   // the lane's queries below it, in the order of its registers, do not see the key
-        if (t * QT + QT - 1 + shift >= first + wave * 32) {
-            const uint32_t qt = lds_address(lds[at]), gt = qt + kTile;
-            const bool whole = t * QT + shift >= first + wave * 32 + 31;
+        if (DIRECT) {
+            constexpr int kLoads = 2 * decltype(fq)::N + QT / 32;
+            if (kSteps == 3 && n + 1 < steps)
+                wait_loads<kLoads>();
+            else
+                wait_loads<0>();
+            barrier();
+            if (n + kSteps - 1 < steps) load(n + kSteps - 1);
+        } else {
+            __syncthreads();
+            load(n);
+            __syncthreads();
+        }
+        const int s = TEAMS * n + team, down = s / per, q0 = (t0 + s - down * per) * QT;
+        // a query i of this step sees key j where j <= i + shift; the lane's rows are in the order of its registers
+        const int limit = key - shift - q0 - 4 * h;
+        if (down < group && q0 + QT - 1 + shift >= key0) {
+            const uint32_t qt = lds_address(step_at(n)), gt = qt + kTile, st = gt + kTile;
+            const bool whole = q0 + shift >= key0 + 31;
 #pragma unroll 1
             for (int b = 0; b < QT / 32; b++) {
-                read.again();
                 f32x16 s = 0.0f, dp = 0.0f;
+                const uint32_t qr = read.rows_of(qt + b * 32 * D * 2);
 #pragma unroll
-                for (int d = 0; d < D / 16; d++) s = Mfma<T>::go(read.row(qt, b * 32, d), k[d], s);
+                for (int d = 0; d < D / 16; d++) s = Mfma<T>::go(read.row(qr, 0, d), k[d], s);
+                // exponent and delta of rows 8 e + 4 h + {0, 1} and {2, 3}
+                const auto stats = [&](int e, int half) {
+                    return *(__attribute__((address_space(3))) const f32x4 *)(uintptr_t)(st + (b * 32 + 8 * e + 4 * h + 2 * half) * 8);
+                };
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const Pack<float> lse2 = *reinterpret_cast<const Pack<float> *>(&stats[at][0][b * 32 + 8 * e + 4 * h]);
-#pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        s[4 * e + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * e + j], c, -lse2.e[j]));
+                for (int e = 0; e < 8; e++) {
+                    const f32x4 st = stats(e / 2, e % 2);
+                    s[2 * e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e], c, -st[0]));
+                    s[2 * e + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e + 1], c, -st[2]));
                 }
                 if (!whole) {
                     stay_apart();
@@ -649,46 +686,71 @@ template <typename T, int D, int QT, bool DIRECT> __global__ __launch_bounds__(2
                         if (8 * (j / 4) + j % 4 < limit - b * 32) s[j] = 0.0f;
                 }
                 const Frag p[2] = {narrow<T>(s, 0), narrow<T>(s, 8)};
-                #pragma unroll
+                const uint32_t gc = read.columns_of(gt + b * 32 * D * 2);
+#pragma unroll
                 for (int e = 0; e < 2; e++)
 #pragma unroll
-                    for (int d = 0; d < D / 32; d++) dv[d] = Mfma<T>::go(read.column(gt, b * 2 + e, d), p[e], dv[d]);
+                    for (int d = 0; d < D / 32; d++) dv[d] = Mfma<T>::go(read.column(gc, e, d), p[e], dv[d]);
+                const uint32_t gr = read.rows_of(gt + b * 32 * D * 2), vr = read.rows_of(lds_address(lds) + wave * 32 * D * 2);
 #pragma unroll
                 for (int d = 0; d < D / 16; d++)
-                    dp = Mfma<T>::go(read.row(gt, b * 32, d), kValuesInLds ? read.row(vt, wave * 32, d) : v[kValuesInLds ? 0 : d], dp);
+                    dp = Mfma<T>::go(read.row(gr, 0, d), kValuesInLds ? read.row(vr, 0, d) : v[kValuesInLds ? 0 : d], dp);
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const Pack<float> delta = *reinterpret_cast<const Pack<float> *>(&stats[at][1][b * 32 + 8 * e + 4 * h]);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) dp[4 * e + j] = s[4 * e + j] * (dp[4 * e + j] - delta.e[j]);
-                }
-                if (!whole) {
-                    stay_apart();
-#pragma unroll
-                    for (int j = 0; j < 16; j++)
-                        if (8 * (j / 4) + j % 4 < limit - b * 32) dp[j] = 0.0f;
+                for (int e = 0; e < 8; e++) {
+                    const f32x4 st = stats(e / 2, e % 2);
+                    dp[2 * e] = s[2 * e] * (dp[2 * e] - st[1]);
+                    dp[2 * e + 1] = s[2 * e + 1] * (dp[2 * e + 1] - st[3]);
                 }
                 const Frag ds[2] = {narrow<T>(dp, 0), narrow<T>(dp, 8)};
-                #pragma unroll
+                const uint32_t qc = read.columns_of(qt + b * 32 * D * 2);
+#pragma unroll
                 for (int e = 0; e < 2; e++)
 #pragma unroll
-                    for (int d = 0; d < D / 32; d++) dk[d] = Mfma<T>::go(read.column(qt, b * 2 + e, d), ds[e], dk[d]);
+                    for (int d = 0; d < D / 32; d++) dk[d] = Mfma<T>::go(read.column(qc, e, d), ds[e], dk[d]);
             }
         }
-        if (n + 1 < steps) store(lds[at ^ 1], stats[at ^ 1][0]);
-        if (++t == t0 + per) t = t0;
+    }
+    // Of two teams the first adds up dv, the second dk; each stores its own.
+    f32x4 *join = reinterpret_cast<f32x4 *>(lds) + wave * 64 + lane;   // a register quad of a wave: 1 KB
+    const auto give = [&](const f32x16(&x)[D / 32]) {
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) join[(d * 4 + e) * 256] = f32x4{x[d][4 * e], x[d][4 * e + 1], x[d][4 * e + 2], x[d][4 * e + 3]};
+    };
+    const auto take = [&](f32x16(&x)[D / 32]) {
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const f32x4 o = join[(d * 4 + e) * 256];
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[d][4 * e + j] += o[j];
+            }
+    };
+    __syncthreads();
+    if (TEAMS == 2) {
+        if (team == 1) give(dv);
+        __syncthreads();
+        if (team == 0) take(dv);
+        __syncthreads();
+        if (team == 0) give(dk);
+        __syncthreads();
+        if (team == 1) take(dk);
+        __syncthreads();
     }
     // keys of the range that do not count get 0 (their lanes hold what a key of zeros would)
-    const int left = sq.k_rows - first - wave * 32;
-    char *mine = lds[0] + wave * 32 * D * 2;
-    __syncthreads();
-    store_rows<T, D>(mine, dv, !there, 1.0f, a.dim, [&](int r) -> T * {
-        return r < left ? out_of<T>(a.dv, sq.k_lo + first + wave * 32 + r, kv_head) : nullptr;
-    });
-    __builtin_amdgcn_wave_barrier();
-    store_rows<T, D>(mine, dk, !there, a.scale, a.dim, [&](int r) -> T * {
-        return r < left ? out_of<T>(a.dk, sq.k_lo + first + wave * 32 + r, kv_head) : nullptr;
-    });
+    const int left = sq.k_rows - key0;
+    char *out = lds + (team * WAVES + wave) * 32 * D * 2;
+    if (team == 0)
+        store_rows<T, D>(out, dv, !there, 1.0f, a.dim, [&](int r) -> T * {
+            return r < left ? out_of<T>(a.dv, sq.k_lo + key0 + r, kv_head) : nullptr;
+        });
+    if (TEAMS == 1) out += WAVES * 32 * D * 2;
+    if (team == TEAMS - 1)
+        store_rows<T, D>(out, dk, !there, a.scale, a.dim, [&](int r) -> T * {
+            return r < left ? out_of<T>(a.dk, sq.k_lo + key0 + r, kv_head) : nullptr;
+        });
 }
 
 // ---------------------------------------------------------------- launches
@@ -739,8 +801,11 @@ template <typename T, int D> int backward(Attention a, void *stream) {
         return e;
     a.tiles = (int)tiles_of(a.key_rows, 128, a.sequences);
     const int64_t keys = a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0;
-    return direct<T>(a, a.q) && direct<T>(a, a.dout) ? launch_items(k_keys_grad<T, D, D == 128 ? 32 : 64, true>, keys, 256, stream, a)
-                                                     : launch_items(k_keys_grad<T, D, D == 128 ? 32 : 64, false>, keys, 256, stream, a);
+    constexpr int QT = D == 32 ? 64 : 32;
+    if (!direct<T>(a, a.q) || !direct<T>(a, a.dout)) return launch_items(k_keys_grad<T, D, QT, 1, false>, keys, 256, stream, a);
+    const int64_t live = (int64_t)a.key_rows / 128 * a.kv_heads;
+    return live < 4 * kCus ? launch_items(k_keys_grad<T, D, QT, 2, true>, keys, 512, stream, a)
+                           : launch_items(k_keys_grad<T, D, QT, 1, true>, keys, 256, stream, a);
 }
 
 template <typename T> int backward(const Attention &a, void *stream) {

@@ -24,6 +24,11 @@ __device__ __forceinline__ void load_to_lds(u32x4 r, int at, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(r) : "memory");
 }
 
+// The same with 4 bytes a lane.
+__device__ __forceinline__ void load_words_to_lds(u32x4 r, int at, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(dst), "v"(at), "s"(r) : "memory");
+}
+
 // The descriptor of `bytes` bytes from p on (both the same for the wave): what lies past them reads as 0.
 __device__ __forceinline__ u32x4 buffer_of(const void *p, uint32_t bytes) {
     const uint64_t at = reinterpret_cast<uint64_t>(p);

@@ -487,7 +487,7 @@ pase_status pase_attention_workspace(int dtype, uint64_t rows, uint64_t key_rows
     REQUIRE(bytes, "bytes is null");
     REQUIRE(backward == 0 || backward == 1, "backward is neither 0 nor 1");
     CHECK(check_attention(dtype, rows, key_rows, sequences, heads, kv_heads, dim));
-    *bytes = backward ? rows * heads * sizeof(float) : attention_bytes(rows, key_rows, sequences, heads, kv_heads, dim);
+    *bytes = backward ? rows * heads * sizeof(RowStats) : attention_bytes(rows, key_rows, sequences, heads, kv_heads, dim);
     return PASE_OK;
 }
 
@@ -509,7 +509,7 @@ pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows,
         REQUIRE_HEADS(out, ldo, hso, rows, heads, dim, dtype);
         REQUIRE(lse && aligned(lse, 4), "lse is null or not aligned to its element");
         REQUIRE_HEADS(dq, lddq, hsdq, rows, heads, dim, dtype);
-        CHECK(check_workspace(workspace, workspace_bytes, rows * heads * sizeof(float)));
+        CHECK(check_workspace(workspace, workspace_bytes, rows * heads * sizeof(RowStats)));
     }
     if (key_rows) {
         REQUIRE_HEADS(k, ldk, hsk, key_rows, kv_heads, dim, dtype);
@@ -525,7 +525,7 @@ pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows,
     a.q = head_rows(q, ldq, hsq), a.k = head_rows(k, ldk, hsk), a.v = head_rows(v, ldv, hsv);
     a.out = head_rows(out, ldo, hso), a.dout = head_rows(dout, lddo, hsdo), a.lse = const_cast<float *>(lse);
     a.dq = head_rows(dq, lddq, hsdq), a.dk = head_rows(dk, lddk, hsdk), a.dv = head_rows(dv, lddv, hsdv);
-    a.delta = static_cast<float *>(workspace);
+    a.stats = static_cast<RowStats *>(workspace);
     return launched(launch_attention_backward(a, stream));
 }
 

@@ -64,13 +64,18 @@ struct HeadRows {
     int64_t ld, head_ld;
 };
 
+struct RowStats {
+    float exponent, delta;   // lse log2 e (infinite where no key is seen) and out . dout
+};
+
 struct Attention {
     int dtype, offsets_64, causal;
     int rows, key_rows, sequences, heads, kv_heads, dim;
     float scale;
     const void *q_offsets, *k_offsets, *k_lengths;
     HeadRows q, k, v, out, dout, dq, dk, dv;
-    float *lse, *delta;  // [heads][rows]
+    float *lse;          // [heads][rows]
+    RowStats *stats;     // [heads][rows], for the second kernel of the backward pass
     float *partial;      // forward with splits > 1: [splits][rows x heads, up to a multiple of 4], then as many rows of dim, up to a multiple of 4
     int splits, tiles;   // tiles: of the queries' (keys') rows, see tiles_of()
     uint32_t first;
