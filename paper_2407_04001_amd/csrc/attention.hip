@@ -128,8 +128,9 @@ template <int D> __device__ __forceinline__ int fold(int r) {
 template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
     static constexpr int kChunks = D / 8, N = ROWS * kChunks / (64 * WAVES);
     static_assert(N >= 1 && ROWS * kChunks == N * 64 * WAVES, "whole loads");
-    // A load of all waves takes kStep rows: where that keeps the fold, one place stands for all.
-    static constexpr int kStep = 64 * WAVES / kChunks, kPlaces = !DIRECT || kStep % 16 == 0 ? 1 : N;
+    // A wave's load takes a kilobyte, kPeriod of which are 16 rows, after which the fold repeats: of a
+    // wave's loads those 16 rows apart share one place.
+    static constexpr int kPeriod = kChunks / 4, kPlaces = !DIRECT || WAVES >= kPeriod ? 1 : kPeriod / WAVES;
     int at[kPlaces];
     Pack<T> r[DIRECT ? 1 : N];
     int64_t ld;
@@ -144,17 +145,21 @@ template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
                 at[n] = c * 8 < dim ? row * (int)ld * 2 + c * 16 : 0x7fffff00;   // past every range
             }
     }
-    __device__ __forceinline__ int chunk(int n) const { return (n * WAVES + wave) * 64 + (threadIdx.x & 63); }
+    __device__ __forceinline__ int block(int n) const {
+        return kPlaces == 1 ? n * WAVES + wave : n / kPlaces * kPeriod + wave * kPlaces + n % kPlaces;
+    }
+    __device__ __forceinline__ int chunk(int n) const { return block(n) * 64 + (threadIdx.x & 63); }
 
     __device__ __forceinline__ void load(const T *p, int rows, const char *lds) {
         if (DIRECT) {
             rows = rows > ROWS ? ROWS : rows;
             const u32x4 range = buffer_of(p, rows > 0 ? ((rows - 1) * (int)ld + dim) * 2 : 0);
-            const uint32_t dst = lds_address(lds) + wave * 1024;
+            const uint32_t dst = lds_address(lds);
 #pragma unroll
-            for (int n = 0; n < N; n++)
-                load_to_lds(range, kPlaces > 1 ? at[n] : (int)((uint32_t)at[0] + (uint32_t)(n * kStep * 2) * (uint32_t)ld),
-                            dst + n * WAVES * 1024);
+            for (int n = 0; n < N; n++) {
+                const uint32_t rows_on = kPlaces == 1 ? n * (64 * WAVES / kChunks) : n / kPlaces * 16;
+                load_to_lds(range, (int)((uint32_t)at[n % kPlaces] + rows_on * 2 * (uint32_t)ld), dst + block(n) * 1024);
+            }
         } else {
 #pragma unroll
             for (int n = 0; n < N; n++) {
@@ -564,16 +569,16 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
 }
 
 // Keys along the lanes: s = q k^T and dp = dout v^T give a lane one key and 16 of 32
-// queries; dv^T += dout^T p and dk^T += q^T ds.  One or two teams of four waves have the
-// same 128 keys: of the steps through the queries of all heads that share them, QT at a
-// time, two teams take every other one each, and their sums are added at the end.
-// DIRECT: three steps in LDS, two on their way (two and one where LDS would hold no second
-// workgroup); else one, loaded where it is needed.
-template <typename T, int D, int QT, int TEAMS, bool DIRECT>
-__global__ __launch_bounds__(TEAMS * 256, TEAMS == 2 ? 1 : D == 128 ? 2 : 3) void k_keys_grad(Attention a) {
+// queries; dv^T += dout^T p and dk^T += q^T ds.  TEAMS teams of waves have the same
+// WAVES x 32 keys: the steps through the queries of all heads that share them, QT at a
+// time, go round the teams, whose sums are added at the end.
+// DIRECT: three steps in LDS, two on their way (two and one where LDS holds no more); else one, loaded where it is needed.
+template <typename T, int D, int QT, int WAVES, int TEAMS, bool DIRECT>
+__global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 3) void k_keys_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
-    constexpr int WAVES = 4, BM = 128, kTile = QT * D * 2, kStats = QT * 8, kStep = 2 * kTile + kStats;
-    constexpr int kSteps = !DIRECT ? 1 : TEAMS == 1 && D == 128 ? 2 : 3, kJoin = BM * D * 4;   // (both gradients pass as many bytes on their way out)
+    constexpr int BM = WAVES * 32, kTile = QT * D * 2, kStats = QT * 8, kStep = 2 * kTile + kStats;
+    constexpr int kSteps = !DIRECT ? 1 : D == 128 ? 2 : 3;
+    constexpr int kPart = BM * D * 4, kJoin = TEAMS > 2 ? (TEAMS - 1) * kPart : kPart;   // (both gradients pass as many bytes on their way out)
     // The accumulators of 128 columns leave no registers for both operands of a wave's keys:
     // the values stay in LDS.
     constexpr bool kValuesInLds = D == 128;
@@ -589,7 +594,7 @@ __global__ __launch_bounds__(TEAMS * 256, TEAMS == 2 ? 1 : D == 128 ? 2 : 3) voi
     const int first = (tile - own.first) * BM;
     if (first < 0 || first >= sq.k_rows) return;
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    const int team = TEAMS == 1 ? 0 : uniform(threadIdx.x >> 8), wave = uniform(threadIdx.x >> 6) & 3;
+    const int team = TEAMS == 1 ? 0 : uniform(threadIdx.x >> 6) / WAVES, wave = uniform(threadIdx.x >> 6) % WAVES;
     const int key0 = first + wave * 32, key = key0 + (lane & 31);
     const bool there = key < sq.keys;
     const int64_t row = sq.k_lo + (there ? key : 0);
@@ -630,7 +635,7 @@ __global__ __launch_bounds__(TEAMS * 256, TEAMS == 2 ? 1 : D == 128 ? 2 : 3) voi
             if (QT == 64)
                 load_words_to_lds(buffer_of(a.stats + at, left > 0 ? (left < QT ? left : QT) * 8 : 0), lane * 4 + 256, lds_address(to + 2 * kTile + 256));
         } else {
-            const int r = threadIdx.x & 255;
+            const int r = threadIdx.x % (WAVES * 64);
             if (r < QT) reinterpret_cast<RowStats *>(to + 2 * kTile)[r] = r < left ? a.stats[at + r] : RowStats{0, 0};
             const int64_t row = left > 0 ? sq.q_lo + r0 : 0, of = left > 0 ? head : 0;
             fq.load(head_of<T>(a.q, row, of), left, to);
@@ -710,31 +715,36 @@ __global__ __launch_bounds__(TEAMS * 256, TEAMS == 2 ? 1 : D == 128 ? 2 : 3) voi
             }
         }
     }
-    // Of two teams the first adds up dv, the second dk; each stores its own.
-    f32x4 *join = reinterpret_cast<f32x4 *>(lds) + wave * 64 + lane;   // a register quad of a wave: 1 KB
-    const auto give = [&](const f32x16(&x)[D / 32]) {
+    // The first team adds up dv in the teams' order, the second dk; each stores its own.
+    const auto join = [&](int part, int quad) -> f32x4 & {
+        return *reinterpret_cast<f32x4 *>(lds + part * kPart + ((quad * WAVES + wave) * 64 + lane) * 16);
+    };
+    const auto give = [&](const f32x16(&x)[D / 32], int to) {
 #pragma unroll
         for (int d = 0; d < D / 32; d++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) join[(d * 4 + e) * 256] = f32x4{x[d][4 * e], x[d][4 * e + 1], x[d][4 * e + 2], x[d][4 * e + 3]};
+            for (int e = 0; e < 4; e++)
+                join(team - (team > to), d * 4 + e) = f32x4{x[d][4 * e], x[d][4 * e + 1], x[d][4 * e + 2], x[d][4 * e + 3]};
     };
     const auto take = [&](f32x16(&x)[D / 32]) {
+#pragma unroll 1
+        for (int part = 0; part < TEAMS - 1; part++)
 #pragma unroll
-        for (int d = 0; d < D / 32; d++)
+            for (int d = 0; d < D / 32; d++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const f32x4 o = join[(d * 4 + e) * 256];
+                for (int e = 0; e < 4; e++) {
+                    const f32x4 o = join(part, d * 4 + e);
 #pragma unroll
-                for (int j = 0; j < 4; j++) x[d][4 * e + j] += o[j];
-            }
+                    for (int j = 0; j < 4; j++) x[d][4 * e + j] += o[j];
+                }
     };
     __syncthreads();
-    if (TEAMS == 2) {
-        if (team == 1) give(dv);
+    if (TEAMS > 1) {
+        if (team != 0) give(dv, 0);
         __syncthreads();
         if (team == 0) take(dv);
         __syncthreads();
-        if (team == 0) give(dk);
+        if (team != 1) give(dk, 1);
         __syncthreads();
         if (team == 1) take(dk);
         __syncthreads();
@@ -747,7 +757,7 @@ __global__ __launch_bounds__(TEAMS * 256, TEAMS == 2 ? 1 : D == 128 ? 2 : 3) voi
             return r < left ? out_of<T>(a.dv, sq.k_lo + key0 + r, kv_head) : nullptr;
         });
     if (TEAMS == 1) out += WAVES * 32 * D * 2;
-    if (team == TEAMS - 1)
+    if (team == (TEAMS > 1))
         store_rows<T, D>(out, dk, !there, a.scale, a.dim, [&](int r) -> T * {
             return r < left ? out_of<T>(a.dk, sq.k_lo + key0 + r, kv_head) : nullptr;
         });
@@ -802,10 +812,10 @@ template <typename T, int D> int backward(Attention a, void *stream) {
     a.tiles = (int)tiles_of(a.key_rows, 128, a.sequences);
     const int64_t keys = a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0;
     constexpr int QT = D == 32 ? 64 : 32;
-    if (!direct<T>(a, a.q) || !direct<T>(a, a.dout)) return launch_items(k_keys_grad<T, D, QT, 1, false>, keys, 256, stream, a);
-    const int64_t live = (int64_t)a.key_rows / 128 * a.kv_heads;
-    return live < 4 * kCus ? launch_items(k_keys_grad<T, D, QT, 2, true>, keys, 512, stream, a)
-                           : launch_items(k_keys_grad<T, D, QT, 1, true>, keys, 256, stream, a);
+    if (!direct<T>(a, a.q) || !direct<T>(a, a.dout)) return launch_items(k_keys_grad<T, D, QT, 4, 1, false>, keys, 256, stream, a);
+    if ((int64_t)a.key_rows / 128 * a.kv_heads >= 4 * kCus) return launch_items(k_keys_grad<T, D, QT, 4, 1, true>, keys, 256, stream, a);
+    a.tiles = (int)tiles_of(a.key_rows, 64, a.sequences);
+    return launch_items(k_keys_grad<T, D, QT, 2, 4, true>, a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0, 512, stream, a);
 }
 
 template <typename T> int backward(const Attention &a, void *stream) {
