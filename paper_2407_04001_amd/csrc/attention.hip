@@ -10,7 +10,7 @@
 //
 // Exponents are powers of two, p = 2^(c s - c m) with c = scale log2 e, one fused
 // multiply-add each.
-#include <cfloat>
+#include <type_traits>
 
 #include "lds.h"
 #include "operators.h"
@@ -291,17 +291,82 @@ struct Queries {
 __device__ __forceinline__ int64_t part_rows(const Attention &a) { return ((int64_t)a.rows * a.heads + 3) & ~3ll; }
 
 // ---------------------------------------------------------------- forward
-// WAVES x 32 queries a workgroup, KT keys a step, keys and values two steps deep in LDS.
-// SPLIT: the tile's keys are dealt to a.splits workgroups, each of which leaves its share's
-// output and log-sum-exp for k_join.
-template <typename T, int D, int WAVES, int KT, bool DIRECT, bool SPLIT>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void k_forward(Attention a) {
+// The softmax of one query a lane, so far: the output as the sum of 2^(c (s - m)) v and the
+// weights' sum over this lane's half of the keys.
+template <typename T, int D, int KT> struct Softmax {
     typedef typename Mfma<T>::Frag Frag;
-    constexpr int BM = WAVES * 32, kTile = KT * D * 2;
+    f32x16 o[D / 32] = {};
+    float m = -__builtin_inff(), sum = 0;
+
+    // KT more keys: kt and vt are their places (along, across), the lane's query q sees `seen` of
+    // them where `some` query of the wave does not see all.  between(): called once the keys are
+    // read; before(): before the values are.
+    template <typename F, typename G>
+    __device__ __forceinline__ void step(uint32_t kt, uint32_t vt, const Frag (&q)[D / 16], int seen, bool some, float c, F between,
+                                         G before) {
+        f32x16 s[KT / 32];
+#pragma unroll
+        for (int b = 0; b < KT / 32; b++) {
+            s[b] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < D / 16; d++) s[b] = Mfma<T>::go(Reader<T, D>::row(kt, b * 32, d), q[d], s[b]);
+        }
+        between();
+        if (some) {
+            stay_apart();
+            seen -= (threadIdx.x >> 5 & 1) * 4;
+#pragma unroll
+            for (int b = 0; b < KT / 32; b++)
+#pragma unroll
+                for (int j = 0; j < 16; j++)
+                    if (b * 32 + 8 * (j / 4) + j % 4 >= seen) s[b][j] = -__builtin_inff();
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KT / 32; b++)
+#pragma unroll
+            for (int j = 0; j < 16; j++) top = fmaxf(top, s[b][j]);
+        top = other_max(top);
+        // The exponents' reference moves only when it is over 8 too low: weights stay below 2^8,
+        // well within either type, and the output is seldom rescaled.
+        if (__any((top - m) * c > 8)) {
+            const float now = fmaxf(m, top), f = now == m ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
+            m = now;
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < D / 32; d++) o[d] *= f;
+        }
+        const float from = m == -__builtin_inff() ? 0.0f : m * c;
+#pragma unroll
+        for (int b = 0; b < KT / 32; b++)
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], c, -from));
+                sum += s[b][j];
+            }
+        before();
+        // weights are rounded to the values' type: by up to 2^-8 (bf16) or 2^-11 of each, either way
+#pragma unroll
+        for (int g = 0; g < KT / 16; g++) {
+            const Frag p = narrow<T>(s[g / 2], g % 2 * 8);
+#pragma unroll
+            for (int d = 0; d < D / 32; d++) o[d] = Mfma<T>::go(Reader<T, D>::column(vt, g, d), p, o[d]);
+        }
+    }
+    // of both halves' sum: a weight of 1 or more, or nothing was seen
+    __device__ __forceinline__ float lse(float all, float c) const {
+        return all == 0 ? -__builtin_inff() : (m * c + __builtin_amdgcn_logf(all)) * kLn2;
+    }
+};
+
+// 128 queries a workgroup, 64 keys a step, keys and values two steps deep in LDS.
+template <typename T, int D, bool DIRECT>
+__global__ __launch_bounds__(256, D == 128 ? 2 : DIRECT ? 4 : 3) void k_forward(Attention a) {
+    typedef typename Mfma<T>::Frag Frag;
+    constexpr int WAVES = 4, BM = 128, KT = 64, kTile = KT * D * 2;
     __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
     static_assert(2 * 2 * kTile >= BM * D * 2, "the output passes the same LDS");
-    const uint32_t block = a.first + blockIdx.x, item = SPLIT ? block / a.splits : block;
-    const int part = SPLIT ? (int)(block - item * a.splits) : 0;
+    const uint32_t item = a.first + blockIdx.x;
     // heads next to each other, so that an XCD's workgroups share as few as may be; late tiles,
     // which see the most keys, first
     const int kv_head = (int)(item % a.kv_heads), tile = a.tiles - 1 - (int)(item / a.kv_heads);
@@ -324,15 +389,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void k_forward(Atte
     const int all_see = busy ? uniform(sq.seen(a, qs.index(wave * 32))) : 0;
     const int any_sees = busy ? uniform(sq.seen(a, qs.index(w_last))) : 0;
     const int end = uniform(sq.seen(a, qs.index(last)));
-    int t0 = 0, t1 = (end + KT - 1) / KT;
-    if (SPLIT) {
-        const int64_t n = t1;
-        t0 = (int)(n * part / a.splits), t1 = (int)(n * (part + 1) / a.splits);
-    }
+    const int tiles = (end + KT - 1) / KT;
 
     const float c = a.scale * kLog2e;
-    f32x16 o[D / 32] = {};
-    float m = -__builtin_inff(), sum = 0;   // sum: of this lane's keys
+    Softmax<T, D, KT> softmax;
     Feed<T, D, KT, WAVES, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
     const Reader<T, D> read;
     const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
@@ -341,127 +401,190 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void k_forward(Atte
         fv.load(v + (int64_t)t * KT * a.v.ld, sq.keys - t * KT, to + kTile);
     };
     const auto store = [&](char *to) { fk.store(to), fv.store(to + kTile); };
-    if (t0 < t1) load(t0, lds[0]), store(lds[0]);
-    for (int t = t0; t < t1; t++) {
-        const int at = (t - t0) & 1;
+    if (tiles) load(0, lds[0]), store(lds[0]);
+    for (int t = 0; t < tiles; t++) {
+        const int at = t & 1;
         arrive<DIRECT>();
-        if (t + 1 < t1) load(t + 1, lds[at ^ 1]);
+        if (t + 1 < tiles) load(t + 1, lds[at ^ 1]);
         if (t * KT < any_sees) {
             const uint32_t tile = lds_address(lds[at]), kt = read.rows_of(tile), vt = read.columns_of(tile + kTile);
-            f32x16 s[KT / 32];
-#pragma unroll
-            for (int b = 0; b < KT / 32; b++) {
-                s[b] = 0.0f;
-#pragma unroll
-                for (int d = 0; d < D / 16; d++) s[b] = Mfma<T>::go(read.row(kt, b * 32, d), q[d], s[b]);
-            }
-            if ((t + 1) * KT > all_see) {
-                stay_apart();
-#pragma unroll
-                for (int b = 0; b < KT / 32; b++)
-#pragma unroll
-                    for (int j = 0; j < 16; j++)
-                        if (8 * (j / 4) + j % 4 >= seen - t * KT - b * 32 - 4 * h) s[b][j] = -__builtin_inff();
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int b = 0; b < KT / 32; b++)
-#pragma unroll
-                for (int j = 0; j < 16; j++) top = fmaxf(top, s[b][j]);
-            top = other_max(top);
-            // The exponents' reference moves only when it is over 8 too low: weights stay below 2^8,
-            // exact in either type's range, and the outputs are seldom rescaled.
-            if (__any((top - m) * c > 8)) {
-                const float now = fmaxf(m, top), f = now == m ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
-                m = now;
-                sum *= f;
-#pragma unroll
-                for (int d = 0; d < D / 32; d++) o[d] *= f;
-            }
-            const float from = m == -__builtin_inff() ? 0.0f : m * c;
-#pragma unroll
-            for (int b = 0; b < KT / 32; b++)
-#pragma unroll
-                for (int j = 0; j < 16; j++) {
-                    s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], c, -from));
-                    sum += s[b][j];
-                }
-            // weights are rounded to the values' type: 2^-9 (bf16) of each, unbiased
-#pragma unroll
-            for (int g = 0; g < KT / 16; g++) {
-                const Frag p = narrow<T>(s[g / 2], g % 2 * 8);
-#pragma unroll
-                for (int d = 0; d < D / 32; d++) o[d] = Mfma<T>::go(read.column(vt, g, d), p, o[d]);
-            }
+            softmax.step(kt, vt, q, seen - t * KT, (t + 1) * KT > all_see, c, [] {}, [] {});
         }
-        if (t + 1 < t1) store(lds[at ^ 1]);
+        if (t + 1 < tiles) store(lds[at ^ 1]);
     }
-    sum = other_sum(sum);
-    const float lse = sum == 0 ? -__builtin_inff() : (m * c + __builtin_amdgcn_logf(sum)) * kLn2;   // sum >= 1 or nothing was seen
-    const float inverse = sum == 0 ? 0.0f : 1.0f / sum;
-    if (SPLIT) {
-        if (!there) return;
-        const int64_t at = (int64_t)(sq.q_lo + i) * a.heads + head, all = part_rows(a);
-        if (h == 0) a.partial[part * all + at] = lse;
-        if (sum == 0) return;   // not read
-        const int width = (a.dim + 3) & ~3;
-        float *out = a.partial + a.splits * all + (part * all + at) * width + 4 * h;
-#pragma unroll
-        for (int d = 0; d < D / 32; d++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                Pack<float> r;
-#pragma unroll
-                for (int j = 0; j < 4; j++) r.e[j] = o[d][4 * e + j] * inverse;
-                if (32 * d + 8 * e + 4 * h < width) *reinterpret_cast<u32x4 *>(out + 32 * d + 8 * e) = r.v;
-            }
-        return;
-    }
+    const float sum = other_sum(softmax.sum), lse = softmax.lse(sum, c);
     if (there && h == 0) a.lse[(int64_t)head * a.rows + sq.q_lo + i] = lse;
     __syncthreads();
-    store_rows<T, D>(lds[0] + wave * 32 * D * 2, o, sum == 0, inverse, a.dim, [&](int r) -> T * {
+    store_rows<T, D>(lds[0] + wave * 32 * D * 2, softmax.o, sum == 0, 1.0f / sum, a.dim, [&](int r) -> T * {
         const int p = wave * 32 + r;
         return qs.has(p) ? out_of<T>(a.out, sq.q_lo + qs.index(p), qs.head(p)) : nullptr;
     });
 }
 
-// Joins the shares of one row and head: weights exp(lse_p - lse).  A wave's half takes
-// every eighth share, its 32 lanes four elements each.
-template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a) {
-    __shared__ float lds[2][256];
-    __shared__ Pack<float> sums[8][32];
-    const int64_t at = (int64_t)a.first + blockIdx.x, all = part_rows(a);
-    const int lane = threadIdx.x & 31, part0 = threadIdx.x >> 5, width = (a.dim + 3) & ~3;
-    float m = -__builtin_inff(), total[1] = {0};
-    for (int p = threadIdx.x; p < a.splits; p += 256) m = fmaxf(m, a.partial[p * all + at]);
-    m = group_max<4>(m, lds[0]);
-    const float from = m == -__builtin_inff() ? 0.0f : m;
-    for (int p = threadIdx.x; p < a.splits; p += 256) total[0] += __expf(a.partial[p * all + at] - from);
-    group_sum<4>(total, lds[1]);
-    Pack<float> sum;
-    sum.v = 0;
-    if (lane * 4 < width)
-        for (int p = part0; p < a.splits; p += 8) {
-            const float lse = a.partial[p * all + at];
-            if (lse == -__builtin_inff()) continue;   // nothing was seen there, or written
-            const float w = __expf(lse - from);
-            const Pack<float> o = load_pack(a.partial + a.splits * all + (p * all + at) * width + lane * 4, 4, 0.0f);
+// Few queries: 32 a workgroup, of one sequence.  Its four waves take every fourth step of 32
+// keys each, with no barrier between them, from LDS of their own: the next step's keys are
+// loaded where this one's were once they are read, values likewise, so that a wave always
+// has loads on their way and LDS holds two workgroups.  The waves' outputs are joined at the end; where tiles are still too few, a.splits workgroups share a tile's keys and leave
+// their outputs and log-sum-exps for k_join.
+template <typename T, int D, bool DIRECT> __global__ __launch_bounds__(256, 2) void k_forward_few(Attention a) {
+    typedef typename Mfma<T>::Frag Frag;
+    constexpr int WAVES = 4, BM = 32, KT = 32, kTile = KT * D * 2;
+    constexpr int kOut = BM * D * 4 + BM * 8;   // a wave's output, references and sums
+    constexpr int kLds = 2 * kTile > kOut ? 2 * kTile : kOut;
+    __shared__ __attribute__((aligned(1024))) char lds[WAVES][kLds];
+    const uint32_t block = a.first + blockIdx.x, item = block / a.splits;
+    const int part = (int)(block - item * a.splits);
+    const int kv_head = (int)(item % a.kv_heads), tile = (int)(item / a.kv_heads), group = a.heads / a.kv_heads;
+    const Owner own(a.q_offsets, a.offsets_64, a.sequences, a.rows, group, BM, tile);
+    const Sequence sq(a, own.v);
+    const Queries qs{group, kv_head * group, sq.q_rows * group, (tile - own.first) * BM};
+    if (tile < own.first || !qs.has(0)) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = lane & 31;
+    const bool there = qs.has(mine);
+    const int i = qs.index(mine), head = qs.head(mine);
+    const int last = qs.rows - 1 - qs.first < BM - 1 ? qs.rows - 1 - qs.first : BM - 1;
+    const int seen = sq.seen(a, i), all_see = uniform(sq.seen(a, qs.index(0)));
+    const int64_t tiles = (uniform(sq.seen(a, qs.index(last))) + KT - 1) / KT;
+    const int t0 = (int)(tiles * part / a.splits) + wave, t1 = (int)(tiles * (part + 1) / a.splits);
+
+    const float c = a.scale * kLog2e;
+    Feed<T, D, KT, 1, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
+    const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
+    char *const kt = lds[wave], *const vt = kt + kTile;
+    const auto load_keys = [&](int t) {
+        if (t < t1) fk.load(k + (int64_t)t * KT * a.k.ld, sq.keys - t * KT, kt), fk.store(kt);
+    };
+    const auto load_values = [&](int t) {
+        if (t < t1) fv.load(v + (int64_t)t * KT * a.v.ld, sq.keys - t * KT, vt), fv.store(vt);
+    };
+    // this wave's loads up to the last N, and its LDS reads and writes, are done
+    const auto done = [](auto n) {
+        if (DIRECT)
+            wait_loads<decltype(n)::value>();
+        else
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    using None = std::integral_constant<int, 0>;
+    using Other = std::integral_constant<int, decltype(fk)::N>;
+    using All = std::integral_constant<int, 63>;   // LDS alone
+    load_keys(t0), load_values(t0);
+    Frag q[D / 16];
+    load_row<T, D>(q, head_of<T>(a.q, there ? sq.q_lo + i : 0, head), there ? a.dim : 0);
+    Softmax<T, D, KT> softmax;
+    const Reader<T, D> read;
+    for (int t = t0; t < t1; t += WAVES) {
+        done(Other{});
+        softmax.step(
+            read.rows_of(lds_address(kt)), read.columns_of(lds_address(vt)), q, seen - t * KT, (t + 1) * KT > all_see, c,
+            [&] { done(All{}), load_keys(t + WAVES); },
+            [&] {
+                if (t + WAVES < t1)
+                    done(Other{});
+                else
+                    done(None{});
+            });
+        done(All{}), load_values(t + WAVES);
+    }
+    // A wave's output in quads of columns, a quad's 32 rows adjacent.
+    const float sum = other_sum(softmax.sum);
+    {
+        f32x4 *out = reinterpret_cast<f32x4 *>(lds[wave]);
 #pragma unroll
-            for (int j = 0; j < 4; j++) sum.e[j] += w * o.e[j];
-        }
-    sums[part0][lane] = sum;
+        for (int d = 0; d < D / 32; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                f32x4 x;
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[j] = softmax.o[d][4 * e + j];
+                out[(d * 8 + e * 2 + h) * 32 + mine] = x;
+            }
+        if (h == 0) reinterpret_cast<float2 *>(out + D * 8)[mine] = {softmax.m, sum};
+    }
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    for (int p = 1; p < 8; p++)
+    const int r = threadIdx.x & 31;
+    if (!qs.has(r)) return;
+    float m[WAVES], w[WAVES], all = 0, top = -__builtin_inff();
 #pragma unroll
-        for (int j = 0; j < 4; j++) sum.e[j] += sums[p][lane].e[j];
+    for (int n = 0; n < WAVES; n++) {
+        const float2 of = reinterpret_cast<const float2 *>(lds[n] + BM * D * 4)[r];
+        m[n] = of.x, w[n] = of.y, top = fmaxf(top, of.x);
+    }
+#pragma unroll
+    for (int n = 0; n < WAVES; n++) {
+        const float f = w[n] == 0 ? 0.0f : __builtin_amdgcn_exp2f((m[n] - top) * c);
+        all += w[n] * f, w[n] = f;
+    }
+    const float inverse = 1.0f / all;
+    const int64_t row = sq.q_lo + qs.index(r), of = qs.head(r), at = row * a.heads + of;
+    if (threadIdx.x < 32) {
+        const float lse = all == 0 ? -__builtin_inff() : (top * c + __builtin_amdgcn_logf(all)) * kLn2;
+        if (a.splits > 1)
+            a.partial[part * part_rows(a) + at] = lse;
+        else
+            a.lse[of * a.rows + row] = lse;
+    }
+    if (a.splits > 1 && all == 0) return;   // not read
+    const int width = (a.dim + 3) & ~3;
+    float *parts = a.partial + a.splits * part_rows(a) + (part * part_rows(a) + at) * width;
+    T *out = out_of<T>(a.out, row, of);
+#pragma unroll
+    for (int n = 0; n < D / 32; n++) {
+        const int quad = threadIdx.x / 32 + n * 8;
+        f32x4 x = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WAVES; k++) {
+            const f32x4 y = reinterpret_cast<const f32x4 *>(lds[k])[quad * 32 + r];
+            if (w[k] != 0) x += y * w[k];   // (what a wave that saw nothing left may be NaN)
+        }
+        x *= inverse;
+        if (quad * 4 >= width) break;
+        if (a.splits > 1) {
+            *reinterpret_cast<f32x4 *>(parts + quad * 4) = x;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (quad * 4 + j < a.dim) out[quad * 4 + j] = all == 0 ? (T)0.0f : (T)x[j];
+        }
+    }
+}
+
+// Joins the shares of 32 columns of one row and head: weights exp(lse_p - lse).  Eight
+// lanes take a share, 32 shares at a time.
+template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a) {
+    __shared__ float lds[2][4], weight[kMaxShares];
+    __shared__ f32x4 sums[4][8];
+    const int groups = (a.dim + 31) / 32, width = (a.dim + 3) & ~3;
+    const int64_t block = (int64_t)a.first + blockIdx.x, at = block / groups, all = part_rows(a);
+    const int column = (int)(block - at * groups) * 32 + (threadIdx.x & 7) * 4;
+    const float lse = (int)threadIdx.x < a.splits ? a.partial[threadIdx.x * all + at] : -__builtin_inff();
+    const float top = group_max<4>(lse, lds[0]);
+    float total[1] = {lse == -__builtin_inff() ? 0.0f : __expf(lse - top)};
+    weight[threadIdx.x] = total[0];
+    group_sum<4>(total, lds[1]);
+    f32x4 sum = 0.0f;
+    const float *parts = a.partial + a.splits * all + at * width + column;
+#pragma unroll
+    for (int n = 0; n < kMaxShares / 32; n++) {
+        const int p = n * 32 + threadIdx.x / 8;
+        // a share without weight was not written
+        if (p < a.splits && column < width && weight[p] != 0) sum += weight[p] * *reinterpret_cast<const f32x4 *>(parts + p * all * width);
+    }
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1)
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum[j] += __shfl_xor(sum[j], d, 64);
+    if ((threadIdx.x & 63) < 8) sums[threadIdx.x >> 6][threadIdx.x & 7] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 8) return;
+    sum = sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] + sums[3][threadIdx.x];
     const int64_t row = at / a.heads, head = at % a.heads;
-    const float inverse = total[0] == 0 ? 0.0f : 1.0f / total[0];
-    T *out = out_of<T>(a.out, row, head) + lane * 4;
+    const bool none = total[0] == 0;
+    T *out = out_of<T>(a.out, row, head) + column;
 #pragma unroll
     for (int j = 0; j < 4; j++)
-        if (lane * 4 + j < a.dim) out[j] = (T)(sum.e[j] * inverse);
-    if (lane == 0) a.lse[head * a.rows + row] = total[0] == 0 ? -__builtin_inff() : m + logf(total[0]);
+        if (column + j < a.dim) out[j] = none ? (T)0.0f : (T)(sum[j] / total[0]);
+    if (column == 0) a.lse[head * a.rows + row] = none ? -__builtin_inff() : top + logf(total[0]);
 }
 
 // ---------------------------------------------------------------- backward
@@ -783,14 +906,14 @@ template <typename T> bool direct(const Attention &a, const HeadRows &x) {
 
 template <typename T, int D, bool DIRECT> int forward(Attention a, void *stream) {
     const int64_t packed = (int64_t)a.rows * (a.heads / a.kv_heads);
-    if (a.splits > 1) {
+    if (a.splits) {
         a.tiles = (int)tiles_of(packed, 32, a.sequences);
         const int64_t items = (int64_t)a.tiles * a.kv_heads * a.splits;
-        if (const int e = launch_items(k_forward<T, D, 1, 32, DIRECT, true>, items, 64, stream, a)) return e;
-        return launch_items(k_join<T>, (int64_t)a.rows * a.heads, 256, stream, a);
+        if (const int e = launch_items(k_forward_few<T, D, DIRECT>, items, 256, stream, a)) return e;
+        return a.splits == 1 ? 0 : launch_items(k_join<T>, (int64_t)a.rows * a.heads * ((a.dim + 31) / 32), 256, stream, a);
     }
     a.tiles = (int)tiles_of(packed, 128, a.sequences);
-    return launch_items(k_forward<T, D, 4, 64, DIRECT, false>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
+    return launch_items(k_forward<T, D, DIRECT>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
 }
 
 template <typename T, int D> int forward(const Attention &a, void *stream) {

@@ -29,7 +29,6 @@ constexpr uint64_t kMaxRows = 1ull << 40, kMaxLd = 1ull << 32;
 constexpr uint64_t kMaxProductDim = 1u << 20;     // n and k of a grouped product
 constexpr uint64_t kMaxProductLd = 1u << 22;      // 256 rows of a tile stay within 2^31 bytes
 constexpr uint64_t kMaxHeadStride = 1ull << 40;
-constexpr int kMaxShares = 256;                   // of a tile's keys
 constexpr uint64_t kMaxClasses = (1ull << 31) - 1024;
 
 int element_bytes(int dtype) { return dtype == PASE_FP32 ? 4 : 2; }
@@ -254,14 +253,16 @@ int grouped_matmul_splits(int64_t rows, int groups, int n, int k) {
     return (int)(most < 1 ? 1 : most > 32 ? 32 : most);
 }
 
-// Shares of at least 128 keys, until four workgroups a CU have one, where the queries alone
-// make fewer.
+// Tiles of 32 queries where sequences have no more on average, or where tiles of 128 would be fewer than
+// CUs; cut into shares of at least 256 keys (eight steps for each of a workgroup's waves are
+// 1024) until there are four a CU.
 int attention_splits(int64_t rows, int64_t key_rows, int sequences, int heads, int kv_heads) {
     const int64_t packed = rows * (heads / kv_heads), some = rows < sequences ? rows : sequences;
     const int64_t large = (packed + 127) / 128, tiles = (large > some ? large : some) * kv_heads;
-    if (tiles <= 0 || tiles >= kCus) return 1;
+    if (packed > 32 * some && tiles >= kCus) return 0;
     const int64_t small = (packed + 31) / 32, items = (small > some ? small : some) * kv_heads;
-    const int64_t want = 4 * kCus / items, deep = key_rows / sequences / 128, most = want < deep ? want : deep;
+    if (!items) return 0;
+    const int64_t want = 4 * kCus / items, deep = key_rows / sequences / 256, most = want < deep ? want : deep;
     return (int)(most < 1 ? 1 : most > kMaxShares ? kMaxShares : most);
 }
 

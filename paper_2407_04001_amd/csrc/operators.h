@@ -77,7 +77,7 @@ struct Attention {
     float *lse;          // [heads][rows]
     RowStats *stats;     // [heads][rows], for the second kernel of the backward pass
     float *partial;      // forward with splits > 1: [splits][rows x heads, up to a multiple of 4], then as many rows of dim, up to a multiple of 4
-    int splits, tiles;   // tiles: of the queries' (keys') rows, see tiles_of()
+    int splits, tiles;   // splits: see attention_splits(); tiles: of the queries' (keys') rows, see tiles_of()
     uint32_t first;
 };
 
@@ -115,9 +115,10 @@ int norm_backward_blocks(int dtype, int64_t rows, int width);
 // parts each group's rows are cut into by the weights' gradient
 int grouped_matmul_splits(int64_t rows, int groups, int n, int k);
 
-// shares each tile's keys are cut into by the forward pass
+// shares that each tile's keys are cut into by the forward pass for few queries; 0: the one for many
 int attention_splits(int64_t rows, int64_t key_rows, int sequences, int heads, int kv_heads);
 
+constexpr int kMaxShares = 256;    // of a tile's keys, in attention
 constexpr int kCus = 256;          // compute units of an MI355X
 constexpr int kBig = 256;          // rows and columns of a tile of the grouped products
 constexpr int kGradVecs = 1024;   // 16-byte vectors of a row that one workgroup of the loss gradient takes
