@@ -549,6 +549,36 @@ template <typename T, int D, bool DIRECT> __global__ __launch_bounds__(256, 2) v
     }
 }
 
+// Joins up to kFewShares shares: eight rows and heads a workgroup, 32 lanes each.
+constexpr int kFewShares = 8;
+
+template <typename T> __global__ __launch_bounds__(256) void k_join_few(Attention a) {
+    const int64_t at = ((int64_t)a.first + blockIdx.x) * 8 + threadIdx.x / 32, all = part_rows(a);
+    const int column = (threadIdx.x & 31) * 4, width = (a.dim + 3) & ~3;
+    if (at >= (int64_t)a.rows * a.heads || column >= width) return;
+    const float *parts = a.partial + a.splits * all + at * width + column;
+    float w[kFewShares], top = -__builtin_inff(), total = 0;
+    f32x4 sum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kFewShares; p++) {
+        w[p] = p < a.splits ? a.partial[p * all + at] : -__builtin_inff();
+        top = fmaxf(top, w[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < kFewShares; p++) {
+        w[p] = w[p] == -__builtin_inff() ? 0.0f : __expf(w[p] - top);
+        total += w[p];
+        if (w[p] != 0) sum += w[p] * *reinterpret_cast<const f32x4 *>(parts + p * all * width);   // else it was not written
+    }
+    const int64_t row = at / a.heads, head = at % a.heads;
+    const bool none = total == 0;
+    T *out = out_of<T>(a.out, row, head) + column;
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+        if (column + j < a.dim) out[j] = none ? (T)0.0f : (T)(sum[j] / total);
+    if (column == 0) a.lse[head * a.rows + row] = none ? -__builtin_inff() : top + logf(total);
+}
+
 // Joins the shares of 32 columns of one row and head: weights exp(lse_p - lse).  Eight
 // lanes take a share, 32 shares at a time.
 template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a) {
@@ -910,7 +940,9 @@ template <typename T, int D, bool DIRECT> int forward(Attention a, void *stream)
         a.tiles = (int)tiles_of(packed, 32, a.sequences);
         const int64_t items = (int64_t)a.tiles * a.kv_heads * a.splits;
         if (const int e = launch_items(k_forward_few<T, D, DIRECT>, items, 256, stream, a)) return e;
-        return a.splits == 1 ? 0 : launch_items(k_join<T>, (int64_t)a.rows * a.heads * ((a.dim + 31) / 32), 256, stream, a);
+        if (a.splits == 1) return 0;
+        if (a.splits <= kFewShares) return launch_items(k_join_few<T>, ((int64_t)a.rows * a.heads + 7) / 8, 256, stream, a);
+        return launch_items(k_join<T>, (int64_t)a.rows * a.heads * ((a.dim + 31) / 32), 256, stream, a);
     }
     a.tiles = (int)tiles_of(packed, 128, a.sequences);
     return launch_items(k_forward<T, D, DIRECT>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);

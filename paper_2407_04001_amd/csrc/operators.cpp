@@ -254,15 +254,16 @@ int grouped_matmul_splits(int64_t rows, int groups, int n, int k) {
 }
 
 // Tiles of 32 queries where sequences have no more on average, or where tiles of 128 would be fewer than
-// CUs; cut into shares of at least 256 keys (eight steps for each of a workgroup's waves are
-// 1024) until there are four a CU.
+// CUs; cut into shares of at least 256 keys (two steps for each of a workgroup's waves) until there are two
+// workgroups a CU, which is what LDS holds (four or eight a CU: 64 tokens over 131072 keys 74 and 79 us
+// against 74, 128 queries over 65536 keys 33 against 29).
 int attention_splits(int64_t rows, int64_t key_rows, int sequences, int heads, int kv_heads) {
     const int64_t packed = rows * (heads / kv_heads), some = rows < sequences ? rows : sequences;
     const int64_t large = (packed + 127) / 128, tiles = (large > some ? large : some) * kv_heads;
     if (packed > 32 * some && tiles >= kCus) return 0;
     const int64_t small = (packed + 31) / 32, items = (small > some ? small : some) * kv_heads;
     if (!items) return 0;
-    const int64_t want = 4 * kCus / items, deep = key_rows / sequences / 256, most = want < deep ? want : deep;
+    const int64_t want = 2 * kCus / items, deep = key_rows / sequences / 256, most = want < deep ? want : deep;
     return (int)(most < 1 ? 1 : most > kMaxShares ? kMaxShares : most);
 }
 
