@@ -70,27 +70,34 @@ struct Range {
 
 // Tiles of `size` of a range's rows x group: range v owns those from start(v) * group /
 // size + v up to its successor's, as many as it needs or one more.  Which range a tile
-// is of follows by a search with 64 probes a step, without a pass over all offsets.
+// is of follows by a search of 128 probes a round, without a pass over all offsets.
 // Offsets that break their rule give some range: whatever it is, rows stay within it.
 struct Owner {
     int v, first;   // the range, and its first tile
 
     __device__ __forceinline__ Owner(const void *offsets, int wide, int sequences, int rows, int group, int size, int tile) {
         const int lane = threadIdx.x & 63;
-        int lo = 0, n = sequences + 2;
-        while (n > 1) {
-            const int step = (n + 63) >> 6, at = lane * step, mine = lo + at;
-            const bool before = at < n && begin(offsets, wide, rows, group, size, mine) <= tile;
-            const int found = __builtin_popcountll(__ballot(before));
-            const int skip = (found > 1 ? found - 1 : 0) * step;
-            lo += skip;
-            n = n - skip < step ? n - skip : step;
+        const auto begin = [&](int v) { return (v == 0 ? 0 : clamped(offsets, wide, v - 1, 0, rows)) * group / size + v; };
+        // of ranges lo .. lo + n - 1, every step-th; the last round's are all of them
+        for (int lo = 0, n = sequences + 2;;) {
+            const int step = (n + 127) >> 7;
+            int probe[2];
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const int at = (lane + 64 * k) * step;
+                probe[k] = at < n ? begin(lo + at) : 0x7fffffff;
+            }
+            const uint64_t before = __ballot(probe[0] <= tile), behind = __ballot(probe[1] <= tile);
+            int found = __builtin_popcountll(before) + __builtin_popcountll(behind);   // ranges begin in order
+            found = found > 1 ? found - 1 : 0;
+            const int value = uniform(__shfl(found < 64 ? probe[0] : probe[1], found & 63, 64));
+            lo += found * step;
+            if (step == 1) {
+                v = uniform(lo), first = value;
+                return;
+            }
+            n = n - found * step < step ? n - found * step : step;
         }
-        v = uniform(lo);
-        first = uniform(begin(offsets, wide, rows, group, size, lo));
-    }
-    static __device__ __forceinline__ int begin(const void *offsets, int wide, int rows, int group, int size, int v) {
-        return (v == 0 ? 0 : clamped(offsets, wide, v - 1, 0, rows)) * group / size + v;
     }
 };
 
@@ -119,6 +126,25 @@ template <int D> __device__ __forceinline__ int fold(int r) {
     if (D == 128) return (r & 3) << 2 | (r >> 2 & 3);
     if (D == 64) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
     return r >> 2 & 3;
+}
+
+// Eight elements from `at` on of a row of n, 0 past its end.  The chunk that the end cuts is read whole from
+// before it, where the row is that long, and shifted.
+template <typename T> __device__ __forceinline__ Pack<T> load_chunk(const T *row, int at, int n) {
+    const int have = n - at;
+    if (have >= 8 || have <= 0 || n < 8) return load_pack(row + at, have, (T)0.0f);
+    union {
+        Pack<T> p;
+        uint64_t u[2];
+    } r;
+    r.p = load_pack(row + n - 8, 8, (T)0.0f);
+    const int bits = (8 - have) * 16;
+    if (bits >= 64) {
+        r.u[0] = r.u[1] >> (bits & 63), r.u[1] = 0;
+    } else {
+        r.u[0] = r.u[0] >> bits | r.u[1] << (64 - bits), r.u[1] >>= bits;
+    }
+    return r.p;
 }
 
 // Loads ROWS rows of a head, D elements of each (0 past `dim` and past the rows that
@@ -226,7 +252,7 @@ __device__ __forceinline__ void load_row(typename Mfma<T>::Frag (&f)[D / 16], co
     const int h = threadIdx.x >> 5 & 1;
 #pragma unroll
     for (int s = 0; s < D / 16; s++) {
-        const Pack<T> r = load_pack(p + 16 * s + 8 * h, n - 16 * s - 8 * h, (T)0.0f);
+        const Pack<T> r = load_chunk(p, 16 * s + 8 * h, n);
         f[s] = __builtin_bit_cast(typename Mfma<T>::Frag, r.v);
     }
 }
