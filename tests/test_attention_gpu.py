@@ -331,3 +331,437 @@ def test_dropout_keeps_its_share(ops):  # noqa: F811
         kept.append(y != 0)
     for a, b in ((0, 1), (0, 2), (1, 2)):   # both kept: 0.81 of all where they are independent
         assert abs(int((kept[a] & kept[b]).sum()) / n - 0.81) < 0.001
+
+
+# ------------------------------------------------------------------ more of attention
+def test_gradients_by_differences(ops):  # noqa: F811
+    """dq, dk, dv, and the rotation's and dropout's gradients, against central differences of the 64-bit definition along
+    random directions (of the sum of out * dout, in fp16: forward roundings stay out of the differences)."""
+    g = gen(31)
+    q, k, v, qo, ko, _ = make(31, [9, 5], [12, 5], 4, 2, 24, HF)
+    dout = rand(g, *q.shape, dtype=HF)
+
+    def value(q, k, v):
+        total = torch.zeros((), dtype=torch.double, device="cuda")
+        for a, b in sequences(qo, ko, None):
+            for h in range(4):
+                s, _ = scores64(q[a, h], k[b, h // 2], True, 24 ** -0.5)
+                total += (torch.softmax(s, 1) @ v[b, h // 2].double() * dout[a, h].double()).sum()
+        return total
+
+    out, lse = ops.attention_forward(q, k, v, qo, ko, causal=True)
+    grads = ops.attention_backward(dout, q, k, v, out, lse, qo, ko, causal=True)
+    base = [t.double() for t in (q, k, v)]
+    for i in range(3):
+        for _ in range(3):
+            d = torch.randn(base[i].shape, generator=g, device="cuda", dtype=torch.double)
+            e = 1e-5
+            up, down = ([t + (s * e * d if j == i else 0) for j, t in enumerate(base)] for s in (1, -1))
+            slope = (value(*up) - value(*down)) / (2 * e)
+            # the difference's own error is e^2 times a third derivative of order 1; each gradient element is off by about its
+            # tolerance of 6 roundings (out, p and ds among them) of the largest terms
+            size = (grads[i].double().abs() * d.abs()).sum()
+            assert (slope - (grads[i].double() * d).sum()).abs() <= 6 * U[HF] * size + 1e-6 * size
+
+
+def decoder_layer(O, x, w, gain, offsets, rows_off, positions, frequencies, seeds, p):
+    """A decoder layer with causal self-attention: products, rotation, attention, dropout, norm, feed-forward."""
+    rows, width = x.shape
+    heads, kv, dim = 4, 2, 32
+    qkv = O.grouped_matmul(x, w[0], rows_off).view(rows, heads + 2 * kv, dim)
+    qk = O.rotary(qkv[:, :heads + kv], positions, frequencies)
+    ctx = O.attention(qk[:, :heads], qk[:, heads:], qkv[:, heads + kv:], offsets, offsets, causal=True)
+    y = O.grouped_matmul(ctx.reshape(rows, heads * dim), w[1], rows_off)
+    z = O.dropout(y, p, seeds[0], residual=x)
+    n = O.layer_norm(z, gain[0])
+    f = O.grouped_matmul(torch.relu(O.grouped_matmul(n, w[2], rows_off)), w[3], rows_off)
+    return O.layer_norm(O.dropout(f, p, seeds[1], residual=n), gain[1])
+
+
+class Plain:
+    """The same in 64-bit torch operations."""
+
+    def __init__(self, rows, width, seeds, p):
+        self.keep = [keep_of(rows, width, p, s) for s in seeds]
+        self.turn = 0
+
+    @staticmethod
+    def grouped_matmul(x, w, offsets):
+        return x @ w[0].t()
+
+    @staticmethod
+    def rotary(x, positions, frequencies):
+        t = positions.double()[:, None] * frequencies
+        half = frequencies.shape[0]
+        a, b = x[..., :half], x[..., half:]
+        return torch.cat([a * t.cos()[:, None] - b * t.sin()[:, None], a * t.sin()[:, None] + b * t.cos()[:, None]], -1)
+
+    @staticmethod
+    def attention(q, k, v, qo, ko, causal):
+        out = []
+        for a, b in sequences(qo, ko, None):
+            for h in range(q.shape[1]):
+                s = q[a, h] @ k[b, h // 2].t() * q.shape[2] ** -0.5
+                s = s.masked_fill(torch.ones_like(s, dtype=torch.bool).triu(1), -INF)
+                out.append(torch.softmax(s, 1) @ v[b, h // 2])
+        n = q.shape[1]
+        return torch.cat([torch.stack(out[i:i + n], 1) for i in range(0, len(out), n)])
+
+    def dropout(self, x, p, seed, residual):
+        keep, drop = self.keep[self.turn]
+        self.turn += 1
+        return residual + torch.where(keep, x * (65536 / (65536 - drop)), 0.0)
+
+    @staticmethod
+    def layer_norm(x, gain):
+        return torch.nn.functional.layer_norm(x, x.shape[1:], gain)
+
+
+def layer_inputs(dtype, rows=80, width=128):
+    g = gen(41)
+    lens = [33, 1, 46]
+    x = rand(g, rows, width, dtype=dtype)
+    w = [rand(g, 1, n, k, dtype=dtype, scale=k ** -0.5) for n, k in ((256, width), (width, 128), (192, width), (width, 192))]
+    gain = [rand(g, width, dtype=dtype, scale=0.1, shift=1.0) for _ in range(2)]
+    positions = torch.cat([torch.arange(n, device="cuda") for n in lens])
+    seeds = torch.randint(-(1 << 60), 1 << 60, (2, 2), generator=g, device="cuda")
+    dy = rand(g, rows, width, dtype=dtype)
+    return x, w, gain, offsets(lens), offsets([rows]), positions, seeds, dy
+
+
+def test_a_decoder_layer_and_its_gradients(ops):  # noqa: F811
+    """All operators together, as a layer of a model calls them, through torch.autograd, against 64 bits."""
+    x, w, gain, off, rows_off, positions, seeds, dy = layer_inputs(HF)
+    frequencies = ops.rotary_frequencies(32)
+    p = 0.25
+    mine = [t.clone().requires_grad_() for t in (x, *w, *gain)]
+    y = decoder_layer(ops, mine[0], mine[1:5], mine[5:], off, rows_off, positions, frequencies, seeds, p)
+    y.backward(dy)
+    plain = [t.double().requires_grad_() for t in (x, *w, *gain)]
+    want = decoder_layer(Plain(*x.shape, seeds, p), plain[0], plain[1:5], plain[5:], off, rows_off, positions, frequencies, seeds, p)
+    want.backward(dy.double())
+    # each of about a dozen operators on the way rounds its results to half precision, by 2^-11 of their size at most; norms
+    # over the whole tensor, where these roundings are independent, stay below their sum
+    assert (y.double() - want).norm() <= 12 * U[HF] * want.norm()
+    for m, t in zip(mine, plain):
+        assert (m.grad.double() - t.grad).norm() <= 24 * U[HF] * t.grad.norm()
+
+
+def passes(ops, x, w, off, few_off, rows_off, positions, frequencies, seeds, dy, p=0.25):  # noqa: F811
+    """The passes of the first half of that layer, forward and backward, as a captured training step makes them."""
+    rows = x.shape[0]
+    qkv = ops.grouped_matmul_forward(x, w[0], rows_off).view(rows, 8, 32)
+    qk = ops.rotary_forward(qkv[:, :6], positions, frequencies)
+    ctx, lse = ops.attention_forward(qk[:, :4], qk[:, 4:], qkv[:, 6:], off, off, causal=True)
+    y = ops.grouped_matmul_forward(ctx.view(rows, 128), w[1], rows_off)
+    z = ops.dropout_forward(y, p, seeds[0], residual=x)
+    d = ops.dropout_backward(dy, p, seeds[0])
+    dctx, dw = ops.grouped_matmul_backward(d, ctx.view(rows, 128), w[1], rows_off)
+    dq, dk, dv = ops.attention_backward(dctx.view(rows, 4, 32), qk[:, :4], qk[:, 4:], qkv[:, 6:], ctx, lse, off, off, causal=True)
+    dqk = ops.rotary_backward(torch.cat([dq, dk], 1), positions, frequencies)
+    few, few_lse = ops.attention_forward(qk[:2, :4], qk[:, 4:], qkv[:, 6:], few_off, off, causal=False)
+    return [qkv, qk, ctx, lse, z, dctx, dw, dq, dk, dv, dqk, few, few_lse]
+
+
+def test_another_stream_and_graph_replays_of_these(ops):  # noqa: F811
+    """The same results on a side stream, and from every replay of a captured graph, with other seeds too."""
+    x, w, _, off, rows_off, positions, seeds, dy = layer_inputs(BF)
+    frequencies, few_off = ops.rotary_frequencies(32), offsets([2, 0, 0])
+
+    def run():
+        return passes(ops, x, w, off, few_off, rows_off, positions, frequencies, seeds, dy)
+
+    want = [t.clone() for t in run()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = run()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.cuda.stream(side):
+        graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = run()
+        with torch.cuda.graph(other, stream=side):   # a second graph, with workspaces of its own
+            out2 = run()
+    torch.cuda.synchronize()
+    kept = x.clone()
+    for turn in range(4):
+        x.copy_(kept * (1 + turn))
+        seeds.add_(turn)
+        eager = [t.clone() for t in run()]
+        for t in out + out2:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        other.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager)), turn
+        assert all(torch.equal(a, b) for a, b in zip(out2, eager)), turn
+
+
+def test_shares_in_a_captured_graph(ops):  # noqa: F811
+    """One token over many kept keys: the shares' workspace is the graph's own."""
+    q, k, v, qo, ko, kl = make(51, [1, 1], [3000, 1], 8, 2, 64, BF, room=1096)
+    want = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl, causal=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out, lse = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl, causal=True)
+    for n in (3000, 1, 0, 4096, 77):   # lengths change between replays
+        kl[0] = n
+        k.view(-1)[:] = k.nan_to_num(0.25).view(-1)
+        v.view(-1)[:] = v.nan_to_num(0.25).view(-1)
+        want = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl, causal=True)
+        out.fill_(float("nan")), lse.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1]), n
+        check_forward((out, lse), q, k, v, qo, ko, kl, True)
+
+
+def test_runs_agree(ops):  # noqa: F811
+    """No sum depends on scheduling: the same bits from every run."""
+    q, k, v, qo, ko, _ = make(61, [700, 333, 1], [700, 333, 1], 8, 2, 64, BF)
+    dout = rand(gen(62), *q.shape, dtype=BF)
+    first = None
+    for _ in range(5):
+        out, lse = ops.attention_forward(q, k, v, qo, ko, causal=True)
+        got = [out, lse, *ops.attention_backward(dout, q, k, v, out, lse, qo, ko, causal=True)]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+@pytest.mark.parametrize("dim,layout", [(64, ""), (128, ""), (24, "odd"), (128, "odd")])
+def test_values_that_are_not_finite_stay_where_they_may(ops, dim, layout):  # noqa: F811
+    """What lies past a sequence's length or in other sequences and heads has no influence, whatever it is."""
+    g = gen(71)
+    q, k, v, qo, ko, kl = make(71, [70, 3, 50], [40, 90, 64], 4, 2, dim, BF, room=30, layout=layout)
+    clean = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl)
+    dout = rand(g, *q.shape, dtype=BF)
+    clean += ops.attention_backward(dout, q, k, v, *clean, qo, ko, k_lengths=kl)
+    for bad in (INF, -INF, float("nan"), torch.finfo(BF).min):
+        q2, k2, v2, d2 = (t.clone() for t in (q, k, v, dout))
+        owned = torch.zeros(k.shape[0], dtype=torch.bool, device="cuda")
+        for _, b in sequences(qo, ko, kl):
+            owned[b] = True
+        k2[~owned], v2[~owned] = bad, bad
+        # the second sequence, and the second pair of heads everywhere
+        a, b = sequences(qo, ko, kl)[1]
+        q2[a], k2[b], v2[b], d2[a] = bad, bad, bad, bad
+        q2[:, 2:], k2[:, 1:], v2[:, 1:], d2[:, 2:] = bad, bad, bad, bad
+        got = ops.attention_forward(q2, k2, v2, qo, ko, k_lengths=kl)
+        got += ops.attention_backward(d2, q2, k2, v2, *got, qo, ko, k_lengths=kl)
+        rows = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
+        rows[a] = False
+        keys = torch.ones(k.shape[0], dtype=torch.bool, device="cuda")
+        keys[b] = False
+        assert torch.equal(got[0][rows, :2], clean[0][rows, :2]) and torch.equal(got[1][:2, rows], clean[1][:2, rows])
+        assert torch.equal(got[2][rows, :2], clean[2][rows, :2])
+        for i in (3, 4):
+            assert torch.equal(got[i][keys, :1], clean[i][keys, :1])
+            assert (got[i][keys & ~owned] == 0).all()
+
+
+def test_scores_of_any_size(ops):  # noqa: F811
+    """Large scores overflow nothing, ties are shared evenly, and one far above the rest takes all."""
+    for scale in (1e-6, 1.0, 100.0):
+        q, k, v, qo, ko, _ = make(81, [130], [200], 2, 2, 64, HF)
+        check_forward(ops.attention_forward(q, k, v, qo, ko, scale=scale), q, k, v, qo, ko, scale=scale)
+        q, k, v, qo, ko, _ = make(81, [3], [2000], 2, 2, 64, HF)
+        check_forward(ops.attention_forward(q, k, v, qo, ko, scale=scale), q, k, v, qo, ko, scale=scale)
+    # rising scores move the reference again and again
+    q, k, v, qo, ko, _ = make(82, [100], [1000], 1, 1, 32, BF)
+    q[:] = 1.0
+    k[:] = torch.linspace(-8, 8, 1000, device="cuda").to(BF)[:, None, None]
+    got = ops.attention_forward(q, k, v, qo, ko, scale=2.0)
+    check_forward(got, q, k, v, qo, ko, scale=2.0)
+    k[:] = 0.0
+    got = ops.attention_forward(q, k, v, qo, ko)   # all alike: the mean
+    assert torch.allclose(got[0].double(), v.double().mean(0).expand(100, 1, 32), atol=2.0 ** -7, rtol=2.0 ** -8)
+    assert torch.allclose(got[1], torch.full((), math.log(1000), device="cuda"), rtol=4 * E)
+
+
+def test_attention_past_32_bits(ops):  # noqa: F811
+    """Rows whose elements are more than 2^31 apart, in the few-query and the many-query kernel and the gradient."""
+    heads, dim, keys = 16, 128, (1 << 31) // (16 * 128) + 3000
+    g = gen(91)
+    kv = torch.zeros(keys, heads, dim, dtype=BF, device="cuda")
+    last = slice(keys - 700, keys)
+    kv[last] = rand(g, 700, heads, dim, dtype=BF)
+    small = kv[last].contiguous()
+    so = offsets([0, 700, 0])
+    for n in (1, 300, 2200):   # shares, shares of longer tiles, whole tiles of 128 queries
+        q = rand(g, n, heads, dim, dtype=BF)
+        qo = offsets([0, n, 0])
+        ko = torch.tensor([0, keys - 700, keys, keys], dtype=torch.int64, device="cuda").int()
+        got = ops.attention_forward(q, kv, kv, qo, ko, causal=True)
+        check_forward(got, q, small, small, qo, so, None, True)
+        if n > 1:
+            dq, dk, dv = ops.attention_backward(q, q, kv, kv, *got, qo, ko, causal=True)
+            check_backward((dq, dk[last], dv[last]), q, q, small, small, *got, qo, so, None, True)
+            assert (dk[:keys - 700] == 0).all() and (dv[:keys - 700] == 0).all()
+    del kv
+    # the rotation and dropout at the end of a buffer of that size
+    x = torch.zeros((1 << 31) // 2048 + 5, 16, 128, dtype=BF, device="cuda")
+    x[-3:] = rand(g, 3, 16, 128, dtype=BF)
+    positions = torch.arange(x.shape[0], device="cuda")
+    f = ops.rotary_frequencies(128)
+    y = ops.rotary_forward(x, positions, f)
+    assert torch.equal(y[-3:], ops.rotary_forward(x[-3:].contiguous(), positions[-3:], f)) and (y[:-3] == 0).all()
+    seed = torch.tensor([5, 6], device="cuda")
+    flat = x.view(-1, 2048)
+    z = ops.dropout_forward(flat, 0.5, seed)
+    keep = z[-3:] != 0
+    assert torch.equal(z[-3:], torch.where(keep, flat[-3:] * 2, 0)) and 2000 < int(keep.sum()) < 4100
+    call = (flat.shape[0] - 1) * 256   # the last row's first call: beyond 2^27 calls and 2^31 elements
+    from test_attention import philox
+    words = philox([call, 0, 6, 0], [5, 0])
+    assert [bool(b) for b in z[-1, :8] != 0] == [n >= 32768 for w in words for n in (w & 0xffff, w >> 16)]
+
+
+def test_offsets_out_of_rule(ops):  # noqa: F811
+    """Offsets and lengths outside their ranges are taken as the nearest within; where they decrease, rows of others are left
+    alone at least: nothing outside the outputs is written and nothing hangs."""
+    q, k, v, qo, ko, _ = make(101, [40, 60], [70, 50], 2, 1, 64, BF)
+    want = ops.attention_forward(q, k, v, qo, ko, k_lengths=torch.tensor([70, 50], dtype=torch.int32, device="cuda"))
+    qx = torch.tensor([-5, 40, 1 << 30], dtype=torch.int32, device="cuda")
+    kx = torch.tensor([-(1 << 31), 70, 121], dtype=torch.int32, device="cuda")
+    kl = torch.tensor([71, 1 << 30], dtype=torch.int32, device="cuda")
+    got = ops.attention_forward(q, k, v, qx, kx, k_lengths=kl)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    dout = rand(gen(102), *q.shape, dtype=BF)
+    for a, b in zip(ops.attention_backward(dout, q, k, v, *got, qx, kx, k_lengths=kl), ops.attention_backward(dout, q, k, v, *want, qo, ko)):
+        assert torch.equal(a, b)
+    kl = torch.tensor([-3, 0], dtype=torch.int32, device="cuda")
+    got = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl)
+    assert (got[0] == 0).all() and (got[1] == -INF).all()
+
+
+def test_refused_tensors_of_these(ops):  # noqa: F811
+    q, k, v, qo, ko, kl = make(111, [4, 4], [6, 6], 4, 2, 8, BF, room=2)
+    out, lse = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl)
+    x, pos, f = q, torch.zeros(8, dtype=torch.int64, device="cuda"), ops.rotary_frequencies(8)
+    m, seed = torch.zeros(4, 8, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    A, B, R, D = ops.attention_forward, ops.attention_backward, ops.rotary_forward, ops.dropout_forward
+    for call in (
+            lambda: A(q.float(), k.float(), v.float(), qo, ko), lambda: A(q, k.half(), v, qo, ko), lambda: A(q, k, v[:-1], qo, ko),
+            lambda: A(q, k[:, :, :7], v, qo, ko), lambda: A(q[:, :3], k, v, qo, ko), lambda: A(q[0], k, v, qo, ko),
+            lambda: A(q, k, v, qo[:2], ko), lambda: A(q, k, v, qo, ko.long()), lambda: A(q, k, v, qo.float(), ko), lambda: A(q, k, v, qo[:1], ko[:1]),
+            lambda: A(q, k, v, qo, ko, k_lengths=kl[:1]), lambda: A(q, k, v, qo, ko, k_lengths=kl.long()), lambda: A(q, k, v, qo.cpu(), ko),
+            lambda: A(q, k.cpu(), v, qo, ko), lambda: A(q, k, v, qo, ko, scale=0.0), lambda: A(q, k, v, qo, ko, scale=-1.0),
+            lambda: A(q.transpose(1, 2), k, v, qo, ko), lambda: A(q[:, :1].expand(8, 4, 8), k, v, qo, ko), lambda: A(q[:1].expand(8, 4, 8), k, v, qo, ko),
+            lambda: A(q[..., :0], k[..., :0], v[..., :0], qo, ko),
+            lambda: B(out[:7], q, k, v, out, lse, qo, ko), lambda: B(out, q, k, v, out.half(), lse, qo, ko), lambda: B(out, q, k, v, out, lse.t(), qo, ko),
+            lambda: B(out, q, k, v, out, lse.double(), qo, ko), lambda: B(out, q, k, v, out, lse[:, ::2], qo, ko),
+            lambda: R(x, pos[:7], f), lambda: R(x, pos.float(), f), lambda: R(x, pos, f.float()), lambda: R(x, pos, f[:0]), lambda: R(x, pos, f[None]),
+            lambda: R(x, pos, ops.rotary_frequencies(10)), lambda: R(x.double(), pos, f), lambda: R(x[0], pos, f), lambda: R(x, pos, f, out=x.half()),
+            lambda: R(x, pos, f, out=x[:7]), lambda: R(x, pos.cpu(), f),
+            lambda: D(m, -0.1, seed), lambda: D(m, 1.5, seed), lambda: D(m, float("nan"), seed), lambda: D(m, 0.1, seed[:1]), lambda: D(m, 0.1, seed.int()),
+            lambda: D(m, 0.1, seed.cpu()), lambda: D(m, 0.1, seed, residual=m.half()), lambda: D(m, 0.1, seed, residual=m[:3]), lambda: D(m[0], 0.1, seed),
+            lambda: D(m.t(), 0.1, seed)):
+        assert refused(ops, call)
+    from paper_2407_04001_amd import PaseError
+    wide = torch.zeros(2, 1, 136, dtype=BF, device="cuda")
+    with pytest.raises(PaseError) as e:
+        A(wide, wide, wide, offsets([2]), offsets([2]))
+    assert e.value.status == 5   # too large
+
+
+def test_nothing_to_attend(ops):  # noqa: F811
+    """No rows, no keys, no heads' worth of either: outputs of 0."""
+    z = torch.zeros(0, 2, 16, dtype=BF, device="cuda")
+    q = rand(gen(121), 5, 4, 16, dtype=BF)
+    none, five = offsets([0]), offsets([5])
+    out, lse = ops.attention_forward(q, z, z, five, none)
+    assert (out == 0).all() and (lse == -INF).all()
+    dq, dk, dv = ops.attention_backward(q, q, z, z, out, lse, five, none)
+    assert (dq == 0).all() and dk.shape == (0, 2, 16)
+    zq, k = z.new_empty(0, 4, 16), rand(gen(122), 7, 2, 16, dtype=BF)
+    out, lse = ops.attention_forward(zq, k, k, none, offsets([7]))
+    assert out.shape == (0, 4, 16) and lse.shape == (4, 0)
+    dq, dk, dv = ops.attention_backward(zq, zq, k, k, out, lse, none, offsets([7]))
+    assert dq.shape == (0, 4, 16) and (dk == 0).all() and (dv == 0).all()
+    empty = torch.zeros(0, dtype=torch.int64, device="cuda")
+    assert ops.rotary_forward(zq, empty, ops.rotary_frequencies(16)).shape == (0, 4, 16)
+    assert ops.dropout_forward(torch.zeros(0, 9, device="cuda"), 0.5, torch.zeros(2, dtype=torch.int64, device="cuda")).shape == (0, 9)
+
+
+def test_differentiable_forms(ops):  # noqa: F811
+    """Gradients through autograd are the passes' own, also for expanded and strided gradients, and second ones are refused."""
+    q, k, v, qo, ko, kl = make(131, [20, 30], [25, 35], 4, 2, 32, HF, room=7)
+    k, v = k.nan_to_num(0.0), v.nan_to_num(0.0)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    out = ops.attention(*leaves, qo, ko, k_lengths=kl, causal=True, scale=0.3)
+    want, lse = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl, causal=True, scale=0.3)
+    assert torch.equal(out, want)
+    for dout in (rand(gen(1), *q.shape, dtype=HF), torch.ones((), dtype=HF, device="cuda").expand(q.shape), rand(gen(2), 32, 4, 50, dtype=HF).permute(2, 1, 0)):
+        got = torch.autograd.grad(out, leaves, dout, retain_graph=True)
+        ref = ops.attention_backward(dout.contiguous(), q, k, v, want, lse, qo, ko, k_lengths=kl, causal=True, scale=0.3)
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    f, pos = ops.rotary_frequencies(32), torch.arange(50, device="cuda")
+    x = q.clone().requires_grad_()
+    y = ops.rotary(x, pos, f, interleaved=True, magnitude=1.5)
+    dy = torch.ones((), dtype=HF, device="cuda").expand(q.shape)
+    assert torch.equal(torch.autograd.grad(y, x, dy, retain_graph=True)[0], ops.rotary_backward(dy.contiguous(), pos, f, interleaved=True, magnitude=1.5))
+    seed = torch.tensor([1, 2], device="cuda")
+    m, r = rand(gen(3), 50, 33).requires_grad_(), rand(gen(4), 50, 33).requires_grad_()
+    z = ops.dropout(m, 0.3, seed, residual=r)
+    seed.add_(1)   # the backward pass takes the seed that the forward pass had
+    dm, dr = torch.autograd.grad(z, (m, r), torch.ones((), device="cuda").expand(50, 33), retain_graph=True)
+    assert torch.equal(dr, torch.ones_like(r)) and torch.equal(dm, ops.dropout_backward(torch.ones(50, 33, device="cuda"), 0.3, torch.tensor([1, 2], device="cuda")))
+    for out, leaf in ((ops.attention(*leaves, qo, ko, k_lengths=kl), leaves[0]), (ops.rotary(x, pos, f), x), (ops.dropout(m, 0.3, seed), m)):
+        grad, = torch.autograd.grad(out.square().sum(), leaf, create_graph=True)
+        with pytest.raises(RuntimeError):
+            grad.sum().backward()
+
+
+def test_rotation_in_place_is_known_to_autograd(ops):  # noqa: F811
+    x = rand(gen(141), 6, 2, 8).requires_grad_()
+    h = x * 2
+    y = h.square().sum()   # saved h
+    ops.rotary_forward(h.detach(), torch.arange(6, device="cuda"), ops.rotary_frequencies(8), out=h.detach())
+    with pytest.raises(RuntimeError):
+        y.backward()
+
+
+def test_outputs_keep_to_their_rows_and_heads(ops):  # noqa: F811
+    """Through the C ABI with wider outputs: what lies between heads and rows is untouched."""
+    L = ops.load()
+    q, k, v, qo, ko, _ = make(151, [70, 30], [50, 61], 4, 2, 40, BF)
+    rows, keys, mark = q.shape[0], k.shape[0], 7.5
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def room(rows, heads):
+        return torch.full((rows + 2, heads + 1, 43), mark, dtype=BF, device="cuda")
+
+    def inside(t):
+        return t[1:-1, :-1, :40]
+
+    def untouched(t):
+        u = t.clone()
+        inside(u)[:] = mark
+        return bool((u == mark).all())
+
+    def arg(t):
+        return t.data_ptr(), t.stride(0), t.stride(1)
+
+    out, lse = room(rows, 4), torch.empty(4, rows, device="cuda")
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    ref = ops.attention_forward(q, k, v, qo, ko, causal=True)
+    assert L.pase_attention_forward(0, rows, keys, 2, 4, 2, 40, *arg(q), *arg(k), *arg(v), qo.data_ptr(), ko.data_ptr(), None, 0, 1, 40 ** -0.5,
+                                    *arg(inside(out)), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream) == 0
+    assert torch.equal(inside(out), ref[0]) and torch.equal(lse, ref[1]) and untouched(out)
+    dq, dk, dv = room(rows, 4), room(keys, 2), room(keys, 2)
+    assert L.pase_attention_backward(0, rows, keys, 2, 4, 2, 40, *arg(q), *arg(q), *arg(k), *arg(v), *arg(inside(out)), lse.data_ptr(), qo.data_ptr(),
+                                     ko.data_ptr(), None, 0, 1, 40 ** -0.5, *arg(inside(dq)), *arg(inside(dk)), *arg(inside(dv)), ws.data_ptr(), ws.numel(), stream) == 0
+    for t, want in zip((dq, dk, dv), ops.attention_backward(q, q, k, v, *ref, qo, ko, causal=True)):
+        assert torch.equal(inside(t), want) and untouched(t)
+    y, pos, f = room(rows, 4), torch.arange(rows, device="cuda"), ops.rotary_frequencies(24)
+    assert L.pase_rotary(0, rows, 4, 40, 24, 1, 0, *arg(q), pos.data_ptr(), 1, f.data_ptr(), 1.0, *arg(inside(y)), stream) == 0
+    assert torch.equal(inside(y), ops.rotary_forward(q, pos, f, interleaved=True)) and untouched(y)
+    m, z, seed = rand(gen(9), rows, 40, dtype=BF), torch.full((rows, 43), mark, dtype=BF, device="cuda"), torch.tensor([3, 4], device="cuda")
+    assert L.pase_dropout(0, rows, 40, m.data_ptr(), 40, None, 0, 0.5, seed.data_ptr(), z.data_ptr(), 43, stream) == 0
+    assert torch.equal(z[:, :40], ops.dropout_forward(m, 0.5, seed)) and (z[:, 40:] == mark).all()
