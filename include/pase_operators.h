@@ -153,7 +153,7 @@ pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t 
  * out 0 and lse -inf.
  * dtype: PASE_BF16 or PASE_FP16, of all matrices.  q, out: [rows, heads, dim], k, v: [key_rows,
  * kv_heads, dim], dim up to PASE_ATTENTION_MAX_DIM; ld* is the distance between
- * rows, hs* between heads (16-byte aligned rows and heads, and a dim that is a multiple of 8, are
+ * rows, hs* between heads (an even dim, and rows and heads that are 4-byte aligned, are much
  * faster).  lse: fp32 [heads, rows].  Offsets and lengths: device arrays of one type,
  * int32 (offsets_64 = 0) or int64 (1), offsets not decreasing and within 0..rows, 0..key_rows, lengths
  * within their ranges.  They are read on the device only and taken as the nearest

@@ -147,11 +147,15 @@ template <typename T> __device__ __forceinline__ Pack<T> load_chunk(const T *row
     return r.p;
 }
 
+// How tiles are loaded: through registers, or from HBM to LDS without (rows 4-byte aligned, dim even; a buffer's
+// range ends with the last row), where a chunk that dim cuts (no multiple of 8) then holds what
+// follows the head in memory until trim(), which its loader calls once it has arrived.
+enum Load { kThrough, kDirect, kCut };
+
 // Loads ROWS rows of a head, D elements of each (0 past `dim` and past the rows that
-// exist), by WAVES waves: from HBM to LDS without registers where rows are 4-byte aligned
-// and dim a multiple of 8 (DIRECT; the buffer's range ends with the last row), else
-// through them.
-template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
+// exist), by WAVES waves.
+template <typename T, int D, int ROWS, int WAVES, Load LOAD> struct Feed {
+    static constexpr bool DIRECT = LOAD != kThrough, CUT = LOAD == kCut;
     static constexpr int kChunks = D / 8, N = ROWS * kChunks / (64 * WAVES);
     static_assert(N >= 1 && ROWS * kChunks == N * 64 * WAVES, "whole loads");
     // A wave's load takes a kilobyte, kPeriod of which are 16 rows, after which the fold repeats: of a
@@ -194,6 +198,15 @@ template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
             }
         }
     }
+    __device__ __forceinline__ void trim(char *lds) const {
+        if (LOAD != kCut) return;
+#pragma unroll
+        for (int n = 0; n < N; n++) {
+            const int q = chunk(n), c = q % kChunks ^ fold<D>(q / kChunks);
+            if (c == dim / 8)
+                for (int e = dim % 8; e < 8; e += 2) *reinterpret_cast<uint32_t *>(lds + q * 16 + e * 2) = 0;
+        }
+    }
     __device__ __forceinline__ void store(char *lds) {
         if (!DIRECT)
 #pragma unroll
@@ -201,10 +214,13 @@ template <typename T, int D, int ROWS, int WAVES, bool DIRECT> struct Feed {
     }
 };
 
-// The loads of a tile have arrived, and every wave is past its reads of the one before.
-template <bool DIRECT> __device__ __forceinline__ void arrive() {
-    if (DIRECT) {
-        wait_loads<0>();
+// The loads of a step of two tiles have arrived, but for the last LEFT of this wave's, and every wave is
+// past its reads of the step before.
+template <int LEFT, typename F> __device__ __forceinline__ void arrive(const F &a, const F &b, char *lds, int size) {
+    if constexpr (F::DIRECT) {
+        wait_loads<LEFT>();
+        a.trim(lds), b.trim(lds + size);
+        if (F::CUT) wait_loads<63>();   // LDS alone
         barrier();
     } else {
         __syncthreads();
@@ -386,8 +402,8 @@ template <typename T, int D, int KT> struct Softmax {
 };
 
 // 128 queries a workgroup, 64 keys a step, keys and values two steps deep in LDS.
-template <typename T, int D, bool DIRECT>
-__global__ __launch_bounds__(256, D == 128 ? 2 : DIRECT ? 4 : 3) void k_forward(Attention a) {
+template <typename T, int D, Load LOAD>
+__global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k_forward(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
     constexpr int WAVES = 4, BM = 128, KT = 64, kTile = KT * D * 2;
     __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
@@ -419,7 +435,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : DIRECT ? 4 : 3) void k_forward(
 
     const float c = a.scale * kLog2e;
     Softmax<T, D, KT> softmax;
-    Feed<T, D, KT, WAVES, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
+    Feed<T, D, KT, WAVES, LOAD> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
     const Reader<T, D> read;
     const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
     const auto load = [&](int t, char *to) {
@@ -430,7 +446,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : DIRECT ? 4 : 3) void k_forward(
     if (tiles) load(0, lds[0]), store(lds[0]);
     for (int t = 0; t < tiles; t++) {
         const int at = t & 1;
-        arrive<DIRECT>();
+        arrive<0>(fk, fv, lds[at], kTile);
         if (t + 1 < tiles) load(t + 1, lds[at ^ 1]);
         if (t * KT < any_sees) {
             const uint32_t tile = lds_address(lds[at]), kt = read.rows_of(tile), vt = read.columns_of(tile + kTile);
@@ -452,7 +468,8 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : DIRECT ? 4 : 3) void k_forward(
 // loaded where this one's were once they are read, values likewise, so that a wave always
 // has loads on their way and LDS holds two workgroups.  The waves' outputs are joined at the end; where tiles are still too few, a.splits workgroups share a tile's keys and leave
 // their outputs and log-sum-exps for k_join.
-template <typename T, int D, bool DIRECT> __global__ __launch_bounds__(256, 2) void k_forward_few(Attention a) {
+template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) void k_forward_few(Attention a) {
+    constexpr bool DIRECT = LOAD != kThrough;
     typedef typename Mfma<T>::Frag Frag;
     constexpr int WAVES = 4, BM = 32, KT = 32, kTile = KT * D * 2;
     constexpr int kOut = BM * D * 4 + BM * 8;   // a wave's output, references and sums
@@ -474,7 +491,7 @@ template <typename T, int D, bool DIRECT> __global__ __launch_bounds__(256, 2) v
     const int t0 = (int)(tiles * part / a.splits) + wave, t1 = (int)(tiles * (part + 1) / a.splits);
 
     const float c = a.scale * kLog2e;
-    Feed<T, D, KT, 1, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
+    Feed<T, D, KT, 1, LOAD> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
     const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
     char *const kt = lds[wave], *const vt = kt + kTile;
     const auto load_keys = [&](int t) {
@@ -501,6 +518,7 @@ template <typename T, int D, bool DIRECT> __global__ __launch_bounds__(256, 2) v
     const Reader<T, D> read;
     for (int t = t0; t < t1; t += WAVES) {
         done(Other{});
+        fk.trim(kt);
         softmax.step(
             read.rows_of(lds_address(kt)), read.columns_of(lds_address(vt)), q, seen - t * KT, (t + 1) * KT > all_see, c,
             [&] { done(All{}), load_keys(t + WAVES); },
@@ -654,12 +672,44 @@ __device__ __forceinline__ float exponent_of(float lse) {   // rows without keys
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
 }
 
+// The sum of a result over teams of `waves` waves: every team but `to` gives its own, in LDS, which `to`
+// then adds to its own in the teams' order.  A part is 128 D bytes for each wave.
+template <int D> struct Join {
+    char *lds;
+    int team, wave, waves;
+
+    __device__ __forceinline__ f32x4 &at(int part, int quad) const {
+        return *reinterpret_cast<f32x4 *>(lds + ((part * waves * D / 8 + quad * waves + wave) * 64 + (threadIdx.x & 63)) * 16);
+    }
+    __device__ __forceinline__ void give(const f32x16 (&x)[D / 32], int to) const {
+        if (team == to) return;
+#pragma unroll
+        for (int d = 0; d < D / 32; d++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                at(team - (team > to), d * 4 + e) = f32x4{x[d][4 * e], x[d][4 * e + 1], x[d][4 * e + 2], x[d][4 * e + 3]};
+    }
+    __device__ __forceinline__ void take(f32x16 (&x)[D / 32], int to, int teams) const {
+        if (team != to) return;
+#pragma unroll 1
+        for (int part = 0; part < teams - 1; part++)
+#pragma unroll
+            for (int d = 0; d < D / 32; d++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const f32x4 o = at(part, d * 4 + e);
+#pragma unroll
+                    for (int j = 0; j < 4; j++) x[d][4 * e + j] += o[j];
+                }
+    }
+};
+
 // Queries along the lanes, as in the forward pass.
-template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(256, 2) void k_queries_grad(Attention a) {
+template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) void k_queries_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
-    constexpr int WAVES = 4, BM = 128, kTile = KT * D * 2;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
-    static_assert(2 * 2 * kTile >= BM * D * 2, "the gradient passes the same LDS");
+    constexpr int WAVES = 4, BM = 128, KT = D == 128 && LOAD == kThrough ? 32 : 64, kTile = KT * D * 2, kStep = 2 * kTile;
+    static_assert(2 * kStep >= BM * D * 2, "the gradient passes the same LDS");
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
     const uint32_t item = a.first + blockIdx.x;
     const int kv_head = (int)(item % a.kv_heads), tile = a.tiles - 1 - (int)(item / a.kv_heads);
     const int group = a.heads / a.kv_heads;
@@ -694,25 +744,26 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
     const int seen = sq.seen(a, i);
     const int all_see = busy ? uniform(sq.seen(a, qs.index(wave * 32))) : 0;
     const int any_sees = busy ? uniform(sq.seen(a, qs.index(w_last))) : 0;
-    const int tiles = (uniform(sq.seen(a, qs.index(last))) + KT - 1) / KT;
+    const int steps = (uniform(sq.seen(a, qs.index(last))) + KT - 1) / KT;
 
     const float c = a.scale * kLog2e;
     f32x16 dq[D / 32] = {};
-    Feed<T, D, KT, WAVES, DIRECT> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
+    Feed<T, D, KT, WAVES, LOAD> fk(a.k.ld, a.dim), fv(a.v.ld, a.dim);
     const Reader<T, D> read;
     const T *k = head_of<T>(a.k, sq.k_lo, kv_head), *v = head_of<T>(a.v, sq.k_lo, kv_head);
-    const auto load = [&](int t, char *to) {
+    const auto step_at = [&](int n) { return lds + (n & 1) * kStep; };
+    const auto load = [&](int t) {
+        char *to = step_at(t);
         fk.load(k + (int64_t)t * KT * a.k.ld, sq.keys - t * KT, to);
         fv.load(v + (int64_t)t * KT * a.v.ld, sq.keys - t * KT, to + kTile);
     };
-    const auto store = [&](char *to) { fk.store(to), fv.store(to + kTile); };
-    if (tiles) load(0, lds[0]), store(lds[0]);
-    for (int t = 0; t < tiles; t++) {
-        const int at = t & 1;
-        arrive<DIRECT>();
-        if (t + 1 < tiles) load(t + 1, lds[at ^ 1]);
+    const auto store = [&](int t) { fk.store(step_at(t)), fv.store(step_at(t) + kTile); };
+    if (steps) load(0), store(0);
+    for (int t = 0; t < steps; t++) {
+        arrive<0>(fk, fv, step_at(t), kTile);
+        if (t + 1 < steps) load(t + 1);
         if (t * KT < any_sees) {
-            const uint32_t tile = lds_address(lds[at]), kt = read.rows_of(tile), vt = read.rows_of(tile + kTile), kc = read.columns_of(tile);
+            const uint32_t tile = lds_address(step_at(t)), kt = read.rows_of(tile), vt = read.rows_of(tile + kTile), kc = read.columns_of(tile);
             const bool whole = (t + 1) * KT <= all_see;
 #pragma unroll
             for (int b = 0; b < KT / 32; b++) {
@@ -738,10 +789,10 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
                 }
             }
         }
-        if (t + 1 < tiles) store(lds[at ^ 1]);
+        if (t + 1 < steps) store(t + 1);
     }
     __syncthreads();
-    store_rows<T, D>(lds[0] + wave * 32 * D * 2, dq, lse2 == __builtin_inff(), a.scale, a.dim, [&](int r) -> T * {
+    store_rows<T, D>(lds + wave * 32 * D * 2, dq, lse2 == __builtin_inff(), a.scale, a.dim, [&](int r) -> T * {
         const int p = wave * 32 + r;
         return qs.has(p) ? out_of<T>(a.dq, sq.q_lo + qs.index(p), qs.head(p)) : nullptr;
     });
@@ -752,8 +803,9 @@ template <typename T, int D, int KT, bool DIRECT> __global__ __launch_bounds__(2
 // WAVES x 32 keys: the steps through the queries of all heads that share them, QT at a
 // time, go round the teams, whose sums are added at the end.
 // DIRECT: three steps in LDS, two on their way (two and one where LDS holds no more); else one, loaded where it is needed.
-template <typename T, int D, int QT, int WAVES, int TEAMS, bool DIRECT>
+template <typename T, int D, int QT, int WAVES, int TEAMS, Load LOAD>
 __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 3) void k_keys_grad(Attention a) {
+    constexpr bool DIRECT = LOAD != kThrough;
     typedef typename Mfma<T>::Frag Frag;
     constexpr int BM = WAVES * 32, kTile = QT * D * 2, kStats = QT * 8, kStep = 2 * kTile + kStats;
     constexpr int kSteps = !DIRECT ? 1 : D == 128 ? 2 : 3;
@@ -788,14 +840,18 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
     const int steps = (per * group + TEAMS - 1) / TEAMS;   // of either team; the second's last one may be empty
     if constexpr (kValuesInLds) {
         if (steps) {
-            Feed<T, D, BM, TEAMS * WAVES, DIRECT> fv(a.v.ld, a.dim);
+            Feed<T, D, BM, TEAMS * WAVES, LOAD> fv(a.v.ld, a.dim);
             fv.load(head_of<T>(a.v, sq.k_lo + first, kv_head), sq.keys - first, lds);
             fv.store(lds);
+            if (LOAD == kCut) {
+                wait_loads<0>();
+                fv.trim(lds);
+            }
         }
     } else {
         load_row<T, D>(v, head_of<T>(a.v, row, kv_head), there ? a.dim : 0);
     }
-    Feed<T, D, QT, WAVES, DIRECT> fq(a.q.ld, a.dim), fg(a.dout.ld, a.dim);
+    Feed<T, D, QT, WAVES, LOAD> fq(a.q.ld, a.dim), fg(a.dout.ld, a.dim);
     const Reader<T, D> read;
     char *const mine = lds + kValues + team * kSteps * kStep;
     const auto step_at = [&](int n) { return mine + (kSteps > 1 ? n % kSteps : 0) * kStep; };
@@ -831,10 +887,9 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
         if (DIRECT) {
             constexpr int kLoads = 2 * decltype(fq)::N + QT / 32;
             if (kSteps == 3 && n + 1 < steps)
-                wait_loads<kLoads>();
+                arrive<kLoads>(fq, fg, step_at(n), kTile);
             else
-                wait_loads<0>();
-            barrier();
+                arrive<0>(fq, fg, step_at(n), kTile);
             if (n + kSteps - 1 < steps) load(n + kSteps - 1);
         } else {
             __syncthreads();
@@ -894,38 +949,17 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
             }
         }
     }
-    // The first team adds up dv in the teams' order, the second dk; each stores its own.
-    const auto join = [&](int part, int quad) -> f32x4 & {
-        return *reinterpret_cast<f32x4 *>(lds + part * kPart + ((quad * WAVES + wave) * 64 + lane) * 16);
-    };
-    const auto give = [&](const f32x16(&x)[D / 32], int to) {
-#pragma unroll
-        for (int d = 0; d < D / 32; d++)
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                join(team - (team > to), d * 4 + e) = f32x4{x[d][4 * e], x[d][4 * e + 1], x[d][4 * e + 2], x[d][4 * e + 3]};
-    };
-    const auto take = [&](f32x16(&x)[D / 32]) {
-#pragma unroll 1
-        for (int part = 0; part < TEAMS - 1; part++)
-#pragma unroll
-            for (int d = 0; d < D / 32; d++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const f32x4 o = join(part, d * 4 + e);
-#pragma unroll
-                    for (int j = 0; j < 4; j++) x[d][4 * e + j] += o[j];
-                }
-    };
+    // the first team adds up dv, the second dk; each stores its own
+    const Join<D> join{lds, team, wave, WAVES};
     __syncthreads();
     if (TEAMS > 1) {
-        if (team != 0) give(dv, 0);
+        join.give(dv, 0);
         __syncthreads();
-        if (team == 0) take(dv);
+        join.take(dv, 0, TEAMS);
         __syncthreads();
-        if (team != 1) give(dk, 1);
+        join.give(dk, 1);
         __syncthreads();
-        if (team == 1) take(dk);
+        join.take(dk, 1, TEAMS);
         __syncthreads();
     }
     // keys of the range that do not count get 0 (their lanes hold what a key of zeros would)
@@ -956,26 +990,33 @@ template <typename K> int launch_items(K *kernel, int64_t items, int threads, vo
     return 0;
 }
 
-template <typename T> bool direct(const Attention &a, const HeadRows &x) {
-    return a.dim % 8 == 0 && reinterpret_cast<uintptr_t>(x.p) % 4 == 0 && x.ld % 2 == 0 && x.head_ld % 2 == 0;
+Load load_of(const Attention &a, const HeadRows &x, const HeadRows &y) {
+    const auto even = [](const HeadRows &x) {
+        return reinterpret_cast<uintptr_t>(x.p) % 4 == 0 && x.ld % 2 == 0 && x.head_ld % 2 == 0;
+    };
+    return a.dim % 2 || !even(x) || !even(y) ? kThrough : a.dim % 8 ? kCut : kDirect;
 }
 
-template <typename T, int D, bool DIRECT> int forward(Attention a, void *stream) {
+template <typename T, int D, Load LOAD> int forward(Attention a, void *stream) {
     const int64_t packed = (int64_t)a.rows * (a.heads / a.kv_heads);
     if (a.splits) {
         a.tiles = (int)tiles_of(packed, 32, a.sequences);
         const int64_t items = (int64_t)a.tiles * a.kv_heads * a.splits;
-        if (const int e = launch_items(k_forward_few<T, D, DIRECT>, items, 256, stream, a)) return e;
+        if (const int e = launch_items(k_forward_few<T, D, LOAD>, items, 256, stream, a)) return e;
         if (a.splits == 1) return 0;
         if (a.splits <= kFewShares) return launch_items(k_join_few<T>, ((int64_t)a.rows * a.heads + 7) / 8, 256, stream, a);
         return launch_items(k_join<T>, (int64_t)a.rows * a.heads * ((a.dim + 31) / 32), 256, stream, a);
     }
     a.tiles = (int)tiles_of(packed, 128, a.sequences);
-    return launch_items(k_forward<T, D, DIRECT>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
+    return launch_items(k_forward<T, D, LOAD>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
 }
 
 template <typename T, int D> int forward(const Attention &a, void *stream) {
-    return direct<T>(a, a.k) && direct<T>(a, a.v) ? forward<T, D, true>(a, stream) : forward<T, D, false>(a, stream);
+    switch (load_of(a, a.k, a.v)) {
+        case kDirect: return forward<T, D, kDirect>(a, stream);
+        case kCut: return forward<T, D, kCut>(a, stream);
+        default: return forward<T, D, kThrough>(a, stream);
+    }
 }
 
 template <typename T> int forward(const Attention &a, void *stream) {
@@ -983,20 +1024,40 @@ template <typename T> int forward(const Attention &a, void *stream) {
     return a.dim <= 64 ? forward<T, 64>(a, stream) : forward<T, 128>(a, stream);
 }
 
-template <typename T, int D> int backward(Attention a, void *stream) {
-    const int64_t packed = (int64_t)a.rows * (a.heads / a.kv_heads);
-    a.tiles = (int)tiles_of(packed, 128, a.sequences);
-    const int64_t items = a.rows ? (int64_t)a.tiles * a.kv_heads : 0;
-    if (const int e = direct<T>(a, a.k) && direct<T>(a, a.v) ? launch_items(k_queries_grad<T, D, 64, true>, items, 256, stream, a)
-                                                             : launch_items(k_queries_grad<T, D, D == 128 ? 32 : 64, false>, items, 256, stream, a))
-        return e;
-    a.tiles = (int)tiles_of(a.key_rows, 128, a.sequences);
-    const int64_t keys = a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0;
+template <typename T, int D, Load LOAD> int queries_grad(Attention a, void *stream) {
+    if (!a.rows) return 0;
+    a.tiles = (int)tiles_of((int64_t)a.rows * (a.heads / a.kv_heads), 128, a.sequences);
+    return launch_items(k_queries_grad<T, D, LOAD>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
+}
+
+// Tiles of 128 keys on one team, or of 64 on four.  Four share a tile's steps: with few tiles and many steps, as
+// where long sequences share heads, no CU waits long for the longest tile's (4 causal sequences, 16384
+// rows, 16 heads of 128 to 4: 736 us against 1185); with many tiles one team has two workgroups a CU (64 x
+// 256 rows, 16 heads of 64: 59 us against 100), and so with few steps, where joining costs as much (59 x 16
+// rows, 16 heads of 128, both kernels: 58 us against 82).
+template <typename T, int D, Load LOAD> int keys_grad(Attention a, void *stream) {
+    if (!a.key_rows) return 0;
     constexpr int QT = D == 32 ? 64 : 32;
-    if (!direct<T>(a, a.q) || !direct<T>(a, a.dout)) return launch_items(k_keys_grad<T, D, QT, 4, 1, false>, keys, 256, stream, a);
-    if ((int64_t)a.key_rows / 128 * a.kv_heads >= 4 * kCus) return launch_items(k_keys_grad<T, D, QT, 4, 1, true>, keys, 256, stream, a);
-    a.tiles = (int)tiles_of(a.key_rows, 64, a.sequences);
-    return launch_items(k_keys_grad<T, D, QT, 2, 4, true>, a.key_rows ? (int64_t)a.tiles * a.kv_heads : 0, 512, stream, a);
+    const int64_t some = a.key_rows < a.sequences ? a.key_rows : a.sequences, large = ((int64_t)a.key_rows + 127) / 128;
+    const int64_t steps = (int64_t)a.rows / a.sequences * (a.heads / a.kv_heads) / QT;
+    if constexpr (LOAD != kThrough) {
+        if ((large > some ? large : some) * a.kv_heads < 4 * kCus && steps >= 16) {
+            a.tiles = (int)tiles_of(a.key_rows, 64, a.sequences);
+            return launch_items(k_keys_grad<T, D, QT, 2, 4, LOAD>, (int64_t)a.tiles * a.kv_heads, 512, stream, a);
+        }
+    }
+    a.tiles = (int)tiles_of(a.key_rows, 128, a.sequences);
+    return launch_items(k_keys_grad<T, D, QT, 4, 1, LOAD>, (int64_t)a.tiles * a.kv_heads, 256, stream, a);
+}
+
+template <typename T, int D> int backward(const Attention &a, void *stream) {
+    const Load kv = load_of(a, a.k, a.v), q = load_of(a, a.q, a.dout);
+    if (const int e = kv == kDirect ? queries_grad<T, D, kDirect>(a, stream)
+                      : kv == kCut  ? queries_grad<T, D, kCut>(a, stream)
+                                    : queries_grad<T, D, kThrough>(a, stream))
+        return e;
+    if (kv == kThrough || q == kThrough) return keys_grad<T, D, kThrough>(a, stream);
+    return q == kDirect ? keys_grad<T, D, kDirect>(a, stream) : keys_grad<T, D, kCut>(a, stream);
 }
 
 template <typename T> int backward(const Attention &a, void *stream) {

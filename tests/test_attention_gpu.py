@@ -168,6 +168,11 @@ CASES = [
     ([65, 64], [65, 64], 2, 2, 64, True, {"layout": "odd"}),
     ([140], [201], 2, 1, 127, False, {"layout": "odd"}),
     ([66, 3], [200, 31], 4, 4, 32, True, {"room": 13}),
+    ([65, 64], [65, 64], 2, 2, 22, True, {"layout": "fused"}),   # heads that end inside 16 bytes, NaN behind them
+    ([140, 70], [201, 70], 4, 2, 118, True, {"layout": "fused", "room": 9}),
+    ([600], [600], 4, 1, 58, True, {"layout": "fused"}),         # few tiles, many steps
+    ([600], [600], 4, 1, 128, True, {"layout": "heads first"}),
+    ([550, 60], [600, 70], 4, 1, 126, False, {"layout": "fused", "room": 3}),
     ([5, 4, 0, 1], [64, 1, 3, 0], 4, 2, 64, True, {"room": 64, "wide": torch.int64}),
     ([17] * 70, [19] * 70, 2, 2, 16, True, {}),               # more sequences than a wave has lanes
     ([2] * 300 + [0] * 50 + [1] * 4100, [3] * 4450, 1, 1, 32, True, {}),
@@ -204,6 +209,8 @@ STEPS = [
     ([40], [4096], 3, 1, 32, {}),
     ([1] * 64, [300 + 7 * i for i in range(64)], 4, 1, 64, {"room": 5}),
     ([1] * 20, [128] * 20, 2, 1, 22, {"room": 200}),
+    ([1, 2], [3000, 900], 4, 2, 106, {"layout": "fused", "room": 5}),
+    ([1, 3], [2000, 900], 4, 2, 30, {"layout": "odd"}),
 ]
 
 
@@ -534,7 +541,7 @@ def test_runs_agree(ops):  # noqa: F811
         assert all(torch.equal(a, b) for a, b in zip(got, first))
 
 
-@pytest.mark.parametrize("dim,layout", [(64, ""), (128, ""), (24, "odd"), (128, "odd")])
+@pytest.mark.parametrize("dim,layout", [(64, ""), (128, ""), (24, "odd"), (128, "odd"), (22, ""), (22, "fused"), (118, "fused"), (60, "fused")])
 def test_values_that_are_not_finite_stay_where_they_may(ops, dim, layout):  # noqa: F811
     """What lies past a sequence's length or in other sequences and heads has no influence, whatever it is."""
     g = gen(71)
