@@ -262,15 +262,18 @@ template <typename T, int D> struct Reader {
     }
 };
 
-// Operand registers of the lane's own row: 16 s + 8 h on, for the D / 16 s; 0 past `n`.
+// Operand registers of the lane's own row: 16 s + 8 h on, for the D / 16 s; 0 past the n that it has.
 template <typename T, int D>
 __device__ __forceinline__ void load_row(typename Mfma<T>::Frag (&f)[D / 16], const T *p, int n) {
     const int h = threadIdx.x >> 5 & 1;
+    if (n == D) {
 #pragma unroll
-    for (int s = 0; s < D / 16; s++) {
-        const Pack<T> r = load_chunk(p, 16 * s + 8 * h, n);
-        f[s] = __builtin_bit_cast(typename Mfma<T>::Frag, r.v);
+        for (int s = 0; s < D / 16; s++)
+            f[s] = __builtin_bit_cast(typename Mfma<T>::Frag, reinterpret_cast<const Unaligned16<T> *>(p + 16 * s + 8 * h)->v);
+        return;
     }
+#pragma unroll
+    for (int s = 0; s < D / 16; s++) f[s] = __builtin_bit_cast(typename Mfma<T>::Frag, load_chunk(p, 16 * s + 8 * h, n).v);
 }
 
 // Eight consecutive registers of a result as an operand.
@@ -421,7 +424,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k
     const bool there = qs.has(mine);
     const int i = qs.index(mine), head = qs.head(mine);
     Frag q[D / 16];
-    load_row<T, D>(q, head_of<T>(a.q, there ? sq.q_lo + i : 0, head), there ? a.dim : 0);
+    load_row<T, D>(q, head_of<T>(a.q, there ? sq.q_lo + i : 0, there ? head : 0), a.dim);   // (a lane without a query: any row)
 
     // keys that the wave's first and last query, and the tile's last, see
     const int last = qs.rows - 1 - qs.first < BM - 1 ? qs.rows - 1 - qs.first : BM - 1;
@@ -513,7 +516,7 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     using All = std::integral_constant<int, 63>;   // LDS alone
     load_keys(t0), load_values(t0);
     Frag q[D / 16];
-    load_row<T, D>(q, head_of<T>(a.q, there ? sq.q_lo + i : 0, head), there ? a.dim : 0);
+    load_row<T, D>(q, head_of<T>(a.q, there ? sq.q_lo + i : 0, there ? head : 0), a.dim);   // (a lane without a query: any row)
     Softmax<T, D, KT> softmax;
     const Reader<T, D> read;
     for (int t = t0; t < t1; t += WAVES) {
@@ -719,25 +722,7 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     if (tile < own.first || !qs.has(0)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = wave * 32 + (lane & 31);
     const bool there = qs.has(mine);
-    const int i = qs.index(mine), head = qs.head(mine), row = there ? sq.q_lo + i : 0, width = there ? a.dim : 0;
-    Frag q[D / 16], g[D / 16];
-    load_row<T, D>(q, head_of<T>(a.q, row, head), width);
-    load_row<T, D>(g, head_of<T>(a.dout, row, head), width);
-    float delta = 0, lse2 = __builtin_inff();
-    {
-        Frag out[D / 16];
-        load_row<T, D>(out, head_of<T>(a.out, row, head), width);
-#pragma unroll
-        for (int d = 0; d < D / 16; d++)
-#pragma unroll
-            for (int j = 0; j < 8; j++) delta += (float)g[d][j] * (float)out[d][j];
-        delta = other_sum(delta);
-        if (there) {
-            const int64_t at = (int64_t)head * a.rows + row;
-            lse2 = exponent_of(a.lse[at]);
-            if (h == 0) a.stats[at] = {lse2, delta};
-        }
-    }
+    const int i = qs.index(mine), head = there ? qs.head(mine) : 0, row = there ? sq.q_lo + i : 0;   // (a lane without a query: any row)
     const int last = qs.rows - 1 - qs.first < BM - 1 ? qs.rows - 1 - qs.first : BM - 1;
     const int w_last = wave * 32 + 31 < last ? wave * 32 + 31 : last;
     const bool busy = wave * 32 <= last;
@@ -758,7 +743,26 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
         fv.load(v + (int64_t)t * KT * a.v.ld, sq.keys - t * KT, to + kTile);
     };
     const auto store = [&](int t) { fk.store(step_at(t)), fv.store(step_at(t) + kTile); };
-    if (steps) load(0), store(0);
+    if (steps) load(0);   // before the rows' own loads are waited for
+    Frag q[D / 16], g[D / 16];
+    load_row<T, D>(q, head_of<T>(a.q, row, head), a.dim);
+    load_row<T, D>(g, head_of<T>(a.dout, row, head), a.dim);
+    float delta = 0, lse2 = __builtin_inff();
+    {
+        Frag out[D / 16];
+        load_row<T, D>(out, head_of<T>(a.out, row, head), a.dim);
+#pragma unroll
+        for (int d = 0; d < D / 16; d++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) delta += (float)g[d][j] * (float)out[d][j];
+        delta = other_sum(delta);
+        if (there) {
+            const int64_t at = (int64_t)head * a.rows + row;
+            lse2 = exponent_of(a.lse[at]);
+            if (h == 0) a.stats[at] = {lse2, delta};
+        }
+    }
+    if (steps) store(0);
     for (int t = 0; t < steps; t++) {
         arrive<0>(fk, fv, step_at(t), kTile);
         if (t + 1 < steps) load(t + 1);
@@ -830,7 +834,7 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
     const bool there = key < sq.keys;
     const int64_t row = sq.k_lo + (there ? key : 0);
     Frag k[D / 16], v[kValuesInLds ? 1 : D / 16];
-    load_row<T, D>(k, head_of<T>(a.k, row, kv_head), there ? a.dim : 0);
+    load_row<T, D>(k, head_of<T>(a.k, row, kv_head), a.dim);   // (a lane without a key: any row)
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
 
     const float c = a.scale * kLog2e;
@@ -849,7 +853,7 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
             }
         }
     } else {
-        load_row<T, D>(v, head_of<T>(a.v, row, kv_head), there ? a.dim : 0);
+        load_row<T, D>(v, head_of<T>(a.v, row, kv_head), a.dim);
     }
     Feed<T, D, QT, WAVES, LOAD> fq(a.q.ld, a.dim), fg(a.dout.ld, a.dim);
     const Reader<T, D> read;
