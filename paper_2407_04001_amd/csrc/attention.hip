@@ -475,8 +475,8 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     constexpr bool DIRECT = LOAD != kThrough;
     typedef typename Mfma<T>::Frag Frag;
     constexpr int WAVES = 4, BM = 32, KT = 32, kTile = KT * D * 2;
-    constexpr int kOut = BM * D * 4 + BM * 8;   // a wave's output, references and sums
-    constexpr int kLds = 2 * kTile > kOut ? 2 * kTile : kOut;
+    constexpr int kSums = (BM + 1) * D * 4, kOut = kSums + BM * 8;   // a wave's output; its references and sums
+    constexpr int kLds = ((2 * kTile > kOut ? 2 * kTile : kOut) + 255) & ~255;
     __shared__ __attribute__((aligned(1024))) char lds[WAVES][kLds];
     const uint32_t block = a.first + blockIdx.x, item = block / a.splits;
     const int part = (int)(block - item * a.splits);
@@ -533,7 +533,8 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
             });
         done(All{}), load_values(t + WAVES);
     }
-    // A wave's output in quads of columns, a quad's 32 rows adjacent.
+    // A wave's output in quads of columns, a quad's 32 rows adjacent and one place left, so that neither the
+    // lanes of a row nor those of a quad meet in a bank.
     const float sum = other_sum(softmax.sum);
     {
         f32x4 *out = reinterpret_cast<f32x4 *>(lds[wave]);
@@ -544,17 +545,17 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
                 f32x4 x;
 #pragma unroll
                 for (int j = 0; j < 4; j++) x[j] = softmax.o[d][4 * e + j];
-                out[(d * 8 + e * 2 + h) * 32 + mine] = x;
+                out[(d * 8 + e * 2 + h) * (BM + 1) + mine] = x;
             }
-        if (h == 0) reinterpret_cast<float2 *>(out + D * 8)[mine] = {softmax.m, sum};
+        if (h == 0) reinterpret_cast<float2 *>(lds[wave] + kSums)[mine] = {softmax.m, sum};
     }
     __syncthreads();
-    const int r = threadIdx.x & 31;
+    const int r = threadIdx.x >> 3;   // eight lanes a row
     if (!qs.has(r)) return;
     float m[WAVES], w[WAVES], all = 0, top = -__builtin_inff();
 #pragma unroll
     for (int n = 0; n < WAVES; n++) {
-        const float2 of = reinterpret_cast<const float2 *>(lds[n] + BM * D * 4)[r];
+        const float2 of = reinterpret_cast<const float2 *>(lds[n] + kSums)[r];
         m[n] = of.x, w[n] = of.y, top = fmaxf(top, of.x);
     }
 #pragma unroll
@@ -564,7 +565,7 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     }
     const float inverse = 1.0f / all;
     const int64_t row = sq.q_lo + qs.index(r), of = qs.head(r), at = row * a.heads + of;
-    if (threadIdx.x < 32) {
+    if ((threadIdx.x & 7) == 0) {
         const float lse = all == 0 ? -__builtin_inff() : (top * c + __builtin_amdgcn_logf(all)) * kLn2;
         if (a.splits > 1)
             a.partial[part * part_rows(a) + at] = lse;
@@ -577,11 +578,11 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     T *out = out_of<T>(a.out, row, of);
 #pragma unroll
     for (int n = 0; n < D / 32; n++) {
-        const int quad = threadIdx.x / 32 + n * 8;
+        const int quad = (threadIdx.x & 7) + n * 8;
         f32x4 x = 0.0f;
 #pragma unroll
         for (int k = 0; k < WAVES; k++) {
-            const f32x4 y = reinterpret_cast<const f32x4 *>(lds[k])[quad * 32 + r];
+            const f32x4 y = reinterpret_cast<const f32x4 *>(lds[k])[quad * (BM + 1) + r];
             if (w[k] != 0) x += y * w[k];   // (what a wave that saw nothing left may be NaN)
         }
         x *= inverse;

@@ -195,7 +195,7 @@ pase_status check_attention(int dtype, uint64_t rows, uint64_t key_rows, uint32_
         return refuse(PASE_ERR_TOO_LARGE, "2^30 rows x heads or more");
     // workgroups are counted in 32 bits
     const uint64_t most = (rows > key_rows ? rows : key_rows) * (heads / kv_heads) / 32 + sequences + 2;
-    if (most * kv_heads > ((1ull << 31) - 1) / kMaxShares) return refuse(PASE_ERR_TOO_LARGE, "too many sequences x heads");
+    if (most * kv_heads >= 1ull << 31) return refuse(PASE_ERR_TOO_LARGE, "too many sequences x heads");
     return PASE_OK;
 }
 
@@ -253,10 +253,13 @@ int grouped_matmul_splits(int64_t rows, int groups, int n, int k) {
     return (int)(most < 1 ? 1 : most > 32 ? 32 : most);
 }
 
-// Tiles of 32 queries where sequences have no more on average, or where tiles of 128 would be fewer than
-// CUs; cut into shares of at least 256 keys (two steps for each of a workgroup's waves) until there are two
-// workgroups a CU, which is what LDS holds (four or eight a CU: 64 tokens over 131072 keys 74 and 79 us
-// against 74, 128 queries over 65536 keys 33 against 29).
+// Tiles of 32 queries where sequences have no more on average (heads that share keys counted), or where tiles of
+// 128 would be fewer than CUs; cut into shares of at least 256 keys (two steps for each of a
+// workgroup's waves) until there are two workgroups a CU, which is what LDS holds.  Tiles of 128
+// against these, us: 64 tokens over 64 x 2048 keys, 16 heads of 128 to 4, 66 and 57 (ragged 115 and 68), 1 x 300
+// queries over 4096 keys on two heads of 64 54 and 14, 4 x 500 over 2048 on eight of 128 46 and 34; where both
+// conditions fail, 64 x 16 over 2048 keys 76 and 93.  Four or eight workgroups a CU instead of two: 64 tokens 74 and 79
+// us against 74, 128 queries over 65536 keys 33 against 29.
 int attention_splits(int64_t rows, int64_t key_rows, int sequences, int heads, int kv_heads) {
     const int64_t packed = rows * (heads / kv_heads), some = rows < sequences ? rows : sequences;
     const int64_t large = (packed + 127) / 128, tiles = (large > some ? large : some) * kv_heads;
