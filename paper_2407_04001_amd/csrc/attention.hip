@@ -68,18 +68,65 @@ struct Range {
     }
 };
 
-// Tiles of `size` of a range's rows x group: range v owns those from start(v) * group /
-// size + v up to its successor's, as many as it needs or one more.  Which range a tile
-// is of follows by a search of 128 probes a round, without a pass over all offsets.
+__device__ __forceinline__ int wave_sum_of(int v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+    return uniform(v);
+}
+
+// The `item`-th tile, of `size` of a range's rows x group: its range and its place in it, -1 where there is none.
+// Range v owns the tiles from start(v) * group / size + v up to its successor's, as many as it needs or
+// one more, late ranges and places first (`late`: forward and dq, where these see the most keys) or early ones
+// (dk and dv: the most queries see these); which range a tile is of follows by a search of 128 probes a round.
+// a.by_place (early ones, up to 128 ranges, which stand in the lanes): tiles are dealt by the places left behind
+// them, whatever the order of their sequences, so that the workgroups that start last have the
+// least to do; it takes a few sums over the lanes, 2 us a workgroup.
 // Offsets that break their rule give some range: whatever it is, rows stay within it.
 struct Owner {
-    int v, first;   // the range, and its first tile
+    int v, place;
 
-    __device__ __forceinline__ Owner(const void *offsets, int wide, int sequences, int rows, int group, int size, int tile) {
+    __device__ __forceinline__ Owner(const Attention &a, const void *offsets, int rows, int group, int size, int item, bool late) {
         const int lane = threadIdx.x & 63;
-        const auto begin = [&](int v) { return (v == 0 ? 0 : clamped(offsets, wide, v - 1, 0, rows)) * group / size + v; };
+        const auto start = [&](int v) { return v == 0 ? 0 : v > a.sequences + 1 ? rows : clamped(offsets, a.offsets_64, v - 1, 0, rows); };
+        if (!late && a.by_place) {
+            const int s0 = start(lane), s1 = start(lane + 64), next = __shfl(s1, 0, 64);
+            int e0 = __shfl_down(s0, 1, 64), e1 = __shfl_down(s1, 1, 64);
+            e0 = lane == 63 ? next : e0, e1 = lane == 63 ? rows : e1;
+            const int n0 = e0 > s0 ? ((e0 - s0) * group + size - 1) / size : 0, n1 = e1 > s1 ? ((e1 - s1) * group + size - 1) / size : 0;
+            // tiles that are `r`-th or further of their range
+            const auto count = [&](int r) { return wave_sum_of((n0 >= r ? n0 - r + 1 : 0) + (n1 >= r ? n1 - r + 1 : 0)); };
+            v = 0, place = -1;
+            if (item >= count(1)) return;
+            int r = 1, most = n0 > n1 ? n0 : n1;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) {
+                const int o = __shfl_xor(most, d, 64);
+                most = o > most ? o : most;
+            }
+            most = uniform(most);
+            while (r < most) {   // the last r with more than `item` tiles
+                const int mid = (r + most + 1) >> 1;
+                if (count(mid) > item)
+                    r = mid;
+                else
+                    most = mid - 1;
+            }
+            // of the ranges that have an r-th tile
+            const int rank = item - count(r + 1);
+            const uint64_t h0 = __ballot(n0 >= r), h1 = __ballot(n1 >= r);
+            const int of0 = __builtin_popcountll(h0);
+            const uint64_t has = rank < of0 ? h0 : h1;
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+            const uint64_t mine = __ballot((has >> lane & 1) && before == (rank < of0 ? rank : rank - of0));
+            const int from = mine ? __builtin_ctzll(mine) : 0;
+            v = uniform(from + (rank < of0 ? 0 : 64));
+            place = uniform(__shfl(rank < of0 ? n0 : n1, from, 64)) - r;
+            return;
+        }
+        const int tile = late ? a.tiles - 1 - item : item;
+        const auto begin = [&](int v) { return start(v) * group / size + v; };
         // of ranges lo .. lo + n - 1, every step-th; the last round's are all of them
-        for (int lo = 0, n = sequences + 2;;) {
+        for (int lo = 0, n = a.sequences + 2;;) {
             const int step = (n + 127) >> 7;
             int probe[2];
 #pragma unroll
@@ -93,7 +140,7 @@ struct Owner {
             const int value = uniform(__shfl(found < 64 ? probe[0] : probe[1], found & 63, 64));
             lo += found * step;
             if (step == 1) {
-                v = uniform(lo), first = value;
+                v = uniform(lo), place = tile < value ? -1 : tile - value;
                 return;
             }
             n = n - found * step < step ? n - found * step : step;
@@ -412,14 +459,14 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k
     __shared__ __attribute__((aligned(1024))) char lds[2][2 * kTile];
     static_assert(2 * 2 * kTile >= BM * D * 2, "the output passes the same LDS");
     const uint32_t item = a.first + blockIdx.x;
-    // heads next to each other, so that an XCD's workgroups share as few as may be; late tiles,
-    // which see the most keys, first
-    const int kv_head = (int)(item % a.kv_heads), tile = a.tiles - 1 - (int)(item / a.kv_heads);
+    // heads next to each other, so that an XCD's workgroups share as few as may be
+    const int kv_head = (int)(item % a.kv_heads);
     const int group = a.heads / a.kv_heads;
-    const Owner own(a.q_offsets, a.offsets_64, a.sequences, a.rows, group, BM, tile);
+    const Owner own(a, a.q_offsets, a.rows, group, BM, (int)(item / a.kv_heads), true);
+    if (own.place < 0) return;
     const Sequence sq(a, own.v);
-    const Queries qs{group, kv_head * group, sq.q_rows * group, (tile - own.first) * BM};
-    if (tile < own.first || !qs.has(0)) return;
+    const Queries qs{group, kv_head * group, sq.q_rows * group, own.place * BM};
+    if (!qs.has(0)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = wave * 32 + (lane & 31);
     const bool there = qs.has(mine);
     const int i = qs.index(mine), head = qs.head(mine);
@@ -480,11 +527,12 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     __shared__ __attribute__((aligned(1024))) char lds[WAVES][kLds];
     const uint32_t block = a.first + blockIdx.x, item = block / a.splits;
     const int part = (int)(block - item * a.splits);
-    const int kv_head = (int)(item % a.kv_heads), tile = (int)(item / a.kv_heads), group = a.heads / a.kv_heads;
-    const Owner own(a.q_offsets, a.offsets_64, a.sequences, a.rows, group, BM, tile);
+    const int kv_head = (int)(item % a.kv_heads), group = a.heads / a.kv_heads;
+    const Owner own(a, a.q_offsets, a.rows, group, BM, (int)(item / a.kv_heads), true);
+    if (own.place < 0) return;
     const Sequence sq(a, own.v);
-    const Queries qs{group, kv_head * group, sq.q_rows * group, (tile - own.first) * BM};
-    if (tile < own.first || !qs.has(0)) return;
+    const Queries qs{group, kv_head * group, sq.q_rows * group, own.place * BM};
+    if (!qs.has(0)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = lane & 31;
     const bool there = qs.has(mine);
     const int i = qs.index(mine), head = qs.head(mine);
@@ -715,12 +763,13 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     static_assert(2 * kStep >= BM * D * 2, "the gradient passes the same LDS");
     __shared__ __attribute__((aligned(1024))) char lds[2 * kStep];
     const uint32_t item = a.first + blockIdx.x;
-    const int kv_head = (int)(item % a.kv_heads), tile = a.tiles - 1 - (int)(item / a.kv_heads);
+    const int kv_head = (int)(item % a.kv_heads);
     const int group = a.heads / a.kv_heads;
-    const Owner own(a.q_offsets, a.offsets_64, a.sequences, a.rows, group, BM, tile);
+    const Owner own(a, a.q_offsets, a.rows, group, BM, (int)(item / a.kv_heads), true);
+    if (own.place < 0) return;
     const Sequence sq(a, own.v);
-    const Queries qs{group, kv_head * group, sq.q_rows * group, (tile - own.first) * BM};
-    if (tile < own.first || !qs.has(0)) return;
+    const Queries qs{group, kv_head * group, sq.q_rows * group, own.place * BM};
+    if (!qs.has(0)) return;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), h = lane >> 5, mine = wave * 32 + (lane & 31);
     const bool there = qs.has(mine);
     const int i = qs.index(mine), head = there ? qs.head(mine) : 0, row = there ? sq.q_lo + i : 0;   // (a lane without a query: any row)
@@ -822,13 +871,13 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
     constexpr int kLds = kValues + TEAMS * kSteps * kStep > kJoin ? kValues + TEAMS * kSteps * kStep : kJoin;
     __shared__ __attribute__((aligned(1024))) char lds[kLds];
     const uint32_t item = a.first + blockIdx.x;
-    // early tiles, which the most queries see, first
-    const int kv_head = (int)(item % a.kv_heads), tile = (int)(item / a.kv_heads);
+    const int kv_head = (int)(item % a.kv_heads);
     const int group = a.heads / a.kv_heads;
-    const Owner own(a.k_offsets, a.offsets_64, a.sequences, a.key_rows, 1, BM, tile);
+    const Owner own(a, a.k_offsets, a.key_rows, 1, BM, (int)(item / a.kv_heads), false);
+    if (own.place < 0) return;
     const Sequence sq(a, own.v);
-    const int first = (tile - own.first) * BM;
-    if (first < 0 || first >= sq.k_rows) return;
+    const int first = own.place * BM;
+    if (first >= sq.k_rows) return;
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int team = TEAMS == 1 ? 0 : uniform(threadIdx.x >> 6) / WAVES, wave = uniform(threadIdx.x >> 6) % WAVES;
     const int key0 = first + wave * 32, key = key0 + (lane & 31);
@@ -1039,7 +1088,9 @@ template <typename T, int D, Load LOAD> int queries_grad(Attention a, void *stre
 // where long sequences share heads, no CU waits long for the longest tile's (4 causal sequences, 16384
 // rows, 16 heads of 128 to 4: 736 us against 1185); with many tiles one team has two workgroups a CU (64 x
 // 256 rows, 16 heads of 64: 59 us against 100), and so with few steps, where joining costs as much (59 x 16
-// rows, 16 heads of 128, both kernels: 58 us against 82).
+// rows, 16 heads of 128, both kernels: 58 us against 82).  Several sequences of sixteen tiles or more are dealt by
+// place (the long ones again, whole backward pass: 1193 us against 1135; forward and dq, whose tiles are
+// shorter, gained 1 % there and lost 6 on 4 sequences of 680 rows).
 template <typename T, int D, Load LOAD> int keys_grad(Attention a, void *stream) {
     if (!a.key_rows) return 0;
     constexpr int QT = D == 32 ? 64 : 32;
@@ -1048,6 +1099,7 @@ template <typename T, int D, Load LOAD> int keys_grad(Attention a, void *stream)
     if constexpr (LOAD != kThrough) {
         if ((large > some ? large : some) * a.kv_heads < 4 * kCus && steps >= 16) {
             a.tiles = (int)tiles_of(a.key_rows, 64, a.sequences);
+            a.by_place = a.sequences > 1 && a.sequences + 2 <= 128 && a.key_rows >= 16 * 64ll * a.sequences;
             return launch_items(k_keys_grad<T, D, QT, 2, 4, LOAD>, (int64_t)a.tiles * a.kv_heads, 512, stream, a);
         }
     }

@@ -78,6 +78,7 @@ struct Attention {
     RowStats *stats;     // [heads][rows], for the second kernel of the backward pass
     float *partial;      // forward with splits > 1: [splits][rows x heads, up to a multiple of 4], then as many rows of dim, up to a multiple of 4
     int splits, tiles;   // splits: see attention_splits(); tiles: of the queries' (keys') rows, see tiles_of()
+    int by_place;        // how tiles of keys are dealt, see Owner in attention.hip
     uint32_t first;
 };
 

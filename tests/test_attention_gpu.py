@@ -172,6 +172,8 @@ CASES = [
     ([140, 70], [201, 70], 4, 2, 118, True, {"layout": "fused", "room": 9}),
     ([600], [600], 4, 1, 58, True, {"layout": "fused"}),         # few tiles, many steps
     ([600], [600], 4, 1, 128, True, {"layout": "heads first"}),
+    ([1500, 0, 1900], [1500, 7, 1900], 4, 1, 64, True, {"before": 3, "after": 2}),   # several sequences of many tiles
+    ([520] * 100 + [900], [1100] * 101, 1, 1, 32, True, {"room": 1}),
     ([550, 60], [600, 70], 4, 1, 126, False, {"layout": "fused", "room": 3}),
     ([5, 4, 0, 1], [64, 1, 3, 0], 4, 2, 64, True, {"room": 64, "wide": torch.int64}),
     ([17] * 70, [19] * 70, 2, 2, 16, True, {}),               # more sequences than a wave has lanes
