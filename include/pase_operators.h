@@ -179,7 +179,8 @@ pase_status pase_attention_workspace(int dtype, uint64_t rows, uint64_t key_rows
  * and ds_ij = p_ij (dout_i . v_j - dout_i . out_i),
  *     dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
  * dk and dv summed over the heads that share them.  p and ds are recomputed, and
- * rounded to dtype before the second products.  Rows of no sequence and keys past a length get 0.
+ * rounded to dtype before the second products (in fp16 a ds above 65504 is infinite, one
+ * below 2^-25 is 0: gradients want the loss scale that training in fp16 has).  Rows of no sequence and keys past a length get 0.
  * No output may be an input. */
 pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
                                     uint32_t kv_heads, uint32_t dim, const void *dout, uint64_t lddo, uint64_t hsdo,

@@ -451,7 +451,15 @@ template <typename T, int D, int KT> struct Softmax {
     }
 };
 
-// 128 queries a workgroup, 64 keys a step, keys and values two steps deep in LDS.
+// 128 queries a workgroup, 64 keys a step, keys and values two steps deep in LDS: 32 queries
+// a wave, whose operand and output stay in registers, at two (128 columns) or four waves a SIMD, so that one
+// multiplies while another takes its exponents.  Per score 4 D operations of the matrix
+// units and, in a lane, a maximum, a multiply-add, an exponential (a quarter of their rate), an addition and
+// half a conversion: at 128 columns both take about as long, at 64 the lanes twice.  Long causal sequences
+// (16384 rows in 4, 16 heads of 128 to 4) 321 us, 930 TFLOP/s (an 8192^3 library product 1170-1245); 4 x 4096, 16 heads
+// of 64, 861 TFLOP/s without the causal limit.  64 x 256 rows, 16 heads of 64: 44 us for 134 MB, waiting for loads
+// half of a wave's time, as a workgroup has four steps only.  Three steps in LDS (and so three
+// workgroups a CU) were slower there, 49.6 us against 44.7.
 template <typename T, int D, Load LOAD>
 __global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k_forward(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
@@ -516,8 +524,12 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k
 // Few queries: 32 a workgroup, of one sequence.  Its four waves take every fourth step of 32
 // keys each, with no barrier between them, from LDS of their own: the next step's keys are
 // loaded where this one's were once they are read, values likewise, so that a wave always
-// has loads on their way and LDS holds two workgroups.  The waves' outputs are joined at the end; where tiles are still too few, a.splits workgroups share a tile's keys and leave
-// their outputs and log-sum-exps for k_join.
+// has loads on their way and LDS holds two workgroups (two steps deep and one workgroup a
+// CU: 80 us against 62 for 64 tokens over 131072 keys, 4 heads of 128).  The waves' outputs are
+// joined at the end; where tiles are still too few, a.splits workgroups share a tile's keys
+// and leave their outputs and log-sum-exps for k_join.
+// Bound by HBM: those 64 tokens 60 us for 269 MB (4.5 TB/s), and 4 us for the join; one token
+// over 131072 keys, 2 heads, 30 us for 134 MB and 6.
 template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) void k_forward_few(Attention a) {
     constexpr bool DIRECT = LOAD != kThrough;
     typedef typename Mfma<T>::Frag Frag;
@@ -645,7 +657,7 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     }
 }
 
-// Joins up to kFewShares shares: eight rows and heads a workgroup, 32 lanes each.
+// Joins up to kFewShares shares: eight rows and heads a workgroup, 32 lanes each (1024 rows and heads 4 us, 8 by k_join).
 constexpr int kFewShares = 8;
 
 template <typename T> __global__ __launch_bounds__(256) void k_join_few(Attention a) {
@@ -718,7 +730,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a)
 // kernels, each with its own outputs in registers: dq over the keys, which also leaves
 // the rows' exponents and deltas, and dk and dv over the queries.  Scores and dp are formed in both (seven
 // products where one kernel with atomics would take five): sums have a fixed order.
-// p and ds are rounded to the operands' type before their second products.
+// p and ds are rounded to the operands' type before their second products: by up to 2^-8
+// (bf16) or 2^-11 of each, either way, as the results are once more.
 
 __device__ __forceinline__ float exponent_of(float lse) {   // rows without keys: p = 0
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
@@ -756,7 +769,10 @@ template <int D> struct Join {
     }
 };
 
-// Queries along the lanes, as in the forward pass.
+// Queries along the lanes, as in the forward pass: 128 a workgroup, 64 keys a step.  Long causal sequences (16384
+// rows in 4, 16 heads of 128 to 4) 420-450 us for 448 GFLOP (1 PFLOP/s); 64 x 256 rows, 16 heads of 64 60 us
+// for 201 MB, waiting for loads two thirds of a wave's time (three steps in LDS, or four waves a SIMD, changed
+// nothing or lost 2 us).
 template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) void k_queries_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
     constexpr int WAVES = 4, BM = 128, KT = D == 128 && LOAD == kThrough ? 32 : 64, kTile = KT * D * 2, kStep = 2 * kTile;
@@ -856,7 +872,11 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
 // queries; dv^T += dout^T p and dk^T += q^T ds.  TEAMS teams of waves have the same
 // WAVES x 32 keys: the steps through the queries of all heads that share them, QT at a
 // time, go round the teams, whose sums are added at the end.
-// DIRECT: three steps in LDS, two on their way (two and one where LDS holds no more); else one, loaded where it is needed.
+// Loads to LDS: three steps in LDS, two on their way (128 columns: two and one); through registers: one, loaded
+// where it is needed.  With 128 columns the accumulators take 128 of a lane's 256 registers at two waves a SIMD; at
+// one wave a SIMD and 512 the compiler moved them to and from the second half in every step (2162 us for the whole
+// backward pass of 16384 rows in 4 causal sequences, 16 heads of 128 to 4, against 1647).  There 735 us for 598
+// GFLOP (814 TFLOP/s); 64 x 256 rows, 16 heads of 64 59 us.
 template <typename T, int D, int QT, int WAVES, int TEAMS, Load LOAD>
 __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 3) void k_keys_grad(Attention a) {
     constexpr bool DIRECT = LOAD != kThrough;

