@@ -30,9 +30,9 @@ SHARED = [dict(dtype=FP32), dict(dtype=7), dict(sequences=0), dict(heads=0), dic
 LARGE = [dict(dim=129), dict(sequences=65537), dict(heads=131072, kv_heads=131072), dict(rows=1 << 30), dict(key_rows=1 << 30),
          dict(sequences=65536, heads=65536, kv_heads=65536)]
 REFUSALS = [
-    ("pase_attention_forward", ATT_F, INVALID, SHARED + [dict(rows=1, key_rows=1000, heads=2, kv_heads=1, ws=None), dict(rows=1, key_rows=1000, ws=P + 8)]),
+    ("pase_attention_forward", ATT_F, INVALID, SHARED + [dict(rows=1, key_rows=5000, heads=2, kv_heads=1, ws=None), dict(rows=1, key_rows=5000, ws=P + 8)]),
     ("pase_attention_forward", ATT_F, TOO_LARGE, LARGE),
-    ("pase_attention_forward", ATT_F, OUT_OF_MEMORY, [dict(rows=1, key_rows=1000, ws_bytes=64)]),
+    ("pase_attention_forward", ATT_F, OUT_OF_MEMORY, [dict(rows=1, key_rows=5000, ws_bytes=64)]),
     ("pase_attention_backward", ATT_B, INVALID, SHARED + [
         dict(do=None), dict(lddo=4), dict(dq=None), dict(hsdq=4), dict(dk=None), dict(lddk=4), dict(dv=P + 1), dict(hsdv=0), dict(ws=None), dict(ws=P + 4)]),
     ("pase_attention_backward", ATT_B, TOO_LARGE, LARGE),

@@ -774,3 +774,34 @@ def test_outputs_keep_to_their_rows_and_heads(ops):  # noqa: F811
     m, z, seed = rand(gen(9), rows, 40, dtype=BF), torch.full((rows, 43), mark, dtype=BF, device="cuda"), torch.tensor([3, 4], device="cuda")
     assert L.pase_dropout(0, rows, 40, m.data_ptr(), 40, None, 0, 0.5, seed.data_ptr(), z.data_ptr(), 43, stream) == 0
     assert torch.equal(z[:, :40], ops.dropout_forward(m, 0.5, seed)) and (z[:, 40:] == mark).all()
+
+
+def test_attention_of_more_tiles_than_one_launch_holds(ops):  # noqa: F811
+    """65536 sequences of one token and one key under 256 heads: over 2^24 workgroups of 256 threads in every kernel.
+    A weight of 1 makes the output the value and dv the gradient, both exactly; ds is what two orders of one sum leave."""
+    n, heads, dim = 65536, 256, 8
+    g = gen(161)
+    q, k, v, dout = (rand(g, n, heads, dim, dtype=BF) for _ in range(4))
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    out, lse = ops.attention_forward(q, k, v, off, off, causal=True)
+    assert torch.equal(out, v)
+    want = (q.double() * k.double()).sum(2).t() * dim ** -0.5
+    size = (q.double() * k.double()).abs().sum(2).t() * dim ** -0.5
+    assert ((lse.double() - want).abs() <= 2 * (dim + 8) * E * size + 8 * E * want.abs() + 2.0 ** -21).all()
+    dq, dk, dv = ops.attention_backward(dout, q, k, v, out, lse, off, off, causal=True)
+    # p = exp(s - lse) is 1 but for the roundings of s, lse and the power
+    p_error = (4 * (dim + 8) * E * size + 16 * E * want.abs() + 2.0 ** -20).t()[..., None]
+    assert ((dv.double() - dout.double()).abs() <= (U[BF] + p_error) * dout.double().abs()).all()
+    noise = (4 * (dim + 8) * E * (dout.double() * v.double()).abs().sum(2))[..., None]
+    assert (dq.double().abs() <= 1.1 * dim ** -0.5 * noise * k.double().abs()).all()
+    assert (dk.double().abs() <= 1.1 * dim ** -0.5 * noise * q.double().abs()).all()
+
+
+def test_rotary_of_more_rows_than_one_launch_holds(ops):  # noqa: F811
+    x = torch.zeros((1 << 24) + 5, 1, 258, dtype=BF, device="cuda")
+    x[-3:] = rand(gen(171), 3, 1, 258, dtype=BF)
+    positions = torch.arange(x.shape[0], device="cuda")
+    f = ops.rotary_frequencies(258)
+    want = ops.rotary_forward(x[-3:].contiguous(), positions[-3:], f)
+    ops.rotary_forward(x, positions, f, out=x)
+    assert torch.equal(x[-3:], want) and not x[:-3].any()
