@@ -178,7 +178,7 @@ pase_status softmax_loss_backward(int dtype, uint64_t rows, uint64_t classes, co
     return launched(launch_softmax_loss_backward(a, stream));
 }
 
-constexpr uint64_t kMaxAttentionRows = 1ull << 30;   // rows x the heads that share keys and values
+constexpr uint64_t kMaxAttentionRows = (1ull << 30) - 1024;   // rows x heads: places of queries and keys are added in 32 bits, a tile past the last ones too
 
 pase_status check_attention(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
                             uint32_t kv_heads, uint32_t dim) {
@@ -192,7 +192,7 @@ pase_status check_attention(int dtype, uint64_t rows, uint64_t key_rows, uint32_
         return refuse(PASE_ERR_TOO_LARGE, "%u sequences, above %d", sequences, PASE_MAX_GROUPS);
     if (heads > 65536) return refuse(PASE_ERR_TOO_LARGE, "%u heads, above 65536", heads);
     if (rows > kMaxAttentionRows / heads || key_rows > kMaxAttentionRows / kv_heads)
-        return refuse(PASE_ERR_TOO_LARGE, "2^30 rows x heads or more");
+        return refuse(PASE_ERR_TOO_LARGE, "rows x heads above 2^30 - 1024");
     // workgroups are counted in 32 bits
     const uint64_t most = (rows > key_rows ? rows : key_rows) * (heads / kv_heads) / 32 + sequences + 2;
     if (most * kv_heads >= 1ull << 31) return refuse(PASE_ERR_TOO_LARGE, "too many sequences x heads");

@@ -28,7 +28,7 @@ SHARED = [dict(dtype=FP32), dict(dtype=7), dict(sequences=0), dict(heads=0), dic
           dict(q_offsets=P + 2), dict(k_offsets=P + 4, off64=1), dict(off64=2), dict(k_lengths=P + 1), dict(causal=2), dict(scale=0.0),
           dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e-40), dict(lse=None), dict(lse=P + 2), dict(o=None), dict(ldo=3)]
 LARGE = [dict(dim=129), dict(sequences=65537), dict(heads=131072, kv_heads=131072), dict(rows=1 << 30), dict(key_rows=1 << 30),
-         dict(sequences=65536, heads=65536, kv_heads=65536)]
+         dict(rows=1 << 30, heads=1, kv_heads=1), dict(key_rows=1 << 30, heads=1, kv_heads=1), dict(sequences=65536, heads=65536, kv_heads=65536)]
 REFUSALS = [
     ("pase_attention_forward", ATT_F, INVALID, SHARED + [dict(rows=1, key_rows=5000, heads=2, kv_heads=1, ws=None), dict(rows=1, key_rows=5000, ws=P + 8)]),
     ("pase_attention_forward", ATT_F, TOO_LARGE, LARGE),
