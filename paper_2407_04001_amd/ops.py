@@ -134,10 +134,10 @@ def _same(name, t, dtype, like):
 
 
 def _vector(name, t, n, dtype, like):
-    if t.dim() != 1 or t.shape[0] != n:
+    if t.shape != (n,):
         _refuse(f"{name} is {tuple(t.shape)}, ({n},) is wanted")
     _same(name, t, dtype, like)
-    if n > 1 and t.stride(0) != 1:
+    if not t.is_contiguous():
         _refuse(f"{name} is not contiguous")
     return t.data_ptr()
 
@@ -354,8 +354,8 @@ def attention_forward(q, k, v, q_offsets, k_offsets, k_lengths=None, causal: boo
     n, qo, ko, kl, wide = _sequences(q_offsets, k_offsets, k_lengths, q)
     L = load()
     ws, wp, have = _workspace(q, "pase_attention_workspace", d, rows, key_rows, n, heads, kv_heads, dim, 0)
-    out = q.new_empty((rows, heads, dim))
-    lse = q.new_empty((heads, rows), dtype=torch.float32)
+    out = q.new_empty(rows, heads, dim)
+    lse = q.new_empty(heads, rows, dtype=torch.float32)
     _check(L.pase_attention_forward(d, rows, key_rows, n, heads, kv_heads, dim, *args, qo, ko, kl, wide, bool(causal), scale,
                                     out.data_ptr(), heads * dim, dim, lse.data_ptr(), wp, have, _raw_stream(q.get_device())))
     return out, lse
@@ -374,8 +374,8 @@ def attention_backward(dout, q, k, v, out, lse, q_offsets, k_offsets, k_lengths=
     n, qo, ko, kl, wide = _sequences(q_offsets, k_offsets, k_lengths, q)
     L = load()
     ws, wp, have = _workspace(q, "pase_attention_workspace", d, rows, key_rows, n, heads, kv_heads, dim, 1)
-    dq = q.new_empty((rows, heads, dim))
-    dk, dv = q.new_empty((key_rows, kv_heads, dim)), q.new_empty((key_rows, kv_heads, dim))
+    dq = q.new_empty(rows, heads, dim)
+    dk, dv = q.new_empty(key_rows, kv_heads, dim), q.new_empty(key_rows, kv_heads, dim)
     _check(L.pase_attention_backward(d, rows, key_rows, n, heads, kv_heads, dim, *hdo, *args, *ho, lse.data_ptr(), qo, ko, kl,
                                      wide, bool(causal), scale, dq.data_ptr(), heads * dim, dim, dk.data_ptr(),
                                      kv_heads * dim, dim, dv.data_ptr(), kv_heads * dim, dim, wp, have,
@@ -409,8 +409,11 @@ def _rotary(x, positions, frequencies, interleaved, magnitude, out, inverse):
     if frequencies.dim() != 1:
         _refuse(f"frequencies is {tuple(frequencies.shape)}, (turned / 2,) is wanted")
     f = _vector("frequencies", frequencies, frequencies.shape[0], torch.float64, x)
-    y = x.new_empty((rows, heads, dim)) if out is None else out
-    hy = _heads("out", y, x, rows, heads, dim)
+    if out is None:
+        y = x.new_empty(rows, heads, dim)
+        hy = y.data_ptr(), heads * dim, dim
+    else:
+        y, hy = out, _heads("out", out, x, rows, heads, dim)
     _check(load().pase_rotary(d, rows, heads, dim, 2 * frequencies.shape[0], bool(interleaved), inverse, *hx, p, wide, f,
                               magnitude, *hy, _raw_stream(x.get_device())))
     _written(out)
@@ -442,7 +445,7 @@ def _dropout(x, p, seed, residual):
     if residual is not None:
         ldr, r = _matrix("residual", residual, x, rows, width), residual.data_ptr()
     s = _vector("seed", seed, 2, torch.int64, x)
-    y = x.new_empty((rows, width))
+    y = x.new_empty(rows, width)
     _check(load().pase_dropout(d, rows, width, x.data_ptr(), ldx, r, ldr, p, s, y.data_ptr(), width, _raw_stream(x.get_device())))
     return y
 
