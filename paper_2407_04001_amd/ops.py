@@ -10,6 +10,8 @@ nothing waits for it.  A refused argument raises `PaseError`.
 
 ``layer_norm``, ``grouped_matmul``, ``attention``, ``rotary``, ``dropout`` and ``softmax_loss`` are differentiable, once
 (`torch.autograd`; a second derivative raises); the others are the passes they are made of.
+A HIP graph captures the passes as they are; their differentiable forms only while no eager graph of the same leaves
+lives, since torch adds up a leaf's gradient on the stream of the first graph that holds it.
 """
 from __future__ import annotations
 
