@@ -228,7 +228,11 @@ pase_status check_heads(const char *name, uint64_t ld, uint64_t hs, uint64_t row
     return PASE_OK;
 }
 
-HeadRows head_rows(const void *p, uint64_t ld, uint64_t hs) { return {const_cast<void *>(p), (int64_t)ld, (int64_t)hs}; }
+// The distance to a next row or head that is not there is the caller's to leave as it likes; attention's loads
+// to LDS tell by it what lies past the last row.
+HeadRows head_rows(const void *p, uint64_t ld, uint64_t hs, uint64_t rows, uint64_t heads, uint64_t dim) {
+    return {const_cast<void *>(p), (int64_t)(rows <= 1 ? dim : ld), (int64_t)(heads == 1 ? dim : hs)};
+}
 
 uint64_t attention_bytes(uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads,
                          uint32_t dim) {
@@ -480,8 +484,8 @@ pase_status pase_attention_forward(int dtype, uint64_t rows, uint64_t key_rows, 
     a.rows = (int)rows, a.key_rows = (int)key_rows, a.sequences = (int)sequences;
     a.heads = (int)heads, a.kv_heads = (int)kv_heads, a.dim = (int)dim, a.scale = scale;
     a.q_offsets = q_offsets, a.k_offsets = k_offsets, a.k_lengths = k_lengths;
-    a.q = head_rows(q, ldq, hsq), a.k = head_rows(k, ldk, hsk), a.v = head_rows(v, ldv, hsv);
-    a.out = head_rows(out, ldo, hso), a.lse = lse;
+    a.q = head_rows(q, ldq, hsq, rows, heads, dim), a.out = head_rows(out, ldo, hso, rows, heads, dim), a.lse = lse;
+    a.k = head_rows(k, ldk, hsk, key_rows, kv_heads, dim), a.v = head_rows(v, ldv, hsv, key_rows, kv_heads, dim);
     a.splits = attention_splits(a.rows, a.key_rows, a.sequences, a.heads, a.kv_heads);
     a.partial = a.splits > 1 ? static_cast<float *>(workspace) : nullptr;
     return launched(launch_attention_forward(a, stream));
@@ -527,9 +531,11 @@ pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows,
     a.rows = (int)rows, a.key_rows = (int)key_rows, a.sequences = (int)sequences;
     a.heads = (int)heads, a.kv_heads = (int)kv_heads, a.dim = (int)dim, a.scale = scale;
     a.q_offsets = q_offsets, a.k_offsets = k_offsets, a.k_lengths = k_lengths;
-    a.q = head_rows(q, ldq, hsq), a.k = head_rows(k, ldk, hsk), a.v = head_rows(v, ldv, hsv);
-    a.out = head_rows(out, ldo, hso), a.dout = head_rows(dout, lddo, hsdo), a.lse = const_cast<float *>(lse);
-    a.dq = head_rows(dq, lddq, hsdq), a.dk = head_rows(dk, lddk, hsdk), a.dv = head_rows(dv, lddv, hsdv);
+    a.q = head_rows(q, ldq, hsq, rows, heads, dim), a.dq = head_rows(dq, lddq, hsdq, rows, heads, dim);
+    a.out = head_rows(out, ldo, hso, rows, heads, dim), a.dout = head_rows(dout, lddo, hsdo, rows, heads, dim);
+    a.lse = const_cast<float *>(lse);
+    a.k = head_rows(k, ldk, hsk, key_rows, kv_heads, dim), a.dk = head_rows(dk, lddk, hsdk, key_rows, kv_heads, dim);
+    a.v = head_rows(v, ldv, hsv, key_rows, kv_heads, dim), a.dv = head_rows(dv, lddv, hsdv, key_rows, kv_heads, dim);
     a.stats = static_cast<RowStats *>(workspace);
     return launched(launch_attention_backward(a, stream));
 }
@@ -556,7 +562,7 @@ pase_status pase_rotary(int dtype, uint64_t rows, uint32_t heads, uint32_t dim, 
     Rotary a{};
     a.dtype = dtype, a.positions_64 = positions_64, a.interleaved = interleaved;
     a.rows = (int64_t)rows, a.heads = (int)heads, a.dim = (int)dim, a.half = (int)turned / 2;
-    a.x = head_rows(x, ldx, hsx), a.y = head_rows(y, ldy, hsy);
+    a.x = head_rows(x, ldx, hsx, rows, heads, dim), a.y = head_rows(y, ldy, hsy, rows, heads, dim);
     a.positions = positions, a.frequencies = frequencies;
     a.magnitude = magnitude, a.sine = inverse ? -magnitude : magnitude;
     return launched(launch_rotary(a, stream));

@@ -1,0 +1,45 @@
+"""Attention, rotary positions and dropout where calls that the documentation allows come close to its limits.
+
+Tolerances are the bounds of test_attention_gpu: u is the unit roundoff of a matrix's type, e = 2^-24 that of fp32."""
+import math
+
+import pytest
+import torch
+
+from test_attention_gpu import bounds, check_backward, check_forward, laid_out, make, offsets, rotary64, sequences  # noqa: F401
+from test_operators_gpu import BF, E, HF, INF, SF, U, close, gen, ops, rand, refused  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def arg(t, ld=None):
+    """Pointer and strides of a [rows, heads, dim] argument of the C ABI."""
+    return t.data_ptr(), t.stride(0) if ld is None else ld, t.stride(1)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [24, 64, 126, 128, 13])
+@pytest.mark.parametrize("keys,heads,kv_heads", [(70, 4, 2), (1, 3, 3), (700, 2, 1)])
+def test_one_row_has_no_row_stride(ops, keys, heads, kv_heads, dim, dtype):  # noqa: F811
+    """Through the C ABI: the row stride of a single row, whatever it is, has no influence."""
+    L = ops.load()
+    g = gen(201)
+    q, dout, out2 = (rand(g, 1, heads, dim, dtype=dtype) for _ in range(3))
+    k, v = rand(g, keys, kv_heads, dim, dtype=dtype), rand(g, keys, kv_heads, dim, dtype=dtype)
+    qo, ko = offsets([1]), offsets([keys])
+    ref = ops.attention_forward(q, k, v, qo, ko)
+    grads = ops.attention_backward(dout, q, k, v, *ref, qo, ko)
+    check_backward(grads, dout, q, k, v, *ref, qo, ko)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    stream, code = torch.cuda.current_stream().cuda_stream, 0 if dtype is BF else 1
+    for ld in (0, 1, dim // 2, dim - 1):
+        key_ld = ld if keys == 1 else None
+        lse, dq, dk, dv = (torch.full_like(t, float("nan")) for t in (ref[1], q, k, v))
+        assert L.pase_attention_forward(code, 1, keys, 1, heads, kv_heads, dim, *arg(q, ld), *arg(k, key_ld), *arg(v, key_ld), qo.data_ptr(),
+                                        ko.data_ptr(), None, 0, 0, dim ** -0.5, *arg(out2, ld), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream) == 0
+        assert torch.equal(out2, ref[0]) and torch.equal(lse, ref[1]), ld
+        assert L.pase_attention_backward(code, 1, keys, 1, heads, kv_heads, dim, *arg(dout, ld), *arg(q, ld), *arg(k, key_ld), *arg(v, key_ld),
+                                         *arg(out2, ld), lse.data_ptr(), qo.data_ptr(), ko.data_ptr(), None, 0, 0, dim ** -0.5, *arg(dq, ld),
+                                         *arg(dk, key_ld), *arg(dv, key_ld), ws.data_ptr(), ws.numel(), stream) == 0
+        for name, a, b in zip(("dq", "dk", "dv"), (dq, dk, dv), grads):
+            assert torch.equal(a, b), (name, ld)
