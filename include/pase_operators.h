@@ -161,7 +161,7 @@ pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t 
  * Keys and values past a sequence's length are not read.  Within it a value that is not
  * finite may reach every query of its sequence, also past the causal limit.
  * scale: positive.  Weights exp(s_ij - lse_i) are rounded to dtype before they
- * multiply the values.  workspace: pase_attention_workspace() bytes, 16-byte
+ * multiply the values (in fp16 those below 2^-20 of the greatest so far by up to 2^-31 of it).  workspace: pase_attention_workspace() bytes, 16-byte
  * aligned.  No output may be an input; rows x heads and key_rows x kv_heads are at most 2^30 - 1024. */
 pase_status pase_attention_forward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
                                    uint32_t kv_heads, uint32_t dim, const void *q, uint64_t ldq, uint64_t hsq,
@@ -180,7 +180,7 @@ pase_status pase_attention_workspace(int dtype, uint64_t rows, uint64_t key_rows
  *     dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
  * dk and dv summed over the heads that share them.  p and ds are recomputed, and
  * rounded to dtype before the second products (in fp16 a ds above 65504 is infinite, one
- * below 2^-25 is 0: gradients want the loss scale that training in fp16 has).  Rows of no sequence and keys past a length get 0.
+ * below 2^-25 is 0: gradients want the loss scale that training in fp16 has; a p below 2^-26 is off by up to 2^-37).  Rows of no sequence and keys past a length get 0.
  * No output may be an input. */
 pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
                                     uint32_t kv_heads, uint32_t dim, const void *dout, uint64_t lddo, uint64_t hsdo,

@@ -37,6 +37,15 @@ template <> struct Mfma<_Float16> {
     }
 };
 
+// fp16's least numbers are 2^-24, which weights of many keys come near: before they are rounded they are 2^kRaised
+// times their size, which the sum and the output share.  Forward they then reach 2^14 (see Softmax), and those below 2^-20 of
+// the reference are off by up to 2^-31 of it instead of 2^-25; backward 2^12, and below 2^-26 by 2^-37.  The rest up to
+// 2^16 is for exponents off by their own roundings.  It costs no instruction: the exponent's reference has it.
+template <typename T> constexpr int kRaised = 0;
+template <typename T> constexpr int kRaisedGrad = 0;
+template <> constexpr int kRaised<_Float16> = 6;
+template <> constexpr int kRaisedGrad<_Float16> = 12;
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // Keeps a uniform branch a branch, where the compiler would make it selects on every path.
@@ -384,7 +393,7 @@ __device__ __forceinline__ int64_t part_rows(const Attention &a) { return ((int6
 
 // ---------------------------------------------------------------- forward
 // The softmax of one query a lane, so far: the output as the sum of 2^(c (s - m)) v and the
-// weights' sum over this lane's half of the keys.
+// weights' sum over this lane's half of the keys, both times 2^kRaised.
 template <typename T, int D, int KT> struct Softmax {
     typedef typename Mfma<T>::Frag Frag;
     f32x16 o[D / 32] = {};
@@ -428,7 +437,7 @@ template <typename T, int D, int KT> struct Softmax {
 #pragma unroll
             for (int d = 0; d < D / 32; d++) o[d] *= f;
         }
-        const float from = m == -__builtin_inff() ? 0.0f : m * c;
+        const float from = m == -__builtin_inff() ? 0.0f : m * c - kRaised<T>;
 #pragma unroll
         for (int b = 0; b < KT / 32; b++)
 #pragma unroll
@@ -437,7 +446,7 @@ template <typename T, int D, int KT> struct Softmax {
                 sum += s[b][j];
             }
         before();
-        // weights are rounded to the values' type: by up to 2^-8 (bf16) or 2^-11 of each, either way
+        // weights are rounded to the values' type: by up to 2^-8 (bf16) or 2^-11 of each (see kRaised), either way
 #pragma unroll
         for (int g = 0; g < KT / 16; g++) {
             const Frag p = narrow<T>(s[g / 2], g % 2 * 8);
@@ -445,9 +454,9 @@ template <typename T, int D, int KT> struct Softmax {
             for (int d = 0; d < D / 32; d++) o[d] = Mfma<T>::go(Reader<T, D>::column(vt, g, d), p, o[d]);
         }
     }
-    // of both halves' sum: a weight of 1 or more, or nothing was seen
+    // of both halves' sum: a weight of 2^kRaised or more, or nothing was seen
     __device__ __forceinline__ float lse(float all, float c) const {
-        return all == 0 ? -__builtin_inff() : (m * c + __builtin_amdgcn_logf(all)) * kLn2;
+        return all == 0 ? -__builtin_inff() : (m * c + (__builtin_amdgcn_logf(all) - kRaised<T>)) * kLn2;
     }
 };
 
@@ -626,7 +635,7 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
     const float inverse = 1.0f / all;
     const int64_t row = sq.q_lo + qs.index(r), of = qs.head(r), at = row * a.heads + of;
     if ((threadIdx.x & 7) == 0) {
-        const float lse = all == 0 ? -__builtin_inff() : (top * c + __builtin_amdgcn_logf(all)) * kLn2;
+        const float lse = all == 0 ? -__builtin_inff() : (top * c + (__builtin_amdgcn_logf(all) - kRaised<T>)) * kLn2;
         if (a.splits > 1)
             a.partial[part * part_rows(a) + at] = lse;
         else
@@ -731,11 +740,14 @@ template <typename T> __global__ __launch_bounds__(256) void k_join(Attention a)
 // the rows' exponents and deltas, and dk and dv over the queries.  Scores and dp are formed in both (seven
 // products where one kernel with atomics would take five): sums have a fixed order.
 // p and ds are rounded to the operands' type before their second products: by up to 2^-8
-// (bf16) or 2^-11 of each, either way, as the results are once more.
+// (bf16) or 2^-11 of each, either way, as the results are once more.  In fp16 p is raised first (kRaisedGrad), as no scale
+// of the loss reaches it; ds is not, as one does.
 
 __device__ __forceinline__ float exponent_of(float lse) {   // rows without keys: p = 0
     return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
 }
+
+template <typename T> constexpr float kLower = 1.0f / (1 << kRaisedGrad<T>);
 
 // The sum of a result over teams of `waves` waves: every team but `to` gives its own, in LDS, which `to`
 // then adds to its own in the teams' order.  A part is 128 D bytes for each wave.
@@ -825,7 +837,7 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
         if (there) {
             const int64_t at = (int64_t)head * a.rows + row;
             lse2 = exponent_of(a.lse[at]);
-            if (h == 0) a.stats[at] = {lse2, delta};
+            if (h == 0) a.stats[at] = {lse2 - kRaisedGrad<T>, delta * kLower<T>};
         }
     }
     if (steps) store(0);
@@ -1011,8 +1023,8 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     const f32x4 st = stats(e / 2, e % 2);
-                    dp[2 * e] = s[2 * e] * (dp[2 * e] - st[1]);
-                    dp[2 * e + 1] = s[2 * e + 1] * (dp[2 * e + 1] - st[3]);
+                    dp[2 * e] = s[2 * e] * __builtin_fmaf(dp[2 * e], kLower<T>, -st[1]);
+                    dp[2 * e + 1] = s[2 * e + 1] * __builtin_fmaf(dp[2 * e + 1], kLower<T>, -st[3]);
                 }
                 const Frag ds[2] = {narrow<T>(dp, 0), narrow<T>(dp, 8)};
                 const uint32_t qc = read.columns_of(qt + b * 32 * D * 2);
@@ -1040,7 +1052,7 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
     const int left = sq.k_rows - key0;
     char *out = lds + (team * WAVES + wave) * 32 * D * 2;
     if (team == 0)
-        store_rows<T, D>(out, dv, !there, 1.0f, a.dim, [&](int r) -> T * {
+        store_rows<T, D>(out, dv, !there, kLower<T>, a.dim, [&](int r) -> T * {
             return r < left ? out_of<T>(a.dv, sq.k_lo + key0 + r, kv_head) : nullptr;
         });
     if (TEAMS == 1) out += WAVES * 32 * D * 2;

@@ -65,7 +65,7 @@ struct HeadRows {
 };
 
 struct RowStats {
-    float exponent, delta;   // lse log2 e (infinite where no key is seen) and out . dout
+    float exponent, delta;   // lse log2 e (infinite where no key is seen) and out . dout, in fp16 lowered (kRaisedGrad in attention.hip)
 };
 
 struct Attention {

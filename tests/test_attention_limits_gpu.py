@@ -43,3 +43,40 @@ def test_one_row_has_no_row_stride(ops, keys, heads, kv_heads, dim, dtype):  # n
                                          *arg(dk, key_ld), *arg(dv, key_ld), ws.data_ptr(), ws.numel(), stream) == 0
         for name, a, b in zip(("dq", "dk", "dv"), (dq, dk, dv), grads):
             assert torch.equal(a, b), (name, ld)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_many_small_weights_count(ops, dtype):  # noqa: F811
+    """A key far above the others, whose weights e^-18 are below half of fp16's least number: together they are 0.2 % of the
+    output.  Half the spacing of fp16's subnormals is 2^-25, of weights that are 2^6 times their size 2^-31 for each."""
+    rows, keys, heads, dim = 8192, 131072, 4, 32   # 256 tiles of 128 queries
+    q, k, v = (torch.zeros(n, heads, dim, dtype=dtype, device="cuda") for n in (rows, keys, keys))
+    q[..., 0], k[0, :, 0], v[1:] = 4.5, 4.0, 1.0
+    out, lse = ops.attention_forward(q, k, v, offsets([rows]), offsets([keys]), scale=1.0)
+    rest = (keys - 1) * math.exp(-18)
+    want = rest / (1 + rest)
+    error = 2 * (dim + 8) * E * 18 + 8 * E * 18 + 2.0 ** -21   # of a weight, as in the bounds of test_attention_gpu
+    tol = want * (2 * U[dtype] + 2 * error + 4 * (keys + 8) * E) + (keys * 2.0 ** -31 if dtype is HF else 0.0)
+    assert (out.double() - want).abs().max() <= tol
+    assert (lse.double() - (18 + math.log1p(rest))).abs().max() <= error + (keys + 8) * E + 8 * E * 18
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,keys,far", [(4096, 256, True), (128, 166937, False), (2048, 166937, False)])
+def test_gradients_of_many_small_weights(ops, rows, keys, far, dtype):  # noqa: F811
+    """dv of weights that are 2^-26, or 100.5 times fp16's least number: each is rounded by u of itself all the same."""
+    dim = 32
+    q, k, v = (torch.zeros(n, 1, dim, dtype=dtype, device="cuda") for n in (rows, keys, keys))
+    if far:
+        q[..., 0], k[0, :, 0] = 4.5, 4.0
+    dout = torch.full_like(q, 16.0)
+    qo, ko = offsets([rows]), offsets([keys])
+    out, lse = ops.attention_forward(q, k, v, qo, ko, scale=1.0)
+    dq, dk, dv = ops.attention_backward(dout, q, k, v, out, lse, qo, ko, scale=1.0)
+    top = 18.0 if far else 0.0
+    l = top + math.log1p((keys - 1) * math.exp(-18)) if far else math.log(keys)
+    want = rows * 16 * math.exp(-l)
+    # (weights that are all alike are powers of two, and their sums below 2^24 of them exact)
+    error = 2 * (dim + 8) * E * top + 16 * E * l + 2.0 ** -20 + ((keys + 8) * E if far else 0.0)
+    assert (dv[1:].double() - want).abs().max() <= want * (2 * U[dtype] + 2 * error + 2 * (rows + 8) * E)
+    assert (dq == 0).all() and (dk == 0).all()   # values of 0
