@@ -162,7 +162,8 @@ pase_status pase_softmax_loss_backward_parts(int dtype, uint64_t rows, uint64_t 
  * finite may reach every query of its sequence, also past the causal limit.
  * scale: positive.  Weights exp(s_ij - lse_i) are rounded to dtype before they
  * multiply the values (in fp16 those below 2^-20 of the greatest so far by up to 2^-31 of it).  workspace: pase_attention_workspace() bytes, 16-byte
- * aligned.  No output may be an input; rows x heads and key_rows x kv_heads are at most 2^30 - 1024. */
+ * aligned.  No output may be an input; rows x heads and key_rows x kv_heads are at most 2^30 - 1024,
+ * heads 65536, sequences x kv_heads 2^30, and ld* 2^22. */
 pase_status pase_attention_forward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
                                    uint32_t kv_heads, uint32_t dim, const void *q, uint64_t ldq, uint64_t hsq,
                                    const void *k, uint64_t ldk, uint64_t hsk, const void *v, uint64_t ldv, uint64_t hsv,

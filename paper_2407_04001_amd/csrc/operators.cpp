@@ -193,9 +193,10 @@ pase_status check_attention(int dtype, uint64_t rows, uint64_t key_rows, uint32_
     if (heads > 65536) return refuse(PASE_ERR_TOO_LARGE, "%u heads, above 65536", heads);
     if (rows > kMaxAttentionRows / heads || key_rows > kMaxAttentionRows / kv_heads)
         return refuse(PASE_ERR_TOO_LARGE, "rows x heads above 2^30 - 1024");
-    // workgroups are counted in 32 bits
-    const uint64_t most = (rows > key_rows ? rows : key_rows) * (heads / kv_heads) / 32 + sequences + 2;
-    if (most * kv_heads >= 1ull << 31) return refuse(PASE_ERR_TOO_LARGE, "too many sequences x heads");
+    // workgroups are counted in 32 bits: tiles of at least 32 rows of a query's heads, of 64 keys
+    const uint64_t query_tiles = rows * (heads / kv_heads) / 32, key_tiles = key_rows / 64;
+    const uint64_t most = (query_tiles > key_tiles ? query_tiles : key_tiles) + sequences + 2;
+    if (most * kv_heads >= 1ull << 31) return refuse(PASE_ERR_TOO_LARGE, "sequences x kv_heads of 2^31 workgroups or more");
     return PASE_OK;
 }
 

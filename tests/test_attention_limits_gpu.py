@@ -80,3 +80,19 @@ def test_gradients_of_many_small_weights(ops, rows, keys, far, dtype):  # noqa: 
     error = 2 * (dim + 8) * E * top + 16 * E * l + 2.0 ** -20 + ((keys + 8) * E if far else 0.0)
     assert (dv[1:].double() - want).abs().max() <= want * (2 * U[dtype] + 2 * error + 2 * (rows + 8) * E)
     assert (dq == 0).all() and (dk == 0).all()   # values of 0
+
+
+def test_many_kept_keys_of_one_large_group(ops):  # noqa: F811
+    """2^29 keys under 128 heads that share them: their rows x heads are within the limit."""
+    keys, heads = 1 << 29, 128
+    k, v = torch.zeros(keys, 1, 2, dtype=BF, device="cuda"), torch.ones(keys, 1, 2, dtype=BF, device="cuda")
+    k[-1, 0, 0], v[-1] = 40.0, 3.0
+    q = torch.zeros(1, heads, 2, dtype=BF, device="cuda")
+    q[0, 64:, 0] = 1.0
+    out, lse = ops.attention_forward(q, k, v, offsets([1]), torch.tensor([0, keys], dtype=torch.int32, device="cuda"), causal=True, scale=1.0)
+    # half of the heads see all keys alike, the others the last one: e^40 against 2^29
+    assert (out[0, :64] == 1).all() and (out[0, 64:] == 3).all()
+    want = torch.tensor([29 * math.log(2)] * 64 + [40 + math.log1p((keys - 1) * math.exp(-40))], dtype=torch.double, device="cuda")
+    got = lse[:65, 0].double()
+    assert ((got - want).abs() <= 16 * E * want + 2.0 ** -20).all()
+    assert (lse[65:, 0] == lse[64, 0]).all()
