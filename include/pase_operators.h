@@ -198,8 +198,8 @@ pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows,
  *     (a, b) -> magnitude (a cos t_i - b sin t_i, a sin t_i + b cos t_i).
  * Pair i < turned / 2 is elements i and i + turned / 2, or (interleaved) 2 i and 2 i + 1; the
  * elements from `turned` on (even, at most dim and 1024) are copied.  inverse = 1 turns the other way: the
- * gradient of x from that of y.  x, y: [rows, heads, dim]; y may be x (same
- * strides).  positions: device array [rows], int32 (positions_64 = 0) or int64 (1).
+ * gradient of x from that of y.  x, y: [rows, heads, dim], heads x dim and ld* at most 2^22; y may be x
+ * (same strides), and overlap it no other way.  positions: device array [rows], int32 (positions_64 = 0) or int64 (1).
  * frequencies: fp64 device array [turned / 2]; angles are formed in fp64. */
 pase_status pase_rotary(int dtype, uint64_t rows, uint32_t heads, uint32_t dim, uint32_t turned, int interleaved,
                         int inverse, const void *x, uint64_t ldx, uint64_t hsx, const void *positions, int positions_64,

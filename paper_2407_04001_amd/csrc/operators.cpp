@@ -235,6 +235,25 @@ HeadRows head_rows(const void *p, uint64_t ld, uint64_t hs, uint64_t rows, uint6
     return {const_cast<void *>(p), (int64_t)(rows <= 1 ? dim : ld), (int64_t)(heads == 1 ? dim : hs)};
 }
 
+// Whether x and y, [rows, heads, dim] of the same strides, have elements in common.  Such elements are i rows,
+// j heads and e elements apart, i ld + j hs + e = y - x; the outer distance is not below all that lies
+// inside it, so that i (and then j) can only be the quotient or one more.
+bool overlap(const void *x, const void *y, int bytes, uint64_t ld, uint64_t hs, uint64_t rows, uint64_t heads, uint64_t dim) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+    const uint64_t apart = (p < q ? q - p : p - q) / (uint64_t)bytes;
+    const bool rows_outside = heads == 1 || (rows > 1 && ld >= hs);
+    const uint64_t outer = rows_outside ? ld : hs, outers = rows_outside ? rows : heads;
+    const uint64_t inner = rows_outside ? hs : ld, inners = rows_outside ? heads : rows;
+    const auto near = [](uint64_t at, uint64_t step) { return at < step ? step - at : at - step; };
+    const uint64_t i = outers > 1 ? apart / outer : 0;
+    for (uint64_t m = i; m <= i + 1 && m < outers; m++) {
+        const uint64_t left = near(apart, m * outer), j = inners > 1 ? left / inner : 0;
+        for (uint64_t n = j; n <= j + 1 && n < inners; n++)
+            if (near(left, n * inner) < dim) return true;
+    }
+    return false;
+}
+
 uint64_t attention_bytes(uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads,
                          uint32_t dim) {
     const uint64_t splits = (uint64_t)attention_splits((int64_t)rows, (int64_t)key_rows, (int)sequences, (int)heads, (int)kv_heads);
@@ -556,6 +575,8 @@ pase_status pase_rotary(int dtype, uint64_t rows, uint32_t heads, uint32_t dim, 
     REQUIRE_HEADS(x, ldx, hsx, rows, heads, dim, dtype);
     REQUIRE_HEADS(y, ldy, hsy, rows, heads, dim, dtype);
     REQUIRE(x != y || (ldx == ldy && hsx == hsy), "y is x with other strides");
+    if (x != y && (rows == 1 || ldx == ldy) && (heads == 1 || hsx == hsy))
+        REQUIRE(!overlap(x, y, element_bytes(dtype), ldx, hsx, rows, heads, dim), "y overlaps x in part");
     REQUIRE(positions, "positions is null");
     REQUIRE(positions_64 == 0 || positions_64 == 1, "positions_64 is neither 0 nor 1");
     REQUIRE(aligned(positions, positions_64 ? 8 : 4), "positions is not aligned to its element");

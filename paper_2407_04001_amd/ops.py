@@ -428,13 +428,13 @@ def rotary_forward(x, positions, frequencies, interleaved: bool = False, magnitu
 
     x: [rows, heads, dim], any distances between rows and heads; positions: [rows], int32 or
     int64; frequencies: float64 [turned / 2] (`rotary_frequencies`).  Pairs are elements i and i + turned / 2,
-    or (interleaved) 2 i and 2 i + 1; the elements from `turned` on stay.  out may be x."""
+    or (interleaved) 2 i and 2 i + 1; the elements from `turned` on stay.  out may be x, or a tensor with no element of x."""
     return _rotary(x, positions, frequencies, interleaved, magnitude, out, 0)
 
 
 @_on_device("dy")
 def rotary_backward(dy, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0, out=None):
-    """dx of `rotary_forward`: the same turned the other way.  out may be dy."""
+    """dx of `rotary_forward`: the same turned the other way.  out may be dy, or a tensor with no element of it."""
     return _rotary(dy, positions, frequencies, interleaved, magnitude, out, 1)
 
 

@@ -23,3 +23,18 @@ MOST = (1 << 30) - 1024   # rows x heads, key rows x kv heads
 def test_sizes_up_to_the_documented_ones(lib, rows, keys, sequences, heads, kv_heads, status, backward):  # noqa: F811
     need = C.c_uint64()
     assert lib.pase_attention_workspace(BF16, rows, keys, sequences, heads, kv_heads, 2, backward, C.byref(need)) == status
+
+
+@pytest.mark.parametrize("rows,heads,dim,ld,hs", [(4, 2, 8, 16, 8), (4, 2, 8, 40, 12), (4, 3, 8, 8, 40), (5, 1, 8, 11, 0), (1, 4, 6, 0, 9), (1, 1, 8, 0, 0),
+                                                  (3, 4, 2, 50, 5), (6, 2, 8, 16, 120)])
+def test_rotation_onto_a_part_of_x(lib, rows, heads, dim, ld, hs):  # noqa: F811
+    """Refused where x and y have an element in common (here the next refusal, of the positions, stands for what passes)."""
+    x = {r * ld + h * hs + e for r in range(rows) for h in range(heads) for e in range(dim)}
+    assert len(x) == rows * heads * dim
+    at = 1 << 20
+    for d in range(-max(x) - 3, max(x) + 4):
+        args = {**ROT, "rows": rows, "heads": heads, "dim": dim, "turned": 2, "x": at, "ldx": ld, "hsx": hs, "y": at + 2 * d, "ldy": ld, "hsy": hs,
+                "positions": None}
+        assert lib.pase_rotary(*args.values()) == INVALID
+        shared = d and not x.isdisjoint({e + d for e in x})
+        assert lib.pase_operator_error() == (b"y overlaps x in part" if shared else b"positions is null"), d

@@ -96,3 +96,23 @@ def test_many_kept_keys_of_one_large_group(ops):  # noqa: F811
     got = lse[:65, 0].double()
     assert ((got - want).abs() <= 16 * E * want + 2.0 ** -20).all()
     assert (lse[65:, 0] == lse[64, 0]).all()
+
+
+def test_out_that_overlaps_x_is_refused(ops):  # noqa: F811
+    """rotary's out is x, or has no element of it."""
+    f = ops.rotary_frequencies(8)
+    b = rand(gen(211), 40, 6, 8, dtype=BF)
+    kept, pos = b.clone(), torch.arange(20, device="cuda")
+    x = b[:20, :4]
+    for out in (b[1:21, :4], b[19:39, :4], b[:20, 1:5], b[:20, 2:6], b[1:21, 1:5]):
+        assert refused(ops, lambda: ops.rotary_forward(x, pos, f, out=out))
+        assert refused(ops, lambda: ops.rotary_backward(out, pos, f, out=x))
+    flat = b.view(-1)
+    assert refused(ops, lambda: ops.rotary_forward(x, pos, f, out=torch.as_strided(flat, (20, 4, 8), (48, 8, 1), 4)))
+    assert torch.equal(b, kept)
+    # no element in common: other rows, other heads of the same rows, the other half of wider heads
+    for x, out in ((b[:20], b[20:]), (b[20:], b[:20]), (b[:20, :3], b[:20, 3:]), (b[:20, 4:], b[:20, 1:3]),
+                   (torch.as_strided(flat, (20, 2, 8), (48, 16, 1), 0), torch.as_strided(flat, (20, 2, 8), (48, 16, 1), 8))):
+        want = ops.rotary_forward(x, pos, f)
+        assert ops.rotary_forward(x, pos, f, out=out) is out
+        assert torch.equal(out, want)
