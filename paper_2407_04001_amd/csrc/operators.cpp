@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 namespace pase {
 namespace {
@@ -233,6 +234,16 @@ pase_status check_heads(const char *name, uint64_t ld, uint64_t hs, uint64_t row
 // to LDS tell by it what lies past the last row.
 HeadRows head_rows(const void *p, uint64_t ld, uint64_t hs, uint64_t rows, uint64_t heads, uint64_t dim) {
     return {const_cast<void *>(p), (int64_t)(rows <= 1 ? dim : ld), (int64_t)(heads == 1 ? dim : hs)};
+}
+
+// No output may be an input or another output: told where they begin alike (null: without rows).
+pase_status check_apart(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs) {
+    for (auto o = outputs.begin(); o != outputs.end(); o++) {
+        if (!*o) continue;
+        for (const void *i : inputs) REQUIRE(i != *o, "an output is an input");
+        for (auto p = outputs.begin(); p != o; p++) REQUIRE(*p != *o, "two outputs are one");
+    }
+    return PASE_OK;
 }
 
 // Whether x and y, [rows, heads, dim] of the same strides, have elements in common.  Such elements are i rows,
@@ -499,6 +510,7 @@ pase_status pase_attention_forward(int dtype, uint64_t rows, uint64_t key_rows, 
     REQUIRE_HEADS(out, ldo, hso, rows, heads, dim, dtype);
     REQUIRE(lse && aligned(lse, 4), "lse is null or not aligned to its element");
     CHECK(check_workspace(workspace, workspace_bytes, attention_bytes(rows, key_rows, sequences, heads, kv_heads, dim)));
+    CHECK(check_apart({out, lse}, {q, key_rows ? k : nullptr, key_rows ? v : nullptr}));
     Attention a{};
     a.dtype = dtype, a.offsets_64 = offsets_64, a.causal = causal;
     a.rows = (int)rows, a.key_rows = (int)key_rows, a.sequences = (int)sequences;
@@ -546,6 +558,9 @@ pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows,
         REQUIRE_HEADS(dk, lddk, hsdk, key_rows, kv_heads, dim, dtype);
         REQUIRE_HEADS(dv, lddv, hsdv, key_rows, kv_heads, dim, dtype);
     }
+    const auto queries = [=](const void *p) { return rows ? p : nullptr; };
+    const auto keys = [=](const void *p) { return key_rows ? p : nullptr; };
+    CHECK(check_apart({queries(dq), keys(dk), keys(dv)}, {queries(dout), queries(q), queries(out), queries(lse), keys(k), keys(v)}));
     Attention a{};
     a.dtype = dtype, a.offsets_64 = offsets_64, a.causal = causal;
     a.rows = (int)rows, a.key_rows = (int)key_rows, a.sequences = (int)sequences;

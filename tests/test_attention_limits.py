@@ -38,3 +38,24 @@ def test_rotation_onto_a_part_of_x(lib, rows, heads, dim, ld, hs):  # noqa: F811
         assert lib.pase_rotary(*args.values()) == INVALID
         shared = d and not x.isdisjoint({e + d for e in x})
         assert lib.pase_operator_error() == (b"y overlaps x in part" if shared else b"positions is null"), d
+
+
+def apart(args):
+    """The same call with arrays of its own for every pointer to P."""
+    at, out = 1 << 20, {}
+    for name, value in args.items():
+        out[name] = value
+        if value == P:
+            out[name], at = at, at + (1 << 16)
+    return out
+
+
+@pytest.mark.parametrize("name,good,pairs", [
+    ("pase_attention_forward", ATT_F, [("o", "q"), ("o", "k"), ("o", "v"), ("lse", "q"), ("lse", "k"), ("lse", "v"), ("lse", "o")]),
+    ("pase_attention_backward", ATT_B, [(o, i) for o in ("dq", "dk", "dv") for i in ("do", "q", "k", "v", "o", "lse")] + [("dk", "dq"), ("dv", "dq"), ("dv", "dk")]),
+])
+def test_outputs_that_are_inputs(lib, name, good, pairs):  # noqa: F811
+    good = apart(good)
+    for output, other in pairs:
+        assert getattr(lib, name)(*{**good, output: good[other]}.values()) == INVALID
+        assert lib.pase_operator_error() in (b"an output is an input", b"two outputs are one"), (output, other)
