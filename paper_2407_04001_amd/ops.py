@@ -30,6 +30,7 @@ _DTYPES = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
 NORM_MAX_WIDTH = 16384
 MAX_GROUPS = 65536
 ATTENTION_MAX_DIM = 128
+MAX_ROW_STRIDE = 1 << 22   # elements, of the products', attention's and the rotation's arguments
 
 EXPORTS = ["pase_operator_error", "pase_layer_norm_forward", "pase_layer_norm_workspace",
            "pase_layer_norm_backward", "pase_grouped_matmul_forward", "pase_grouped_matmul_workspace",
@@ -564,8 +565,10 @@ def _rows_adjacent(t):
 
 
 def _heads_adjacent(t):
-    """The same for [rows, heads, dim]."""
-    return t if t.stride(-1) == 1 and all(s >= t.shape[2] for s, n in zip(t.stride()[:2], t.shape) if n > 1) else t.contiguous()
+    """The same for [rows, heads, dim], whose rows may also be further apart than the operators take."""
+    rows, heads, dim = t.shape
+    ld, hs, step = t.stride()
+    return t if step == 1 and (rows < 2 or dim <= ld <= MAX_ROW_STRIDE) and (heads < 2 or hs >= dim) else t.contiguous()
 
 
 class _LayerNorm(torch.autograd.Function):

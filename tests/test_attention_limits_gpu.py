@@ -116,3 +116,18 @@ def test_out_that_overlaps_x_is_refused(ops):  # noqa: F811
         want = ops.rotary_forward(x, pos, f)
         assert ops.rotary_forward(x, pos, f, out=out) is out
         assert torch.equal(out, want)
+
+
+def test_gradients_whose_rows_are_far_apart(ops):  # noqa: F811
+    """Autograd may hand over a slice of a wide gradient, with rows further apart than the operators take."""
+    q, k, v, qo, ko, _ = make(251, [20, 10], [25, 15], 4, 2, 16, BF)
+    wide = torch.zeros(30, (1 << 22) + 64, dtype=BF, device="cuda")
+    dout = wide[:, 64:128].view(30, 4, 16)
+    dout.copy_(rand(gen(252), 30, 4, 16, dtype=BF))
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    out, lse = ops.attention_forward(q, k, v, qo, ko)
+    got = torch.autograd.grad(ops.attention(*leaves, qo, ko), leaves, dout)
+    assert all(torch.equal(a, b) for a, b in zip(got, ops.attention_backward(dout.contiguous(), q, k, v, out, lse, qo, ko)))
+    f, pos = ops.rotary_frequencies(16), torch.arange(30, device="cuda")
+    got, = torch.autograd.grad(ops.rotary(leaves[0], pos, f), leaves[0], dout)
+    assert torch.equal(got, ops.rotary_backward(dout.contiguous(), pos, f))
