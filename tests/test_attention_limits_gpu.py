@@ -131,3 +131,26 @@ def test_gradients_whose_rows_are_far_apart(ops):  # noqa: F811
     f, pos = ops.rotary_frequencies(16), torch.arange(30, device="cuda")
     got, = torch.autograd.grad(ops.rotary(leaves[0], pos, f), leaves[0], dout)
     assert torch.equal(got, ops.rotary_backward(dout.contiguous(), pos, f))
+
+
+# Offsets for which tiles of keys are dealt by place (four teams: at least 16 steps of the average sequence; keys of 16 tiles of 64 a
+# sequence) with ranges in both halves of the search, that is 63 to 126 sequences.
+BY_PLACE = [
+    ([520] * 100 + [900], [1100] * 101, 2, 1, 32, {"room": 1}),
+    ([520] * 62 + [530], [1030 + 37 * (i % 5) for i in range(63)], 1, 1, 64, {}),
+    ([18 * (i % 62) for i in range(126)], [19 * ((i * 7) % 126) for i in range(126)], 1, 1, 64, {"before": 3, "after": 2}),
+    ([0] * 80 + [412] + [0] * 20, [0] * 40 + [70] * 40 + [102000] + [1] * 20, 128, 1, 64, {}),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("case", BY_PLACE, ids=[f"{len(c[0])}_h{c[2]}-{c[3]}_d{c[4]}" for c in BY_PLACE])
+def test_keys_of_many_long_sequences(ops, case, dtype):  # noqa: F811
+    *sizes, rest = case
+    n, group, step = len(sizes[0]), sizes[2] // sizes[3], 64 if sizes[4] == 32 else 32
+    q, k, v, qo, ko, kl = make(221, *sizes, dtype, **rest)
+    assert q.shape[0] // n * group // step >= 16 and 64 < n + 2 <= 128 and k.shape[0] >= 16 * 64 * n
+    dout = rand(gen(222), *q.shape, dtype=dtype, scale=0.5)
+    out, lse = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl, causal=True)
+    check_forward((out, lse), q, k, v, qo, ko, kl, True)
+    check_backward(ops.attention_backward(dout, q, k, v, out, lse, qo, ko, k_lengths=kl, causal=True), dout, q, k, v, out, lse, qo, ko, kl, True)
