@@ -154,3 +154,72 @@ def test_keys_of_many_long_sequences(ops, case, dtype):  # noqa: F811
     out, lse = ops.attention_forward(q, k, v, qo, ko, k_lengths=kl, causal=True)
     check_forward((out, lse), q, k, v, qo, ko, kl, True)
     check_backward(ops.attention_backward(dout, q, k, v, out, lse, qo, ko, k_lengths=kl, causal=True), dout, q, k, v, out, lse, qo, ko, kl, True)
+
+
+@pytest.mark.parametrize("rows,keys,heads,kv_heads,q_offsets,k_offsets", [
+    (100, 120, 4, 2, [0, 60, 40, 100], [0, 100, 30, 120]),             # one tile each
+    (100, 120, 4, 2, [90, 50, 10, 0], [120, 80, 5, -7]),               # only decreasing
+    (4, 9000, 4, 4, [0, 3, 1, 4], [0, 8000, 500, 9000]),               # few queries: shares and their join
+    (3000, 3000, 4, 1, [0, 2500, 100, 3000], [0, 2900, 50, 3000]),     # four teams, dealt by place
+    (40, 40, 2, 2, [40, 0] * 90, [0, 40] * 90),                        # more ranges than a wave has lanes
+])
+@pytest.mark.parametrize("dim", [64, 13])
+def test_decreasing_offsets_keep_to_the_outputs(ops, rows, keys, heads, kv_heads, q_offsets, k_offsets, dim):  # noqa: F811
+    """Results are undefined there, but nothing outside the outputs is written and the calls end."""
+    L = ops.load()
+    g = gen(231)
+    n, mark = len(q_offsets) - 1, 7.5
+    q, dout = rand(g, rows, heads, dim, dtype=BF), rand(g, rows, heads, dim, dtype=BF)
+    k, v = rand(g, keys, kv_heads, dim, dtype=BF), rand(g, keys, kv_heads, dim, dtype=BF)
+    qo, ko = (torch.tensor(t, dtype=torch.int32, device="cuda") for t in (q_offsets, k_offsets))
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def room(rows, heads):
+        return torch.full((rows + 2, heads + 1, dim + 1), mark, dtype=BF, device="cuda")
+
+    def untouched(t):
+        u = t.clone()
+        u[1:-1, :-1, :dim] = mark
+        return bool((u == mark).all())
+
+    def guarded(n, dtype=torch.float32):
+        return torch.full((n + 512,), mark, dtype=dtype, device="cuda")
+
+    def place(t):
+        return arg(t[1:-1, :-1, :dim])
+
+    lse = guarded(heads * rows)
+    for backward in (0, 1):
+        need = ops._bytes("pase_attention_workspace", 0, rows, keys, n, heads, kv_heads, dim, backward)
+        ws = guarded(need // 4)
+        if not backward:
+            out = room(rows, heads)
+            assert L.pase_attention_forward(0, rows, keys, n, heads, kv_heads, dim, *arg(q), *arg(k), *arg(v), qo.data_ptr(), ko.data_ptr(), None, 0, 1,
+                                            dim ** -0.5, *place(out), lse.data_ptr(), ws.data_ptr(), need, stream) == 0
+            outs = [out]
+        else:
+            outs = [room(rows, heads), room(keys, kv_heads), room(keys, kv_heads)]
+            assert L.pase_attention_backward(0, rows, keys, n, heads, kv_heads, dim, *arg(dout), *arg(q), *arg(k), *arg(v), *place(out), lse.data_ptr(),
+                                             qo.data_ptr(), ko.data_ptr(), None, 0, 1, dim ** -0.5, *(a for t in outs for a in place(t)), ws.data_ptr(),
+                                             need, stream) == 0
+        assert all(untouched(t) for t in outs) and (lse[heads * rows:] == mark).all() and (ws[need // 4:] == mark).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_gradients_of_rotation_and_dropout_by_differences(ops, interleaved):  # noqa: F811
+    """Against central differences of the 64-bit definitions along random directions; both are linear, so that the differences are
+    exact but for 2^-53 of their terms over the step, and a gradient element is off by u of itself and its own fp32 steps."""
+    g = gen(241)
+    x, dy = rand(g, 9, 3, 26, dtype=HF), rand(g, 9, 3, 26, dtype=HF)
+    f, pos = ops.rotary_frequencies(24), torch.arange(9, device="cuda") * 100
+    seed = torch.tensor([7, 8], device="cuda")
+    keep = ops.dropout_forward(torch.ones(27, 26, device="cuda"), 0.25, seed).view(9, 3, 26) != 0   # (test_dropout has the mask from its definition)
+    for dx, value in ((ops.rotary_backward(dy, pos, f, interleaved=interleaved, magnitude=1.25), lambda t: rotary64(t, pos, f, interleaved, 1.25)),
+                      (ops.dropout_backward(dy.view(27, 26), 0.25, seed).view(9, 3, 26), lambda t: torch.where(keep, t / 0.75, 0.0))):
+        for _ in range(3):
+            d = torch.randn(x.shape, generator=g, device="cuda", dtype=torch.double)
+            e = 2.0 ** -10
+            slope = ((value(x.double() + e * d) - value(x.double() - e * d)) * dy.double()).sum() / (2 * e)
+            # the rotation's terms are at most 1.25 (|a| + |b|)
+            size = (2 * 1.25 * dy.double().abs().amax() * d.abs()).sum()
+            assert (slope - (dx.double() * d).sum()).abs() <= (U[HF] + 16 * E) * (dx.double().abs() * d.abs()).sum() + 2.0 ** -20 * size
