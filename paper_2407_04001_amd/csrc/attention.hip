@@ -438,13 +438,15 @@ template <typename T, int D, int KT> struct Softmax {
             for (int d = 0; d < D / 32; d++) o[d] *= f;
         }
         const float from = m == -__builtin_inff() ? 0.0f : m * c - kRaised<T>;
+        float more = 0;   // a step's sum by itself: small weights, one by one, would vanish behind a large one before them
 #pragma unroll
         for (int b = 0; b < KT / 32; b++)
 #pragma unroll
             for (int j = 0; j < 16; j++) {
                 s[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][j], c, -from));
-                sum += s[b][j];
+                more += s[b][j];
             }
+        sum += more;
         before();
         // weights are rounded to the values' type: by up to 2^-8 (bf16) or 2^-11 of each (see kRaised), either way
 #pragma unroll

@@ -223,3 +223,20 @@ def test_gradients_of_rotation_and_dropout_by_differences(ops, interleaved):  # 
             # the rotation's terms are at most 1.25 (|a| + |b|)
             size = (2 * 1.25 * dy.double().abs().amax() * d.abs()).sum()
             assert (slope - (dx.double() * d).sum()).abs() <= (U[HF] + 16 * E) * (dx.double().abs() * d.abs()).sum() + 2.0 ** -20 * size
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,far", [(8192, 18.0), (8192, 16.5), (1, 16.5)])
+def test_long_sums_behind_a_large_weight(ops, rows, far, dtype):  # noqa: F811
+    """The weights' sum after a first one of 1: 131071 of e^-18 or e^-16.5, each below half of the last bit of 1.  A lane adds up its weights
+    of a step of keys, at most 32 of the 64, then the steps: these sums are off by E each, of less than 2."""
+    keys, heads, dim = 131072, 4, 32
+    q, k, v = (torch.zeros(n, heads, dim, dtype=dtype, device="cuda") for n in (rows, keys, keys))
+    q[..., 0], k[0, :, 0], v[:] = 1.0, far, 1.0
+    out, lse = ops.attention_forward(q, k, v, offsets([rows]), offsets([keys]), scale=1.0)
+    want = far + math.log1p((keys - 1) * math.exp(-far))
+    weight = 2 * (dim + 8) * E * far + 8 * E * far + 2.0 ** -21
+    sums = (2 * keys / 64 + 64) * E
+    assert (lse.double() - want).abs().max() <= weight * (keys - 1) * math.exp(-far) + 2.0 ** -21 + sums + 8 * E * far
+    # values of 1: the products' sum is rounded in other places, over 16 keys at a time
+    assert (out.double() - 1).abs().max() <= U[dtype] * 2 + sums + 2 * (keys / 16 + 16) * E * 2 + (keys * 2.0 ** -31 if dtype is HF else 0)
