@@ -182,6 +182,7 @@ pase_status pase_attention_workspace(int dtype, uint64_t rows, uint64_t key_rows
  * dk and dv summed over the heads that share them.  p and ds are recomputed, and
  * rounded to dtype before the second products (in fp16 a ds above 65504 is infinite, one
  * below 2^-25 is 0: gradients want the loss scale that training in fp16 has; a p below 2^-26 is off by up to 2^-37).  Rows of no sequence and keys past a length get 0.
+ * A value of dout that is not finite may, as others, reach every row and key of its sequence.
  * No output may be an input or another output. */
 pase_status pase_attention_backward(int dtype, uint64_t rows, uint64_t key_rows, uint32_t sequences, uint32_t heads,
                                     uint32_t kv_heads, uint32_t dim, const void *dout, uint64_t lddo, uint64_t hsdo,

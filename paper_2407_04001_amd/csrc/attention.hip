@@ -467,9 +467,9 @@ template <typename T, int D, int KT> struct Softmax {
 // multiplies while another takes its exponents.  Per score 4 D operations of the matrix
 // units and, in a lane, a maximum, a multiply-add, an exponential (a quarter of their rate), an addition and
 // half a conversion: at 128 columns both take about as long, at 64 the lanes twice.  Long causal sequences
-// (16384 rows in 4, 16 heads of 128 to 4) 321 us, 930 TFLOP/s (an 8192^3 library product 1170-1245); 4 x 4096, 16 heads
-// of 64, 861 TFLOP/s without the causal limit.  64 x 256 rows, 16 heads of 64: 44 us for 134 MB, waiting for loads
-// half of a wave's time, as a workgroup has four steps only.  Three steps in LDS (and so three
+// (16384 rows in 4, 16 heads of 128 to 4) 324 us, 923 TFLOP/s (an 8192^3 library product 1170-1245); 4 x 4096, 16 heads
+// of 64, 861 TFLOP/s without the causal limit.  64 x 256 rows, 16 heads of 64: 46 us for 134 MB, waiting for loads
+// 43 % of a wave's time, as a workgroup has four steps only (heads of 63, through registers: 88).  Three steps in LDS (and so three
 // workgroups a CU) were slower there, 49.6 us against 44.7.
 template <typename T, int D, Load LOAD>
 __global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k_forward(Attention a) {
@@ -539,7 +539,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : LOAD == kDirect ? 4 : 3) void k
 // CU: 80 us against 62 for 64 tokens over 131072 keys, 4 heads of 128).  The waves' outputs are
 // joined at the end; where tiles are still too few, a.splits workgroups share a tile's keys
 // and leave their outputs and log-sum-exps for k_join.
-// Bound by HBM: those 64 tokens 60 us for 269 MB (4.5 TB/s), and 4 us for the join; one token
+// Bound by HBM: those 64 tokens 58 us for 269 MB (4.6 TB/s), and 4 us for the join; one token
 // over 131072 keys, 2 heads, 30 us for 134 MB and 6.
 template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) void k_forward_few(Attention a) {
     constexpr bool DIRECT = LOAD != kThrough;
@@ -784,8 +784,8 @@ template <int D> struct Join {
 };
 
 // Queries along the lanes, as in the forward pass: 128 a workgroup, 64 keys a step.  Long causal sequences (16384
-// rows in 4, 16 heads of 128 to 4) 420-450 us for 448 GFLOP (1 PFLOP/s); 64 x 256 rows, 16 heads of 64 60 us
-// for 201 MB, waiting for loads two thirds of a wave's time (three steps in LDS, or four waves a SIMD, changed
+// rows in 4, 16 heads of 128 to 4) 443 us for 448 GFLOP (1 PFLOP/s), the median of 66 passes; 64 x 256 rows, 16 heads of 64 60 us
+// for 201 MB, waiting for loads 63 % of a wave's time (three steps in LDS, or four waves a SIMD, changed
 // nothing or lost 2 us).
 template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) void k_queries_grad(Attention a) {
     typedef typename Mfma<T>::Frag Frag;
@@ -889,8 +889,10 @@ template <typename T, int D, Load LOAD> __global__ __launch_bounds__(256, 2) voi
 // Loads to LDS: three steps in LDS, two on their way (128 columns: two and one); through registers: one, loaded
 // where it is needed.  With 128 columns the accumulators take 128 of a lane's 256 registers at two waves a SIMD; at
 // one wave a SIMD and 512 the compiler moved them to and from the second half in every step (2162 us for the whole
-// backward pass of 16384 rows in 4 causal sequences, 16 heads of 128 to 4, against 1647).  There 735 us for 598
-// GFLOP (814 TFLOP/s); 64 x 256 rows, 16 heads of 64 59 us.
+// backward pass of 16384 rows in 4 causal sequences, 16 heads of 128 to 4, against 1647).  There 702 us for 598
+// GFLOP (852 TFLOP/s), the median of 66 passes; 64 x 256 rows, 16 heads of 64 60 us.
+// Through registers nothing is on its way while a step is multiplied: 64 x 256 rows, 16 heads of 63 116 us, 6508 rows
+// in 2 sequences, 2 heads of 35, 319 (of 36, in four teams: 71).
 template <typename T, int D, int QT, int WAVES, int TEAMS, Load LOAD>
 __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 3) void k_keys_grad(Attention a) {
     constexpr bool DIRECT = LOAD != kThrough;
@@ -1050,7 +1052,7 @@ __global__ __launch_bounds__(TEAMS * WAVES * 64, TEAMS > 1 ? 1 : D == 128 ? 2 : 
         join.take(dk, 1, TEAMS);
         __syncthreads();
     }
-    // keys of the range that do not count get 0 (their lanes hold what a key of zeros would)
+    // keys of the range that do not count get 0 (their lanes hold another row's result, or anything)
     const int left = sq.k_rows - key0;
     char *out = lds + (team * WAVES + wave) * 32 * D * 2;
     if (team == 0)
@@ -1120,11 +1122,11 @@ template <typename T, int D, Load LOAD> int queries_grad(Attention a, void *stre
 
 // Tiles of 128 keys on one team, or of 64 on four.  Four share a tile's steps: with few tiles and many steps, as
 // where long sequences share heads, no CU waits long for the longest tile's (4 causal sequences, 16384
-// rows, 16 heads of 128 to 4: 736 us against 1185); with many tiles one team has two workgroups a CU (64 x
-// 256 rows, 16 heads of 64: 59 us against 100), and so with few steps, where joining costs as much (59 x 16
-// rows, 16 heads of 128, both kernels: 58 us against 82).  Several sequences of sixteen tiles or more are dealt by
-// place (the long ones again, whole backward pass: 1193 us against 1135; forward and dq, whose tiles are
-// shorter, gained 1 % there and lost 6 on 4 sequences of 680 rows).
+// rows, 16 heads of 128 to 4: 702 us against 1108 on one); with many tiles one team has two workgroups a CU (64 x
+// 256 rows, 16 heads of 64: 60 us against 148 on four), and so with few steps, where joining costs as much (59 x 16
+// rows, 16 heads of 128, both kernels: 38 us against 57).  Several sequences of sixteen tiles or more are dealt by
+// place (the long ones again: 702 us against 746 in their order; forward and dq, whose tiles are
+// shorter, gained 1 % there and lost 6 on 4 sequences of 680 rows).  Medians of 66 passes.
 template <typename T, int D, Load LOAD> int keys_grad(Attention a, void *stream) {
     if (!a.key_rows) return 0;
     constexpr int QT = D == 32 ? 64 : 32;

@@ -349,7 +349,7 @@ def attention_forward(q, k, v, q_offsets, k_offsets, k_lengths=None, causal: boo
     that the last one sees all, as where new tokens follow kept ones.
 
     q: [rows, heads, dim]; k, v: [key rows, kv heads, dim], each read by heads / kv heads heads next to each
-    other; any distances between rows and heads.  Offsets and lengths: int32 or int64,
+    other; rows and heads any distance apart that keeps them from overlapping (rows up to 2 ** 22).  Offsets and lengths: int32 or int64,
     alike, on the device.  scale: dim ** -0.5 unless given.  out: [rows, heads, dim];
     lse: float32 [heads, rows].  Queries that see no key, and rows of no sequence, have out 0
     and lse -inf."""
@@ -391,7 +391,7 @@ def rotary_frequencies(turned: int, base: float = 10000.0, factor: float = 1.0, 
                        fast: float = 32.0, device="cuda"):
     """Frequencies of the turned / 2 pairs for `rotary`, float64: base ** (-2 i / turned), divided by
     `factor` for sequences that many times as long.  With `trained`, the length trained on, by
-    parts: pairs that turn more than `fast` times over that length keep their
+    parts (Peng, Quesnelle, Fan, Shippole 2023): pairs that turn more than `fast` times over that length keep their
     frequency, those below `slow` turns are divided, those between are mixed in proportion to their turns."""
     if turned < 2 or turned % 2:
         _refuse(f"{turned} elements cannot be turned in pairs")
@@ -427,7 +427,7 @@ def _rotary(x, positions, frequencies, interleaved, magnitude, out, inverse):
 def rotary_forward(x, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0, out=None):
     """Turns pair i of every head of row t by the angle positions[t] * frequencies[i], times magnitude.
 
-    x: [rows, heads, dim], any distances between rows and heads; positions: [rows], int32 or
+    x: [rows, heads, dim], rows and heads as for attention; positions: [rows], int32 or
     int64; frequencies: float64 [turned / 2] (`rotary_frequencies`).  Pairs are elements i and i + turned / 2,
     or (interleaved) 2 i and 2 i + 1; the elements from `turned` on stay.  out may be x, or a tensor with no element of x."""
     return _rotary(x, positions, frequencies, interleaved, magnitude, out, 0)
